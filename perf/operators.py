@@ -118,14 +118,14 @@ def _ints(values):
 
 
 def _frequencies(c):
-    """float64 on the host: radians per position of every pair, base^(-2i/rotary); with a factor, slow ones (less than one turn in
+    """float64: radians per position of every pair, base^(-2i/rotary); with a factor, slow ones (less than one turn in
     8192 positions) divided by it, fast ones (more than four) kept, between them a blend."""
     f = [c["base"] ** (-2.0 * i / c["rotary"]) for i in range(c["rotary"] // 2)]
     factor = c.get("factor", 1.0)
     if factor != 1.0:
         blend = [min(1.0, max(0.0, (8192 * x / (2 * math.pi) - 1.0) / 3.0)) for x in f]
         f = [x * b + x / factor * (1.0 - b) for x, b in zip(f, blend)]
-    return torch.tensor(f, dtype=torch.float64)
+    return torch.tensor(f, dtype=torch.float64, device="cuda")
 
 
 def _outside_layout(c, x):
@@ -328,7 +328,7 @@ def _turn(x, cos, sin, pairs, back=False):
 
 
 def _angles(st, pos):
-    angle = pos.double()[..., None] * st["freqs"].to("cuda")
+    angle = pos.double()[..., None] * st["freqs"]
     return angle.cos().float(), angle.sin().float()
 
 

@@ -16,10 +16,10 @@
  *     ordinary host memory.  The caller owns every buffer, including workspaces; the library
  *     allocates no device memory and keeps no state between calls (the fixed scratch array of
  *     sepattn_decode_noalloc and a counter that numbers launches aside).
- *   - Alignment: token_ids, Q, K, V, O, dO, dQ, dK, dV, q, Kc, Vc, out, k_new, v_new and rope tables
+ *   - Alignment: token_ids, Q, K, V, O, dO, dQ, dK, dV, q, Kc, Vc, Kp, Vp, out, k_new, v_new and rope tables
  *     must be 16-byte aligned, is_sep 4-byte aligned, workspaces 256-byte aligned; a misaligned
  *     buffer is refused with SEPATTN_ERR_PARAM (workspaces: SEPATTN_ERR_WORKSPACE).
- *   - Tensors are dense and contiguous with the head dimension d innermost.
+ *   - Tensors are dense and contiguous with the head dimension d innermost (sepattn_rope takes strides).
  *   - `stream` is a hipStream_t passed as void* (NULL = the default stream).  Calls validate their
  *     arguments synchronously, enqueue their kernels on `stream` and return without waiting.
  *     Nothing is enqueued when a validation error (any status but SEPATTN_ERR_HIP) is returned.
@@ -229,6 +229,61 @@ int sepattn_backward_headwise(const sepattn_params *p, const int32_t *n_per_head
                               size_t ws_bytes, void *stream);
 
 /* ------------------------------------------------------------------------------------------
+ * Rotary positions in front of the attention (the backbones of Sec. 4.1 encode positions by turning pairs of dimensions
+ * of q and k).  Pair p of a row at position t is turned by the angle t * freqs[p]:
+ *     (x, y) -> (x cos - y sin, y cos + x sin),   p < rotary_dim / 2,
+ * with (x, y) the dimensions (p, p + rotary_dim/2), or (2p, 2p+1) where `interleaved`; dimensions from rotary_dim on stay.
+ * Angles are formed in fp64 (any int32 position), cos / sin and the turn in fp32, and each result is rounded once.
+ * sepattn_rope also lays the tensors out: it reads q, k, v with any strides (as a projection leaves them, token by token)
+ * and writes Q, K, V with any others (dense [B, H, L, d] for sepattn_forward); V is copied bit for bit.
+ * sepattn_rope_backward is its gradient, i.e. the turn by the opposite angles: from dQ, dK, dV as
+ * sepattn_backward writes them to the gradients of q, k, v in the projections' layout.
+ *   p->rotary_dim   even, 2 <= rotary_dim <= d (SEPATTN_ERR_PARAM otherwise)
+ *   freqs      DEVICE fp64 [rotary_dim/2]  radians per position (sepattn_rope_frequencies, or the caller's own), 8-byte aligned
+ *   positions  DEVICE int32 [B, L], or NULL: a token's index in its row, minus doc_start if that is given
+ *   doc_start  DEVICE int32 [B, L] as from sepattn_doc_bounds (positions start anew with every document), or NULL;
+ *              not together with positions (SEPATTN_ERR_PARAM)
+ *   strides    HOST, elements between neighbours in the batch, head and token dimension (the head dimension is
+ *              contiguous); NULL: dense [B, H, L, d].  Rows are 16-byte aligned: pointers, and strides of dimensions larger
+ *              than 1 in bytes, are multiples of 16.  Inputs may be broadcast (stride 0); the rows of an output must not overlap
+ *              (SEPATTN_ERR_PARAM, as for a negative stride)
+ *   v, V       both NULL where the values are laid out already (dv, dV likewise)
+ * An output may be its own input (same pointer and strides: in place); otherwise outputs must not overlap inputs.
+ * ------------------------------------------------------------------------------------------ */
+typedef struct {
+    int B;           /* sequences                                                              */
+    int Hq;          /* query heads                                                            */
+    int Hkv;         /* key/value heads (any number: heads are independent here)                */
+    int L;           /* tokens per sequence                                                    */
+    int d;           /* head dimension: 64 or 128                                              */
+    int rotary_dim;  /* leading dimensions of a head that are turned                           */
+    int interleaved; /* 0: dimension p pairs with p + rotary_dim/2; 1: 2p with 2p + 1           */
+    int dtype;       /* sepattn_dtype of all tensors                                           */
+} sepattn_rope_params;
+typedef struct {
+    int64_t b, h, l;
+} sepattn_strides;
+
+/* Frequencies for contexts longer than the trained one.  freqs HOST fp64 [rotary_dim/2] out:
+ *   f_p = base^(-2p/rotary_dim),
+ *   original_length == 0: f_p / factor (all positions interpolated); low and high are not looked at
+ *   original_length >  0: by the turns w = original_length * f_p / 2pi that a pair makes over the trained context:
+ *                         w <= low: f_p / factor, w >= high: f_p, between: f_p ((1 - g) / factor + g), g = (w - low) / (high - low)
+ * base > 1, factor >= 1, 0 <= low < high (SEPATTN_ERR_PARAM).  factor 1 gives f_p.  (A method that also scales the logits does
+ * so through `scale` of the attention calls.) */
+int sepattn_rope_frequencies(int rotary_dim, double base, double factor, double low, double high, int original_length,
+                             double *freqs);
+int sepattn_rope(const sepattn_rope_params *p, const double *freqs, const int32_t *positions, const int32_t *doc_start,
+                 const void *q, const sepattn_strides *q_strides, const void *k, const sepattn_strides *k_strides,
+                 const void *v, const sepattn_strides *v_strides, void *Q, const sepattn_strides *Q_strides, void *K,
+                 const sepattn_strides *K_strides, void *V, const sepattn_strides *V_strides, void *stream);
+int sepattn_rope_backward(const sepattn_rope_params *p, const double *freqs, const int32_t *positions,
+                          const int32_t *doc_start, const void *dQ, const sepattn_strides *dQ_strides, const void *dK,
+                          const sepattn_strides *dK_strides, const void *dV, const sepattn_strides *dV_strides, void *dq,
+                          const sepattn_strides *dq_strides, void *dk, const sepattn_strides *dk_strides, void *dv,
+                          const sepattn_strides *dv_strides, void *stream);
+
+/* ------------------------------------------------------------------------------------------
  * Streaming generation on the four-block KV cache (Sec. 3.3).
  * Cache layout, per (sequence, KV head): c slots of d values,
  *     [0, a)       Initial Cache
@@ -295,6 +350,9 @@ int sepattn_decode(const sepkv_params *p, const void *q, const void *Kc, const v
  *       runs (same stream, or synchronised).
  */
 int sepkv_rope_table(int n_pos, int d, double base, float *table, void *stream);
+/* The same table for frequencies of the caller's (contexts longer than the trained one): freqs DEVICE fp64 [d/2], radians per
+ * position, as sepattn_rope_frequencies(d, ...) gives them; 8-byte aligned. */
+int sepkv_rope_table_frequencies(int n_pos, int d, const double *freqs, float *table, void *stream);
 int sepattn_decode_rope(const sepkv_params *p, const void *q, const void *Kc, const void *Vc,
                         const int32_t *sizes, const float *rope_table, int n_pos, void *out,
                         float *lse, void *ws, size_t ws_bytes, void *stream);
@@ -331,6 +389,17 @@ int sepattn_decode_noalloc(const sepkv_params *p, const void *q, const void *Kc,
 int sepkv_append(const sepkv_params *p, const void *k_new, const void *v_new,
                  const uint8_t *is_sep_new, void *Kc, void *Vc, uint8_t *win_is_sep,
                  int32_t *sizes, void *stream);
+
+/* The same for a token whose query and key are not turned yet, for caches whose keys carry the positions of the text: q and k_new
+ * are turned by positions[s] (conventions of sepattn_rope), the query goes to q_out, the key and v_new enter the
+ * cache as in sepkv_append, in one launch.  A sequence whose window region is full gets its query and keeps its cache.
+ *   freqs      DEVICE fp64 [rotary_dim/2], 8-byte aligned;  positions  DEVICE int32 [S]
+ *   q          DEVICE dtype [S, Hq, d];  q_out  DEVICE dtype [S, Hq, d]  out, may be q
+ */
+int sepkv_append_rope(const sepkv_params *p, int rotary_dim, int interleaved, const double *freqs,
+                      const int32_t *positions, const void *q, const void *k_new, const void *v_new,
+                      const uint8_t *is_sep_new, void *q_out, void *Kc, void *Vc, uint8_t *win_is_sep, int32_t *sizes,
+                      void *stream);
 
 /* Compression step (Sec. 3.3; caption of the streaming-design figure): the separators of the Past
  * Window Cache are appended to the Separator Cache, its other entries are dropped, and the Local
@@ -385,6 +454,51 @@ int sepkv_fill_from_prefill_zeroed(const sepkv_params *p, int L, int nw, const v
                                    int32_t *sizes, void *stream);
 
 /* ------------------------------------------------------------------------------------------
+ * Generation behind shared prompts.  Sequences that begin with the same prompt keep its entries once: G prefix caches, each a
+ * four-block cache of the layout above that is filled once (sepkv_fill_from_prefill, or a prompt kept whole in the
+ * window of a cache with a = s = 0, w = 1, c = its length) and not written afterwards, beside a cache of its own per sequence for
+ * what follows.  A sequence attends to all entries of its prefix and all of its own: Eq. 1 with M = 1 over both.
+ *
+ * sepkv_group_sequences lists the sequences by prefix, once per batch (the list serves all layers and tokens):
+ *   prefix_of    DEVICE int32 [S]    prefix of each sequence, 0 <= prefix_of[s] < G, or anything else: none
+ *   group_start  DEVICE int32 [G+1]  out: sequences of prefix g are entries group_start[g] .. group_start[g+1]-1 of
+ *   group_seq    DEVICE int32 [S]    out: ascending within a prefix; entries from group_start[G] on are 0
+ *   S, G <= 65535 (SEPATTN_ERR_SHAPE)
+ *
+ * sepattn_decode_shared: as sepattn_decode, plus
+ *   pp           sepkv_params of the prefix caches: pp->S = G; Hq, Hkv, d, dtype, scale as in p (SEPATTN_ERR_SHAPE if sizes,
+ *                SEPATTN_ERR_DTYPE if d or dtype differ; pp->scale is not looked at)
+ *   Kp, Vp       DEVICE dtype [G, Hkv, pp->c, d];  prefix_sizes  DEVICE int32 [G, 6]
+ *   prefix_of, group_start, group_seq   DEVICE, as above (values outside their ranges give wrong results, never an access out of
+ *                bounds)
+ *   ws           DEVICE, >= sepattn_decode_shared_workspace_bytes(p, pp) bytes, 256-byte aligned; may hold anything.
+ *                Calls that overlap in time need a workspace each
+ * A sequence without any entry, own or of a prefix, yields out = 0, lse = -inf.
+ *
+ * sepattn_decode_shared_rope: with positions within the caches (see sepattn_decode_rope): the entries of a sequence's prefix,
+ * oldest first, are at positions 0 .. np-1, its own at np .. np+nv-1, the query at np+nv-1.  The positions of a
+ * prefix never change, so its keys are turned once, by sepkv_rope_cache, and Kp holds them turned; own keys and q are
+ * stored without encoding.  rope_table needs n_pos >= pp->c + p->c rows (SEPATTN_ERR_SHAPE).  Turned values count with 16 bits or
+ * more of mantissa, so that lse holds to 1e-5 here.
+ *   sepkv_rope_cache: the key of the entry of rank e (oldest first) is turned by table row e, for all valid entries of
+ *                Kc DEVICE dtype [S, Hkv, c, d] -> K_out, of the same shape, which may be Kc (in place: once).  Slots without a
+ *                valid entry are not written.  n_pos >= c.
+ * ------------------------------------------------------------------------------------------ */
+int sepkv_group_sequences(const int32_t *prefix_of, int S, int G, int32_t *group_start, int32_t *group_seq, void *stream);
+int sepkv_rope_cache(const sepkv_params *p, const int32_t *sizes, const float *rope_table, int n_pos, const void *Kc, void *K_out,
+                     void *stream);
+size_t sepattn_decode_shared_workspace_bytes(const sepkv_params *p, const sepkv_params *pp);
+int sepattn_decode_shared(const sepkv_params *p, const sepkv_params *pp, const void *q, const void *Kc, const void *Vc,
+                          const int32_t *sizes, const void *Kp, const void *Vp, const int32_t *prefix_sizes,
+                          const int32_t *prefix_of, const int32_t *group_start, const int32_t *group_seq, void *out,
+                          float *lse, void *ws, size_t ws_bytes, void *stream);
+int sepattn_decode_shared_rope(const sepkv_params *p, const sepkv_params *pp, const void *q, const void *Kc, const void *Vc,
+                               const int32_t *sizes, const void *Kp, const void *Vp, const int32_t *prefix_sizes,
+                               const int32_t *prefix_of, const int32_t *group_start, const int32_t *group_seq,
+                               const float *rope_table, int n_pos, void *out, float *lse, void *ws, size_t ws_bytes,
+                               void *stream);
+
+/* ------------------------------------------------------------------------------------------
  * Measurement hooks (not part of the method).  A benchmark that times whole steps can also report one
  * kernel's own duration: it creates a handle for that kernel, attaches it to the thread that makes
  * the library calls, and from then on every launch of the kernel by that thread is bracketed by a
@@ -394,6 +508,8 @@ int sepkv_fill_from_prefill_zeroed(const sepkv_params *p, int L, int nw, const v
  * same time; one handle must not be attached to two threads.
  * Every launch is recorded under one id.  Where the backward of a small bf16 call runs dQ and dK/dV side by side in one launch, that
  * launch counts as SEPATTN_K_BWD_DKV, and SEPATTN_K_BWD_DQ is the short one in front of it that forms the row values.
+ * The launches of sepattn_decode_shared count as SEPATTN_K_DECODE_SPLIT and SEPATTN_K_DECODE_MERGE, that of sepkv_append_rope as
+ * SEPATTN_K_CACHE_APPEND; sepattn_rope, sepkv_rope_cache and sepkv_group_sequences have no id.
  *   sepattn_profile_create   kernel: a sepattn_kernel_id; max_records: events are created up front
  *                            for this many launches, further launches are not recorded;
  *                            *out receives the handle (HOST)

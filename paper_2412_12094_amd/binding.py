@@ -57,6 +57,16 @@ EXPORTS = (
     "sepkv_rope_table",
     "sepattn_decode_rope",
     "sepkv_append",
+    "sepattn_rope_frequencies",
+    "sepattn_rope",
+    "sepattn_rope_backward",
+    "sepkv_rope_table_frequencies",
+    "sepkv_append_rope",
+    "sepkv_group_sequences",
+    "sepkv_rope_cache",
+    "sepattn_decode_shared_workspace_bytes",
+    "sepattn_decode_shared",
+    "sepattn_decode_shared_rope",
     "sepattn_kernel_name",
     "sepattn_profile_create",
     "sepattn_profile_attach",
@@ -76,6 +86,14 @@ class SepkvParams(ctypes.Structure):
     _fields_ = [("S", ctypes.c_int), ("Hq", ctypes.c_int), ("Hkv", ctypes.c_int), ("d", ctypes.c_int),
                 ("a", ctypes.c_int), ("s", ctypes.c_int), ("w", ctypes.c_int), ("c", ctypes.c_int),
                 ("scale", ctypes.c_float), ("dtype", ctypes.c_int)]
+
+
+class SepattnRopeParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("B", "Hq", "Hkv", "L", "d", "rotary_dim", "interleaved", "dtype")]
+
+
+class SepattnStrides(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("b", "h", "l")]
 
 
 class SepattnError(RuntimeError):
@@ -159,6 +177,26 @@ def load(path: Optional[str] = None):
     lib.sepattn_decode_rope.argtypes = [kp, vp, vp, vp, vp, vp, ci, vp, vp, vp, sz, vp]
     lib.sepkv_append.restype = ci
     lib.sepkv_append.argtypes = [kp] + [vp] * 8
+    cd, rp = ctypes.c_double, ctypes.POINTER(SepattnRopeParams)
+    lib.sepattn_rope_frequencies.restype = ci
+    lib.sepattn_rope_frequencies.argtypes = [ci, cd, cd, cd, cd, ci, vp]
+    for name in ("sepattn_rope", "sepattn_rope_backward"):
+        getattr(lib, name).restype = ci
+        getattr(lib, name).argtypes = [rp, vp, vp, vp] + [vp, ctypes.POINTER(SepattnStrides)] * 6 + [vp]
+    lib.sepkv_rope_table_frequencies.restype = ci
+    lib.sepkv_rope_table_frequencies.argtypes = [ci, ci, vp, vp, vp]
+    lib.sepkv_append_rope.restype = ci
+    lib.sepkv_append_rope.argtypes = [kp, ci, ci] + [vp] * 12
+    lib.sepkv_group_sequences.restype = ci
+    lib.sepkv_group_sequences.argtypes = [vp, ci, ci, vp, vp, vp]
+    lib.sepkv_rope_cache.restype = ci
+    lib.sepkv_rope_cache.argtypes = [kp, vp, vp, ci, vp, vp, vp]
+    lib.sepattn_decode_shared_workspace_bytes.restype = sz
+    lib.sepattn_decode_shared_workspace_bytes.argtypes = [kp, kp]
+    lib.sepattn_decode_shared.restype = ci
+    lib.sepattn_decode_shared.argtypes = [kp, kp] + [vp] * 13 + [sz, vp]
+    lib.sepattn_decode_shared_rope.restype = ci
+    lib.sepattn_decode_shared_rope.argtypes = [kp, kp] + [vp] * 11 + [ci, vp, vp, vp, sz, vp]
     lib.sepattn_kernel_name.restype = ctypes.c_char_p
     lib.sepattn_kernel_name.argtypes = [ci]
     lib.sepattn_profile_create.restype = ci
@@ -413,3 +451,87 @@ def sepkv_fill_from_prefill(K, V, is_sep, sep_idx, sep_prefix, Hq: int, a: int, 
     """Prefill K, V [S,Hkv,L,d] -> (Kc, Vc [S,Hkv,c,d], win_is_sep uint8 [S,c-a-s], sizes int32 [S,6]).
     Freshly allocated outputs are zero-filled (the call leaves slots beyond the sizes untouched)."""
     return _native().fill_from_prefill(K, V, is_sep, sep_idx, sep_prefix, Hq, a, s, w, c, nw, out)
+
+
+# ---- rotary positions in front of the attention --------------------------------------------------
+def sepattn_rope_frequencies(rotary_dim: int, base: float, factor: float = 1.0, low: float = 1.0, high: float = 4.0,
+                             original_length: int = 0, device="cpu") -> torch.Tensor:
+    """-> float64 [rotary_dim/2], radians per position: base^(-2p/rotary_dim), for contexts longer than the trained one
+    divided by `factor` (all, or with original_length > 0 the pairs that make fewer than `low` turns in it, blended up to `high`).
+    The calls take it on the GPU."""
+    f = torch.empty(max(1, int(rotary_dim) // 2), dtype=torch.float64)
+    _check("sepattn_rope_frequencies", load().sepattn_rope_frequencies(
+        int(rotary_dim), float(base), float(factor), float(low), float(high), int(original_length), _ptr(f)))
+    return f.to(device)
+
+
+def sepattn_rope(q, k, v, freqs, positions: Optional[torch.Tensor] = None, doc_start: Optional[torch.Tensor] = None,
+                 interleaved: bool = False, out=None):
+    """q [B,Hq,L,d], k, v [B,Hkv,L,d] with any strides (views of what the projections put out) -> (Q, K, V) dense, Q and K turned
+    by the tokens' positions: `positions` int32 [B,L], else the index in the row, minus doc_start int32 [B,L] if given.  freqs float64
+    [rotary_dim/2] (GPU).  v may be None, then V is.  `out`: three tensors of the same shapes, any strides."""
+    return _native().rope(q, k, v, freqs, positions, doc_start, interleaved, out)
+
+
+def sepattn_rope_backward(dQ, dK, dV, freqs, positions: Optional[torch.Tensor] = None, doc_start: Optional[torch.Tensor] = None,
+                          interleaved: bool = False, out=None):
+    """Gradient of sepattn_rope: dQ [B,Hq,L,d], dK, dV [B,Hkv,L,d] -> (dq, dk, dv) of the same shapes.  Unless `out` is given (views
+    of a projection's gradient), they are views of one buffer [B, L, Hq + 2 Hkv, d]."""
+    return _native().rope_backward(dQ, dK, dV, freqs, positions, doc_start, interleaved, out)
+
+
+def sepkv_rope_table_frequencies(n_pos: int, freqs: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """sepkv_rope_table for frequencies of the caller's: freqs float64 [d/2] (GPU) -> fp32 [n_pos, 2, d/2]."""
+    _dev(freqs)
+    if freqs.dtype != torch.float64 or freqs.dim() != 1:
+        raise TypeError("freqs: float64 [d/2]")
+    d = 2 * freqs.numel()
+    if out is None:
+        out = torch.empty((int(n_pos), 2, d // 2), dtype=torch.float32, device=freqs.device)
+    _dev(out)
+    if out.dtype != torch.float32 or tuple(out.shape) != (int(n_pos), 2, d // 2) or out.device != freqs.device:
+        raise ValueError("out: fp32 [n_pos, 2, d/2] on the device of freqs")
+    with torch.cuda.device(out.device):
+        _check("sepkv_rope_table_frequencies",
+               load().sepkv_rope_table_frequencies(int(n_pos), d, _ptr(freqs), _ptr(out), _stream(out)))
+    return out
+
+
+def sepkv_append_rope(q, k_new, v_new, is_sep_new, positions, freqs, Kc, Vc, win_is_sep, sizes, a: int, s: int, w: int,
+                      interleaved: bool = False, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """sepkv_append for a token that is not turned yet: q [S,Hq,d] turned by positions int32 [S] is returned, k_new, v_new [S,Hkv,d]
+    enter Kc, Vc, win_is_sep, sizes in place, the key turned.  `out` may be q."""
+    return _native().append_rope(q, k_new, v_new, is_sep_new, positions, freqs, Kc, Vc, win_is_sep, sizes, a, s, w, interleaved, out)
+
+
+# ---- shared prompts ----------------------------------------------------------------------------------
+def sepkv_group_sequences(prefix_of: torch.Tensor, n_prefixes: int, out=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """prefix_of int32 [S] (anything outside 0 .. n_prefixes-1: none) -> (group_start int32 [n_prefixes+1], group_seq int32 [S])."""
+    return _native().group_sequences(prefix_of, n_prefixes, out)
+
+
+def sepkv_rope_cache(Kc, sizes, rope_table, a: int, s: int, w: int, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The keys of Kc [S,Hkv,c,d] turned by their positions within the cache, in place or into `out` (other slots as they are)."""
+    return _native().rope_cache(Kc, sizes, rope_table, a, s, w, out)
+
+
+def sepattn_decode_shared_workspace_bytes(q, Kc, a: int, s: int, w: int, Kp, prefix_a: int, prefix_s: int, prefix_w: int) -> int:
+    return _native().decode_shared_workspace_bytes(q, Kc, a, s, w, Kp, prefix_a, prefix_s, prefix_w)
+
+
+def sepattn_decode_shared(q, Kc, Vc, sizes, a: int, s: int, w: int, Kp, Vp, prefix_sizes, prefix_a: int, prefix_s: int, prefix_w: int,
+                          prefix_of, group_start, group_seq, scale: float, out=None, ws: Optional[torch.Tensor] = None):
+    """sepattn_decode behind shared prompts: Kp, Vp [G,Hkv,prefix_c,d] and prefix_sizes int32 [G,6] are the prefix caches, prefix_of
+    int32 [S] says which one a sequence shares, group_start, group_seq come from sepkv_group_sequences
+    -> (out [S,Hq,d], lse fp32 [S,Hq])."""
+    return _native().decode_shared(q, Kc, Vc, sizes, a, s, w, Kp, Vp, prefix_sizes, prefix_a, prefix_s, prefix_w, prefix_of, group_start,
+                                   group_seq, None, scale, out, ws)
+
+
+def sepattn_decode_shared_rope(q, Kc, Vc, sizes, a: int, s: int, w: int, Kp, Vp, prefix_sizes, prefix_a: int, prefix_s: int,
+                               prefix_w: int, prefix_of, group_start, group_seq, rope_table, scale: float, out=None,
+                               ws: Optional[torch.Tensor] = None):
+    """The same with positions within the caches, the prefix's first: Kp holds keys turned by sepkv_rope_cache, Kc and q are
+    stored without encoding; rope_table with prefix_c + c rows or more."""
+    return _native().decode_shared_rope(q, Kc, Vc, sizes, a, s, w, Kp, Vp, prefix_sizes, prefix_a, prefix_s, prefix_w, prefix_of,
+                                        group_start, group_seq, rope_table, scale, out, ws)

@@ -472,6 +472,88 @@ int sepattn_backward_packed(const sepattn_params *p, const int32_t *doc_start, c
                                 doc_end, dQ, dK, dV, ws, static_cast<hipStream_t>(stream));
 }
 
+int sepattn_rope_frequencies(int rotary_dim, double base, double factor, double low, double high, int original_length,
+                             double *freqs) {
+    if (!freqs) return SEPATTN_ERR_NULL;
+    if (rotary_dim < 2 || rotary_dim % 2 != 0 || rotary_dim > kMaxRotary) return SEPATTN_ERR_PARAM;
+    if (!(base > 1.0) || base > 1e30 || !(factor >= 1.0) || factor > 1e30 || original_length < 0) return SEPATTN_ERR_PARAM;
+    if (original_length > 0 && (!(low >= 0.0) || !(high > low) || high > 1e30)) return SEPATTN_ERR_PARAM;
+    return rope_frequencies(rotary_dim, base, factor, low, high, original_length, freqs);
+}
+
+// One tensor's strides: its own or those of a dense [B, H, L, d]; of an output, rows that do not overlap.
+static int rope_strides(const sepattn_rope_params &p, int H, const sepattn_strides *given, bool output, const void *ptr,
+                        sepattn_strides &s) {
+    s = given ? *given : sepattn_strides{(int64_t)H * p.L * p.d, (int64_t)p.L * p.d, p.d};
+    const int64_t size[3] = {p.B, H, p.L}, stride[3] = {s.b, s.h, s.l}, unit = p.dtype == SEPATTN_BF16 ? 8 : 4;
+    if (!aligned(ptr, 16)) return SEPATTN_ERR_PARAM;
+    int order[3] = {0, 1, 2};  // by stride, ascending
+    for (int i = 0; i < 3; ++i) {
+        if (size[i] == 1) continue;
+        if (stride[i] < 0 || stride[i] % unit != 0) return SEPATTN_ERR_PARAM;
+        if (stride[i] > (int64_t)1 << 40) return SEPATTN_ERR_SHAPE;
+    }
+    if (!output) return SEPATTN_OK;
+    for (int i = 0; i < 3; ++i)
+        for (int j = i + 1; j < 3; ++j)
+            if (stride[order[j]] < stride[order[i]]) {
+                const int t = order[i];
+                order[i] = order[j], order[j] = t;
+            }
+    int64_t span = p.d;  // elements from the first to the last of what the dimensions so far reach
+    for (int k = 0; k < 3; ++k) {
+        const int i = order[k];
+        if (size[i] == 1) continue;
+        if (stride[i] < span) return SEPATTN_ERR_PARAM;
+        span += (size[i] - 1) * stride[i];
+    }
+    return SEPATTN_OK;
+}
+
+static int rope(const sepattn_rope_params *p, const double *freqs, const int32_t *positions, const int32_t *doc_start,
+                const void *const (&src)[3], const sepattn_strides *const (&from)[3], void *const (&dst)[3],
+                const sepattn_strides *const (&to)[3], bool backward, void *stream) {
+    if (!p || !freqs) return SEPATTN_ERR_NULL;
+    if (p->B <= 0 || p->Hq <= 0 || p->Hkv <= 0 || p->L <= 0 || p->B > 65535) return SEPATTN_ERR_SHAPE;
+    if ((long)p->Hq + 2L * p->Hkv > 65535L || (long)p->B * (p->Hq + p->Hkv) * p->L > (1L << 40)) return SEPATTN_ERR_SHAPE;
+    if (p->d != 64 && p->d != 128) return SEPATTN_ERR_DTYPE;
+    if (p->dtype != SEPATTN_BF16 && p->dtype != SEPATTN_FP32) return SEPATTN_ERR_DTYPE;
+    if (p->rotary_dim < 2 || p->rotary_dim > p->d || p->rotary_dim % 2 != 0) return SEPATTN_ERR_PARAM;
+    if (positions && doc_start) return SEPATTN_ERR_PARAM;
+    if (!src[0] || !src[1] || !dst[0] || !dst[1] || !src[2] != !dst[2]) return SEPATTN_ERR_NULL;
+    if (!aligned(freqs, 8)) return SEPATTN_ERR_PARAM;
+    sepattn_strides f[3] = {}, t[3] = {};
+    for (int i = 0; i < 3; ++i) {
+        if (!src[i]) continue;
+        int rc = rope_strides(*p, i == 0 ? p->Hq : p->Hkv, from[i], false, src[i], f[i]);
+        if (rc == SEPATTN_OK) rc = rope_strides(*p, i == 0 ? p->Hq : p->Hkv, to[i], true, dst[i], t[i]);
+        if (rc != SEPATTN_OK) return rc;
+    }
+    discard_stale_hip_error();
+    return launch_rope(*p, freqs, positions, doc_start, src, f, dst, t, backward, static_cast<hipStream_t>(stream));
+}
+
+int sepattn_rope(const sepattn_rope_params *p, const double *freqs, const int32_t *positions, const int32_t *doc_start,
+                 const void *q, const sepattn_strides *q_strides, const void *k, const sepattn_strides *k_strides,
+                 const void *v, const sepattn_strides *v_strides, void *Q, const sepattn_strides *Q_strides, void *K,
+                 const sepattn_strides *K_strides, void *V, const sepattn_strides *V_strides, void *stream) {
+    const void *const src[3] = {q, k, v};
+    void *const dst[3] = {Q, K, V};
+    const sepattn_strides *const from[3] = {q_strides, k_strides, v_strides}, *const to[3] = {Q_strides, K_strides, V_strides};
+    return rope(p, freqs, positions, doc_start, src, from, dst, to, false, stream);
+}
+
+int sepattn_rope_backward(const sepattn_rope_params *p, const double *freqs, const int32_t *positions,
+                          const int32_t *doc_start, const void *dQ, const sepattn_strides *dQ_strides, const void *dK,
+                          const sepattn_strides *dK_strides, const void *dV, const sepattn_strides *dV_strides, void *dq,
+                          const sepattn_strides *dq_strides, void *dk, const sepattn_strides *dk_strides, void *dv,
+                          const sepattn_strides *dv_strides, void *stream) {
+    const void *const src[3] = {dQ, dK, dV};
+    void *const dst[3] = {dq, dk, dv};
+    const sepattn_strides *const from[3] = {dQ_strides, dK_strides, dV_strides}, *const to[3] = {dq_strides, dk_strides, dv_strides};
+    return rope(p, freqs, positions, doc_start, src, from, dst, to, true, stream);
+}
+
 size_t sepattn_decode_workspace_bytes(const sepkv_params *p) {
     if (check_kv(p) != SEPATTN_OK) return 0;
     return decode_workspace(*p);
@@ -496,7 +578,16 @@ int sepkv_rope_table(int n_pos, int d, double base, float *table, void *stream) 
     if (!(base > 1.0) || base > 1e30) return SEPATTN_ERR_PARAM;
     if (!aligned(table, 16)) return SEPATTN_ERR_PARAM;
     discard_stale_hip_error();
-    return launch_rope_table(n_pos, d, base, table, static_cast<hipStream_t>(stream));
+    return launch_rope_table(n_pos, d, base, nullptr, table, static_cast<hipStream_t>(stream));
+}
+
+int sepkv_rope_table_frequencies(int n_pos, int d, const double *freqs, float *table, void *stream) {
+    if (!table || !freqs) return SEPATTN_ERR_NULL;
+    if (n_pos < 1 || n_pos > (1 << 28)) return SEPATTN_ERR_SHAPE;
+    if (d != 64 && d != 128) return SEPATTN_ERR_DTYPE;
+    if (!aligned(table, 16) || !aligned(freqs, 8)) return SEPATTN_ERR_PARAM;
+    discard_stale_hip_error();
+    return launch_rope_table(n_pos, d, 2.0, freqs, table, static_cast<hipStream_t>(stream));
 }
 
 int sepattn_decode_rope(const sepkv_params *p, const void *q, const void *Kc, const void *Vc,
@@ -522,6 +613,94 @@ int sepkv_append(const sepkv_params *p, const void *k_new, const void *v_new, co
     discard_stale_hip_error();
     return launch_cache_append(*p, k_new, v_new, is_sep_new, Kc, Vc, win_is_sep, sizes,
                                static_cast<hipStream_t>(stream));
+}
+
+int sepkv_append_rope(const sepkv_params *p, int rotary_dim, int interleaved, const double *freqs,
+                      const int32_t *positions, const void *q, const void *k_new, const void *v_new,
+                      const uint8_t *is_sep_new, void *q_out, void *Kc, void *Vc, uint8_t *win_is_sep, int32_t *sizes,
+                      void *stream) {
+    int rc = check_kv(p);
+    if (rc != SEPATTN_OK) return rc;
+    if (!freqs || !positions || !q || !k_new || !v_new || !is_sep_new || !q_out || !Kc || !Vc || !win_is_sep || !sizes)
+        return SEPATTN_ERR_NULL;
+    if (rotary_dim < 2 || rotary_dim > p->d || rotary_dim % 2 != 0) return SEPATTN_ERR_PARAM;
+    if (!aligned(freqs, 8) || !aligned(q, 16) || !aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(q_out, 16) ||
+        !aligned(Kc, 16) || !aligned(Vc, 16))
+        return SEPATTN_ERR_PARAM;
+    discard_stale_hip_error();
+    return launch_cache_append_rope(*p, rotary_dim, interleaved, freqs, positions, q, k_new, v_new, is_sep_new, q_out, Kc, Vc,
+                                    win_is_sep, sizes, static_cast<hipStream_t>(stream));
+}
+
+int sepkv_group_sequences(const int32_t *prefix_of, int S, int G, int32_t *group_start, int32_t *group_seq, void *stream) {
+    if (!prefix_of || !group_start || !group_seq) return SEPATTN_ERR_NULL;
+    if (S <= 0 || G <= 0 || S > 65535 || G > 65535) return SEPATTN_ERR_SHAPE;
+    discard_stale_hip_error();
+    return launch_group_sequences(prefix_of, S, G, group_start, group_seq, static_cast<hipStream_t>(stream));
+}
+
+int sepkv_rope_cache(const sepkv_params *p, const int32_t *sizes, const float *rope_table, int n_pos, const void *Kc, void *K_out,
+                     void *stream) {
+    int rc = check_kv(p);
+    if (rc != SEPATTN_OK) return rc;
+    if (!sizes || !rope_table || !Kc || !K_out) return SEPATTN_ERR_NULL;
+    if (n_pos < p->c) return SEPATTN_ERR_SHAPE;  // a row for every position a full cache can hold
+    if (!aligned(rope_table, 16) || !aligned(Kc, 16) || !aligned(K_out, 16)) return SEPATTN_ERR_PARAM;
+    discard_stale_hip_error();
+    return launch_rope_cache(*p, sizes, rope_table, n_pos, Kc, K_out, static_cast<hipStream_t>(stream));
+}
+
+// own and prefix caches of one call
+static int check_shared(const sepkv_params *p, const sepkv_params *pp) {
+    int rc = check_kv(p);
+    if (rc == SEPATTN_OK) rc = check_kv(pp);
+    if (rc != SEPATTN_OK) return rc;
+    if (p->Hq != pp->Hq || p->Hkv != pp->Hkv) return SEPATTN_ERR_SHAPE;
+    if (p->d != pp->d || p->dtype != pp->dtype) return SEPATTN_ERR_DTYPE;
+    return SEPATTN_OK;
+}
+
+size_t sepattn_decode_shared_workspace_bytes(const sepkv_params *p, const sepkv_params *pp) {
+    if (check_shared(p, pp) != SEPATTN_OK) return 0;
+    return decode_shared_workspace(*p, *pp);
+}
+
+static int decode_shared(const sepkv_params *p, const sepkv_params *pp, const void *q, const void *Kc, const void *Vc,
+                         const int32_t *sizes, const void *Kp, const void *Vp, const int32_t *prefix_sizes,
+                         const int32_t *prefix_of, const int32_t *group_start, const int32_t *group_seq,
+                         const float *rope_table, int n_pos, void *out, float *lse, void *ws, size_t ws_bytes, void *stream) {
+    if (!q || !Kc || !Vc || !sizes || !Kp || !Vp || !prefix_sizes || !prefix_of || !group_start || !group_seq || !out)
+        return SEPATTN_ERR_NULL;
+    if (!aligned(q, 16) || !aligned(Kc, 16) || !aligned(Vc, 16) || !aligned(Kp, 16) || !aligned(Vp, 16) || !aligned(out, 16))
+        return SEPATTN_ERR_PARAM;
+    if (!ws || ws_bytes < decode_shared_workspace(*p, *pp) || !aligned(ws, 256)) return SEPATTN_ERR_WORKSPACE;
+    discard_stale_hip_error();
+    return launch_decode_shared({*p, *pp, q, Kc, Vc, Kp, Vp, sizes, prefix_sizes, prefix_of, group_start, group_seq, rope_table,
+                                 n_pos, out, lse, static_cast<float *>(ws)}, static_cast<hipStream_t>(stream));
+}
+
+int sepattn_decode_shared(const sepkv_params *p, const sepkv_params *pp, const void *q, const void *Kc, const void *Vc,
+                          const int32_t *sizes, const void *Kp, const void *Vp, const int32_t *prefix_sizes,
+                          const int32_t *prefix_of, const int32_t *group_start, const int32_t *group_seq, void *out,
+                          float *lse, void *ws, size_t ws_bytes, void *stream) {
+    const int rc = check_shared(p, pp);
+    if (rc != SEPATTN_OK) return rc;
+    return decode_shared(p, pp, q, Kc, Vc, sizes, Kp, Vp, prefix_sizes, prefix_of, group_start, group_seq, nullptr, 0, out, lse,
+                         ws, ws_bytes, stream);
+}
+
+int sepattn_decode_shared_rope(const sepkv_params *p, const sepkv_params *pp, const void *q, const void *Kc, const void *Vc,
+                               const int32_t *sizes, const void *Kp, const void *Vp, const int32_t *prefix_sizes,
+                               const int32_t *prefix_of, const int32_t *group_start, const int32_t *group_seq,
+                               const float *rope_table, int n_pos, void *out, float *lse, void *ws, size_t ws_bytes,
+                               void *stream) {
+    const int rc = check_shared(p, pp);
+    if (rc != SEPATTN_OK) return rc;
+    if (!rope_table) return SEPATTN_ERR_NULL;
+    if ((long)n_pos < (long)pp->c + p->c) return SEPATTN_ERR_SHAPE;  // a row for every position of two full caches
+    if (!aligned(rope_table, 16)) return SEPATTN_ERR_PARAM;
+    return decode_shared(p, pp, q, Kc, Vc, sizes, Kp, Vp, prefix_sizes, prefix_of, group_start, group_seq, rope_table, n_pos, out,
+                         lse, ws, ws_bytes, stream);
 }
 
 size_t sepkv_evict_workspace_bytes(const sepkv_params *p) {

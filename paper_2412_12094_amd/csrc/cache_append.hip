@@ -7,7 +7,12 @@
 //
 // One workgroup per sequence; a thread copies 16-byte pieces of the 2 * Hkv rows.  All threads read
 // the sizes, then (after a barrier) thread 0 writes the new ones.
+//
+// cache_append_rope_kernel: the same for a token whose query and key are turned by its position in the text on the way (rope.hip), in one
+// launch: a launch of its own for the turn is what a step of generation would wait for longest.  A second workgroup per sequence
+// turns the query, which needs nothing of the cache.
 #include "decode_common.h"
+#include "rotary.h"
 
 namespace sepattn {
 
@@ -52,6 +57,59 @@ __global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(
     }
 }
 
+// the new sizes and the window's flag
+__device__ inline void count_appended(const sepkv_params &p, const CacheMap &cm, long sq, bool is_sep, uint8_t *__restrict__ win_is_sep,
+                                      int32_t *__restrict__ sz) {
+    if (cm.n_init < p.a) {
+        sz[0] = cm.n_init + 1;
+    } else {
+        win_is_sep[sq * cm.wcap + win_index(cm, cm.n_past + cm.n_loc)] = is_sep ? 1 : 0;
+        const int over = (cm.n_loc + 1 > p.w) ? 1 : 0;
+        sz[2] = cm.n_past + over;
+        sz[3] = cm.n_loc + 1 - over;
+    }
+}
+
+template <typename T, PairLayout LAYOUT>
+__global__ __launch_bounds__(kAppendThreads) void cache_append_rope_kernel(
+    sepkv_params p, int n_pairs, int log_groups, const double *__restrict__ freqs, const int32_t *__restrict__ positions, const T *q,
+    const T *__restrict__ k_new, const T *__restrict__ v_new, const uint8_t *__restrict__ is_sep_new, T *q_out, T *__restrict__ Kc,
+    T *__restrict__ Vc, uint8_t *__restrict__ win_is_sep, int32_t *__restrict__ sizes) {
+    const long sq = blockIdx.x;
+    const int group = threadIdx.x & ((1 << log_groups) - 1), row = threadIdx.x >> log_groups, rows = kAppendThreads >> log_groups;
+    const bool turned = group * Angles<T>::E < n_pairs;
+    const int t = positions[sq];
+    Angles<T> w;
+    if (blockIdx.y == 1) {  // the query
+        if (turned) w.form(freqs, n_pairs, group, t, 1.f);
+        for (int h = row; h < p.Hq; h += rows) {
+            Pairs<T> x;
+            x.template load<LAYOUT>(q + (sq * p.Hq + h) * p.d, group, n_pairs);
+            if (turned) x.template turn<LAYOUT>(w, group, n_pairs);
+            x.template store<LAYOUT>(q_out + (sq * p.Hq + h) * p.d, group, n_pairs);
+        }
+        return;
+    }
+    int32_t *sz = sizes + SEPKV_SIZES_COLS * sq;
+    const CacheMap cm = cache_map(p, sz);
+    const int u = cm.n_past + cm.n_loc;
+    __syncthreads();  // every thread has the old sizes before thread 0 replaces them
+    int slot;
+    if (cm.n_init < p.a) slot = cm.n_init;
+    else if (u < cm.wcap) slot = p.a + p.s + win_index(cm, u);
+    else return;  // window region full (uniform over the workgroup)
+    if (turned) w.form(freqs, n_pairs, group, t, 1.f);
+    for (int i = row; i < 2 * p.Hkv; i += rows) {
+        const bool value = i >= p.Hkv;
+        const int h = value ? i - p.Hkv : i;
+        Pairs<T> x;
+        x.template load<LAYOUT>((value ? v_new : k_new) + (sq * p.Hkv + h) * p.d, group, n_pairs);
+        if (turned && !value) x.template turn<LAYOUT>(w, group, n_pairs);
+        x.template store<LAYOUT>((value ? Vc : Kc) + ((sq * p.Hkv + h) * p.c + slot) * p.d, group, n_pairs);
+    }
+    if (threadIdx.x == 0) count_appended(p, cm, sq, is_sep_new[sq], win_is_sep, sz);
+}
+
 }  // namespace
 
 int launch_cache_append(const sepkv_params &p, const void *k_new, const void *v_new, const uint8_t *is_sep_new,
@@ -62,6 +120,30 @@ int launch_cache_append(const sepkv_params &p, const void *k_new, const void *v_
     hipLaunchKernelGGL(cache_append_kernel, dim3(p.S), dim3(kAppendThreads), 0, st, p, row16,
                        static_cast<const uint4 *>(k_new), static_cast<const uint4 *>(v_new), is_sep_new,
                        static_cast<uint4 *>(Kc), static_cast<uint4 *>(Vc), win_is_sep, sizes);
+    return launch_status();
+}
+
+int launch_cache_append_rope(const sepkv_params &p, int rotary_dim, int interleaved, const double *freqs, const int32_t *positions,
+                             const void *q, const void *k_new, const void *v_new, const uint8_t *is_sep_new, void *q_out, void *Kc,
+                             void *Vc, uint8_t *win_is_sep, int32_t *sizes, hipStream_t st) {
+    const int groups = p.d * (p.dtype == SEPATTN_BF16 ? 2 : 4) / 32;
+    int log_groups = 0;
+    while ((1 << log_groups) < groups) ++log_groups;
+    ProfScope prof(SEPATTN_K_CACHE_APPEND, st);
+    auto go = [&](auto T_) {
+        using T = decltype(T_);
+        const int layout = pair_layout<T>(rotary_dim, interleaved);
+#define APPEND(LAYOUT)                                                                                                               \
+    hipLaunchKernelGGL((cache_append_rope_kernel<T, LAYOUT>), dim3(p.S, 2), dim3(kAppendThreads), 0, st, p, rotary_dim / 2, log_groups, \
+                       freqs, positions, static_cast<const T *>(q), static_cast<const T *>(k_new), static_cast<const T *>(v_new),    \
+                       is_sep_new, static_cast<T *>(q_out), static_cast<T *>(Kc), static_cast<T *>(Vc), win_is_sep, sizes)
+        if (layout == kNeighbours) APPEND(kNeighbours);
+        else if (layout == kHalves) APPEND(kHalves);
+        else APPEND(kHalvesOdd);
+#undef APPEND
+    };
+    if (p.dtype == SEPATTN_BF16) go(uint16_t{});
+    else go(float{});
     return launch_status();
 }
 

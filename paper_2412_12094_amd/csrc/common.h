@@ -154,6 +154,14 @@ int launch_backward_bf16(const sepattn_params &p, const HeadWin &hw, const void 
                          const int32_t *sep_count, const int32_t *sep_prefix, const int32_t *doc_start,
                          const int32_t *doc_end, void *dQ, void *dK, void *dV, void *ws, hipStream_t st);
 
+// ---- rotary positions in front of the attention --------------------------------------------------
+constexpr int kMaxRotary = 128;  // the largest head dimension
+int rope_frequencies(int rotary_dim, double base, double factor, double low, double high, int original_length, double *freqs);
+// src, dst: q, k, v (src[2] nullptr: no values); backward: the opposite angles
+int launch_rope(const sepattn_rope_params &p, const double *freqs, const int32_t *positions, const int32_t *doc_start,
+                const void *const (&src)[3], const sepattn_strides (&from)[3], void *const (&dst)[3], const sepattn_strides (&to)[3],
+                bool backward, hipStream_t st);
+
 // ---- streaming cache ---------------------------------------------------------------------------
 int check_kv_params(const sepkv_params *p);  // host validation shared by every cache call
 size_t decode_workspace(const sepkv_params &p);
@@ -161,12 +169,31 @@ size_t decode_workspace(const sepkv_params &p);
 int launch_decode(const sepkv_params &p, const void *q, const void *Kc, const void *Vc,
                   const int32_t *sizes, const float *rope, int n_pos, void *out, float *lse, void *ws,
                   hipStream_t st);
-int launch_rope_table(int n_pos, int d, double base, float *table, hipStream_t st);
+// freqs: DEVICE, radians per position of every pair, or nullptr (base^(-2i/d))
+int launch_rope_table(int n_pos, int d, double base, const double *freqs, float *table, hipStream_t st);
 int launch_cache_append(const sepkv_params &p, const void *k_new, const void *v_new, const uint8_t *is_sep_new,
                         void *Kc, void *Vc, uint8_t *win_is_sep, int32_t *sizes, hipStream_t st);
+int launch_cache_append_rope(const sepkv_params &p, int rotary_dim, int interleaved, const double *freqs, const int32_t *positions,
+                             const void *q, const void *k_new, const void *v_new, const uint8_t *is_sep_new, void *q_out, void *Kc,
+                             void *Vc, uint8_t *win_is_sep, int32_t *sizes, hipStream_t st);
+int launch_rope_cache(const sepkv_params &p, const int32_t *sizes, const float *rope, int n_pos, const void *Kc, void *K_out, hipStream_t st);
+int launch_group_sequences(const int32_t *prefix_of, int S, int G, int32_t *group_start, int32_t *group_seq, hipStream_t st);
 size_t evict_workspace(const sepkv_params &p);
 int launch_evict(const sepkv_params &p, void *Kc, void *Vc, const uint8_t *win_is_sep, int32_t *sizes,
                  void *ws, hipStream_t st);
+// ---- shared prefixes ----
+struct SharedDecode {  // arguments of one call
+    sepkv_params p, pp;
+    const void *q, *Kc, *Vc, *Kp, *Vp;
+    const int32_t *sizes, *prefix_sizes, *prefix_of, *group_start, *group_seq;
+    const float *rope;  // nullptr: keys and queries as they are
+    int n_pos;
+    void *out;
+    float *lse;
+    float *part;  // workspace
+};
+size_t decode_shared_workspace(const sepkv_params &p, const sepkv_params &pp);
+int launch_decode_shared(const SharedDecode &x, hipStream_t st);
 int launch_cache_fill(const sepkv_params &p, int L, int nw, const void *K, const void *V, const uint8_t *is_sep,
                       const int32_t *sep_idx, int cap, const int32_t *sep_prefix, void *Kc, void *Vc,
                       uint8_t *win_is_sep, int32_t *sizes, bool zero_rest, hipStream_t st);

@@ -42,12 +42,28 @@ __device__ inline int decode_slot_of(const CacheMap &m, int e) {
     if (e < m.n_init + m.n_sep) return sep_slot(m, e - m.n_init);
     return m.a + m.s + win_index(m, e - m.n_init - m.n_sep);
 }
+// the other way round: rank of the entry in a slot, -1 for a slot without a valid one
+__device__ inline int rank_of_slot(const CacheMap &m, int slot) {
+    if (slot < m.a) return slot < m.n_init ? slot : -1;
+    if (slot < m.a + m.s) {
+        const int k = slot - m.a - m.sep_head, e = k < 0 ? k + m.s : k;
+        return e < m.n_sep ? m.n_init + e : -1;
+    }
+    const int u = slot - m.a - m.s - m.win_head, e = u < 0 ? u + m.wcap : u;
+    return e < m.n_past + m.n_loc ? m.n_init + m.n_sep + e : -1;
+}
 
 __device__ inline uint16_t decode_f32_to_bf16(float f) {
     uint32_t u = __float_as_uint(f);
     u += 0x7FFFu + ((u >> 16) & 1u);
     return (uint16_t)(u >> 16);
 }
+
+// The vector-ALU kernel of decode.hip without the sum over the slices: records of d + 2 floats (max, sum, unnormalised outputs),
+// [sequence][head][slice]
+int decode_record_slices(const sepkv_params &p);
+int launch_decode_records(const sepkv_params &p, int nsplit, const void *q, const void *Kc, const void *Vc, const int32_t *sizes,
+                          const float *rope, int n_pos, float *part, hipStream_t st);
 
 bool decode_mfma_applicable(const sepkv_params &p);
 int decode_mfma_nsplit(const sepkv_params &p);

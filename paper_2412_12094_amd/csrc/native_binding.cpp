@@ -14,6 +14,7 @@
 
 #include <ATen/ATen.h>
 #include <ATen/hip/EmptyTensor.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <dlfcn.h>
 #include <torch/csrc/Exceptions.h>
@@ -34,10 +35,15 @@ namespace {
     X(sepkv_fill_from_prefill) X(sepattn_decode_rope) X(sepkv_append)
 // what some of them call where the outputs are their own, fresh ones
 #define LIB_FRESH_FUNCTIONS(F) F(sepattn_compact_indices_filled) F(sepattn_mark_compact_filled) F(sepkv_fill_from_prefill_zeroed)
+// rotary positions in front of the attention, shared prompts
+#define LIB_POSITION_FUNCTIONS(P)                                                                                      \
+    P(sepattn_rope) P(sepattn_rope_backward) P(sepkv_append_rope) P(sepkv_group_sequences) P(sepkv_rope_cache)          \
+    P(sepattn_decode_shared_workspace_bytes) P(sepattn_decode_shared) P(sepattn_decode_shared_rope)
 struct Lib {
 #define X(name) decltype(&::name) name;
     LIB_FUNCTIONS(X)
     LIB_FRESH_FUNCTIONS(X)
+    LIB_POSITION_FUNCTIONS(X)
 #undef X
 } lib;
 PyObject *g_raise = nullptr;  // Python callable: raises SepattnError(function, status)
@@ -572,6 +578,247 @@ PyObject *fill_from_prefill(PyObject *const *a) {
     return tuple_of(wrap(std::move(Kc)), wrap(std::move(Vc)), wrap(std::move(flags)), wrap(std::move(sizes)));
 }
 
+// ---- rotary positions ------------------------------------------------------------------------------
+// The tensors of a call live on one device, which is the current one while the library is called.
+template <typename... T>
+void one_device(const at::Tensor &first, const T &...others) {
+    const bool same[] = {true, (!others.defined() || others.device() == first.device())...};
+    for (const bool s : same)
+        if (!s) fail(PyExc_ValueError, "tensors on different devices");
+}
+// an optional tensor: undefined for None
+at::Tensor dev_or_none(PyObject *o) { return o == Py_None ? at::Tensor() : dev(o); }
+void *ptr_or_null(const at::Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; }
+
+// [B, H, L, d] on the GPU with any strides, d innermost
+const at::Tensor &rows_arg(PyObject *o) {
+    const at::Tensor &t = tensor(o);
+    if (!t.is_cuda()) fail(PyExc_ValueError, "libsepattn works on GPU tensors only");
+    if (t.dim() != 4) fail(PyExc_ValueError, "[B, H, L, d] is expected");
+    if (t.size(3) != 1 && t.stride(3) != 1) fail(PyExc_ValueError, "the head dimension must be contiguous");
+    return t;
+}
+struct Rows {  // one of q, k, v and what becomes of it
+    at::Tensor from, to;
+    sepattn_strides from_strides, to_strides;
+    static sepattn_strides strides_of(const at::Tensor &t) { return {t.stride(0), t.stride(1), t.stride(2)}; }
+    void finish() {
+        if (!from.defined()) return;
+        from_strides = strides_of(from);
+        to_strides = strides_of(to);
+    }
+    const sepattn_strides *from_s() const { return from.defined() ? &from_strides : nullptr; }
+    const sepattn_strides *to_s() const { return from.defined() ? &to_strides : nullptr; }
+};
+const double *freqs_arg(const at::Tensor &f) {
+    require(f.scalar_type() == at::kDouble && f.dim() == 1, "freqs: float64 [rotary_dim / 2]");
+    return static_cast<const double *>(f.data_ptr());
+}
+
+// rope(q, k, v, freqs, positions, doc_start, interleaved, out)
+template <bool BACKWARD>
+PyObject *rope(PyObject *const *a) {
+    Rows r[3];
+    for (int i = 0; i < 3; ++i)
+        if (i < 2 || a[i] != Py_None) r[i].from = rows_arg(a[i]);
+    const at::Tensor &q = r[0].from, &k = r[1].from, &v = r[2].from;
+    const at::Tensor &f = dev(a[3]);
+    const at::Tensor pos = dev_or_none(a[4]), doc = dev_or_none(a[5]);
+    const int64_t want[4] = {q.size(0), k.size(1), q.size(2), q.size(3)};
+    require(k.sizes() == c10::IntArrayRef(want, 4) && (!v.defined() || v.sizes() == k.sizes()) && k.scalar_type() == q.scalar_type() &&
+                (!v.defined() || v.scalar_type() == q.scalar_type()), "q [B, Hq, L, d], k and v [B, Hkv, L, d] of one dtype");
+    const double *freqs = freqs_arg(f);
+    for (const at::Tensor *t : {&pos, &doc})
+        require(!t->defined() || (t->scalar_type() == at::kInt && t->dim() == 2 && t->size(0) == q.size(0) && t->size(1) == q.size(2)),
+                "positions, doc_start: int32 [B, L]");
+    sepattn_rope_params p;
+    p.B = (int)q.size(0), p.Hq = (int)q.size(1), p.Hkv = (int)k.size(1), p.L = (int)q.size(2), p.d = (int)q.size(3);
+    p.rotary_dim = (int)(2 * f.numel());
+    p.interleaved = as_bool(a[6]);
+    p.dtype = dtype_code(q);
+    const Out<3> out(a[7]);
+    for (int i = 0; out.given() && i < 3; ++i) {
+        if (!r[i].from.defined()) {
+            require(out[i] == Py_None, "out: no values were given");
+            continue;
+        }
+        r[i].to = rows_arg(out[i]);
+        require(r[i].to.sizes() == r[i].from.sizes() && r[i].to.scalar_type() == r[i].from.scalar_type(), "out: shapes and dtype of the inputs");
+    }
+    one_device(q, k, v, f, pos, doc, r[0].to, r[1].to, r[2].to);
+    check(BACKWARD ? "sepattn_rope_backward" : "sepattn_rope", unlocked([&] {
+              const c10::DeviceGuard guard(q.device());
+              if (!out.given()) {
+                  if constexpr (BACKWARD) {  // as one fused projection puts them out: [B, L, q heads | k heads | v heads, d]
+                      const int64_t Hv = v.defined() ? p.Hkv : 0;
+                      const at::Tensor dx = empty({p.B, p.L, p.Hq + p.Hkv + Hv, p.d}, q.scalar_type(), q.device());
+                      r[0].to = dx.narrow(2, 0, p.Hq).transpose(1, 2);
+                      r[1].to = dx.narrow(2, p.Hq, p.Hkv).transpose(1, 2);
+                      if (v.defined()) r[2].to = dx.narrow(2, p.Hq + p.Hkv, Hv).transpose(1, 2);
+                  } else {
+                      for (Rows &x : r)
+                          if (x.from.defined()) x.to = fresh_like(x.from);
+                  }
+              }
+              for (Rows &x : r) x.finish();
+              return (BACKWARD ? lib.sepattn_rope_backward : lib.sepattn_rope)(
+                  &p, freqs, (const int32_t *)ptr_or_null(pos), (const int32_t *)ptr_or_null(doc), ptr(q), r[0].from_s(), ptr(k), r[1].from_s(),
+                  ptr_or_null(v), r[2].from_s(), ptr(r[0].to), r[0].to_s(), ptr(r[1].to), r[1].to_s(), ptr_or_null(r[2].to), r[2].to_s(),
+                  stream_of(q));
+          }));
+    if (out.given()) return tuple_of(keep(out[0]), keep(out[1]), keep(out[2]));
+    return tuple_of(wrap(r[0].to), wrap(r[1].to), v.defined() ? wrap(r[2].to) : keep(Py_None));
+}
+
+// append_rope(q, k_new, v_new, is_sep_new, positions, freqs, Kc, Vc, win_is_sep, sizes, a, s, w, interleaved, out)
+PyObject *append_rope(PyObject *const *a) {
+    const at::Tensor &q = dev(a[0]), &k = dev(a[1]), &v = dev(a[2]), &sep = dev(a[3]), &pos = dev(a[4]), &f = dev(a[5]), &Kc = dev(a[6]),
+                     &Vc = dev(a[7]), &flags = dev(a[8]);
+    const at::Tensor &sizes = sizes_arg(a[9]);
+    if (q.dim() != 3) fail(PyExc_ValueError, "q [S,Hq,d] is expected");
+    const sepkv_params p = kv_params(Kc, (int)q.size(0), (int)q.size(1), as_int(a[10]), as_int(a[11]), as_int(a[12]), 1.0f);
+    const int64_t want[3] = {p.S, p.Hkv, p.d};
+    require(k.sizes() == c10::IntArrayRef(want, 3) && v.sizes() == k.sizes() && k.scalar_type() == Kc.scalar_type() &&
+                v.scalar_type() == Kc.scalar_type(), "k_new, v_new: [S, Hkv, d] in the cache's dtype");
+    require(q.size(2) == p.d && q.scalar_type() == Kc.scalar_type(), "q: [S, Hq, d] in the cache's dtype");
+    require(Kc.size(0) == p.S && Vc.sizes() == Kc.sizes() && Vc.scalar_type() == Kc.scalar_type(), "Kc, Vc: [S, Hkv, c, d] of one dtype");
+    require(sep.scalar_type() == at::kByte && flags.scalar_type() == at::kByte && sep.numel() == p.S && flags.dim() == 2 &&
+                flags.size(0) == p.S && flags.size(1) == (int64_t)p.c - p.a - p.s, "is_sep_new: uint8 [S], win_is_sep: uint8 [S, c-a-s]");
+    require(pos.scalar_type() == at::kInt && pos.dim() == 1 && pos.size(0) == p.S && sizes.size(0) == p.S, "positions: int32 [S], sizes: int32 [S, 6]");
+    const double *freqs = freqs_arg(f);
+    const int rotary_dim = (int)(2 * f.numel()), interleaved = as_bool(a[13]);
+    at::Tensor o;
+    if (a[14] != Py_None) {
+        o = dev(a[14]);
+        require(o.sizes() == q.sizes() && o.scalar_type() == q.scalar_type(), "out: like q");
+    }
+    one_device(q, k, v, sep, pos, f, Kc, Vc, flags, sizes, o);
+    check("sepkv_append_rope", unlocked([&] {
+              const c10::DeviceGuard guard(q.device());
+              if (!o.defined()) o = fresh_like(q);
+              return lib.sepkv_append_rope(&p, rotary_dim, interleaved, freqs, i32(pos), ptr(q), ptr(k), ptr(v), (const uint8_t *)ptr(sep), ptr(o),
+                                           ptr(Kc), ptr(Vc), (uint8_t *)ptr(flags), (int32_t *)ptr(sizes), stream_of(q));
+          }));
+    return a[14] == Py_None ? wrap(std::move(o)) : keep(a[14]);
+}
+
+// ---- shared prompts ----------------------------------------------------------------------------------
+// group_sequences(prefix_of, n_prefixes, out)
+PyObject *group_sequences(PyObject *const *a) {
+    const at::Tensor &of = dev(a[0]);
+    require(of.scalar_type() == at::kInt && of.dim() == 1, "prefix_of: int32 [S]");
+    const int S = (int)of.numel(), G = as_int(a[1]);
+    const Out<2> out(a[2]);
+    at::Tensor start, seq;
+    if (out.given()) {
+        start = dev(out[0]);
+        seq = dev(out[1]);
+        require(start.scalar_type() == at::kInt && start.numel() == (int64_t)G + 1 && seq.scalar_type() == at::kInt && seq.numel() == S,
+                "out: int32 [n_prefixes + 1], int32 [S]");
+    }
+    one_device(of, start, seq);
+    check("sepkv_group_sequences", unlocked([&] {
+              const c10::DeviceGuard guard(of.device());
+              if (!out.given()) {
+                  start = empty({G > 0 ? (int64_t)G + 1 : 1}, at::kInt, of.device());
+                  seq = empty({S}, at::kInt, of.device());
+              }
+              return lib.sepkv_group_sequences(i32(of), S, G, (int32_t *)ptr(start), (int32_t *)ptr(seq), stream_of(of));
+          }));
+    if (out.given()) return tuple_of(keep(out[0]), keep(out[1]));
+    return tuple_of(wrap(std::move(start)), wrap(std::move(seq)));
+}
+
+void table_arg(const at::Tensor &table, int64_t d) {
+    require(table.scalar_type() == at::kFloat && table.dim() == 3 && table.size(1) == 2 && table.size(2) * 2 == d, "rope_table: fp32 [n_pos, 2, d/2]");
+}
+
+// rope_cache(Kc, sizes, rope_table, a, s, w, out): out None: in place
+PyObject *rope_cache(PyObject *const *a) {
+    const at::Tensor &Kc = dev(a[0]), &sizes = sizes_arg(a[1]), &table = dev(a[2]);
+    if (Kc.dim() != 4) fail(PyExc_ValueError, "Kc [S,Hkv,c,d] is expected");
+    const sepkv_params p = kv_params(Kc, (int)Kc.size(0), (int)Kc.size(1), as_int(a[3]), as_int(a[4]), as_int(a[5]), 1.0f);
+    table_arg(table, p.d);
+    require(sizes.size(0) == p.S, "sizes: int32 [S, 6]");
+    const at::Tensor &o = a[6] == Py_None ? Kc : dev(a[6]);
+    require(o.sizes() == Kc.sizes() && o.scalar_type() == Kc.scalar_type(), "out: like Kc");
+    one_device(Kc, sizes, table, o);
+    check("sepkv_rope_cache", unlocked([&] {
+              const c10::DeviceGuard guard(Kc.device());
+              return lib.sepkv_rope_cache(&p, i32(sizes), (const float *)ptr(table), (int)table.size(0), ptr(Kc), ptr(o), stream_of(Kc));
+          }));
+    return keep(a[6] == Py_None ? a[0] : a[6]);
+}
+
+// Own and prefix caches of a shared decode: q, Kc, a, s, w, Kp, pa, ps, pw, scale
+struct SharedParams {
+    sepkv_params p, pp;
+    SharedParams(const at::Tensor &q, const at::Tensor &Kc, PyObject *const *own, const at::Tensor &Kp, PyObject *const *prefix, float scale) {
+        if (q.dim() != 3) fail(PyExc_ValueError, "q [S,Hq,d] is expected");
+        p = kv_params(Kc, (int)q.size(0), (int)q.size(1), as_int(own[0]), as_int(own[1]), as_int(own[2]), scale);
+        pp = kv_params(Kp, (int)Kp.size(0), (int)q.size(1), as_int(prefix[0]), as_int(prefix[1]), as_int(prefix[2]), scale);
+        require(q.size(2) == p.d && q.scalar_type() == Kc.scalar_type() && Kc.size(0) == p.S, "q [S, Hq, d], Kc [S, Hkv, c, d] of one dtype");
+        require(Kp.size(1) == p.Hkv && Kp.size(3) == p.d && Kp.scalar_type() == Kc.scalar_type(), "Kp: [G, Hkv, prefix_c, d] in the cache's dtype");
+    }
+};
+
+// decode_shared(q, Kc, Vc, sizes, a, s, w, Kp, Vp, prefix_sizes, pa, ps, pw, prefix_of, group_start, group_seq, rope_table, scale, out, ws)
+template <bool ROPE>
+PyObject *decode_shared(PyObject *const *a) {
+    const at::Tensor &q = dev(a[0]), &Kc = dev(a[1]), &Vc = dev(a[2]), &sizes = sizes_arg(a[3]), &Kp = dev(a[7]), &Vp = dev(a[8]),
+                     &psizes = sizes_arg(a[9]), &of = dev(a[13]), &start = dev(a[14]), &seq = dev(a[15]);
+    const at::Tensor table = ROPE ? dev(a[16]) : at::Tensor();
+    const SharedParams x(q, Kc, a + 4, Kp, a + 10, as_float(a[17]));
+    const int S = x.p.S, G = x.pp.S;
+    require(Vc.sizes() == Kc.sizes() && Vc.scalar_type() == Kc.scalar_type() && Vp.sizes() == Kp.sizes() && Vp.scalar_type() == Kp.scalar_type(),
+            "Vc like Kc, Vp like Kp");
+    require(sizes.size(0) == S && psizes.size(0) == G, "sizes: int32 [S, 6], prefix_sizes: int32 [G, 6]");
+    require(of.scalar_type() == at::kInt && of.numel() == S && start.scalar_type() == at::kInt && start.numel() == (int64_t)G + 1 &&
+                seq.scalar_type() == at::kInt && seq.numel() == S, "prefix_of, group_seq: int32 [S], group_start: int32 [G + 1]");
+    if (ROPE) table_arg(table, x.p.d);
+    const Out<2> out(a[18]);
+    at::Tensor o, lse;
+    if (out.given()) {
+        o = dev(out[0]);
+        lse = dev_or_none(out[1]);  // None: no LSE wanted
+        require(o.sizes() == q.sizes() && o.scalar_type() == q.scalar_type() &&
+                    (!lse.defined() || (lse.scalar_type() == at::kFloat && lse.numel() == (int64_t)S * x.p.Hq)), "out: like q, lse: fp32 [S, Hq]");
+    }
+    Workspace ws(a[19]);
+    at::Tensor given_ws;
+    if (ws.given) {
+        given_ws = dev(a[19]);
+        ws.bytes = (size_t)given_ws.nbytes();
+    }
+    one_device(q, Kc, Vc, sizes, Kp, Vp, psizes, of, start, seq, table, o, lse, given_ws);
+    check(ROPE ? "sepattn_decode_shared_rope" : "sepattn_decode_shared", unlocked([&] {
+              const c10::DeviceGuard guard(q.device());
+              if (!out.given()) {
+                  o = fresh_like(q);
+                  lse = empty({S, x.p.Hq}, at::kFloat, q.device());
+              }
+              if (!ws.given) ws.allocate(lib.sepattn_decode_shared_workspace_bytes(&x.p, &x.pp), q.device());
+              float *l = static_cast<float *>(ptr_or_null(lse));
+              void *st = stream_of(q);
+              if constexpr (ROPE)
+                  return lib.sepattn_decode_shared_rope(&x.p, &x.pp, ptr(q), ptr(Kc), ptr(Vc), i32(sizes), ptr(Kp), ptr(Vp), i32(psizes), i32(of),
+                                                        i32(start), i32(seq), (const float *)ptr(table), (int)table.size(0), ptr(o), l, ws.p, ws.bytes, st);
+              else
+                  return lib.sepattn_decode_shared(&x.p, &x.pp, ptr(q), ptr(Kc), ptr(Vc), i32(sizes), ptr(Kp), ptr(Vp), i32(psizes), i32(of),
+                                                   i32(start), i32(seq), ptr(o), l, ws.p, ws.bytes, st);
+          }));
+    if (out.given()) return tuple_of(keep(out[0]), keep(out[1]));
+    return tuple_of(wrap(std::move(o)), wrap(std::move(lse)));
+}
+
+// decode_shared_workspace_bytes(q, Kc, a, s, w, Kp, pa, ps, pw)
+PyObject *decode_shared_workspace_bytes(PyObject *const *a) {
+    const at::Tensor &q = tensor(a[0]);
+    const SharedParams x(q, tensor(a[1]), a + 2, tensor(a[5]), a + 6, 1.0f);
+    const c10::DeviceGuard guard(q.device());
+    return PyLong_FromSize_t(lib.sepattn_decode_shared_workspace_bytes(&x.p, &x.pp));
+}
+
 // ---- module ------------------------------------------------------------------------------------------
 typedef PyObject *(*Body)(PyObject *const *);
 template <Body F, int N>
@@ -611,6 +858,7 @@ PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n) {
     }
     LIB_FUNCTIONS(X)
     LIB_FRESH_FUNCTIONS(X)
+    LIB_POSITION_FUNCTIONS(X)
 #undef X
     Py_INCREF(args[1]);
     Py_XSETREF(g_raise, args[1]);
@@ -637,6 +885,14 @@ PyMethodDef methods[] = {
     METHOD("append", append, 11),
     METHOD("evict_window", evict_window, 9),
     METHOD("fill_from_prefill", fill_from_prefill, 12),
+    METHOD("rope", rope<false>, 8),
+    METHOD("rope_backward", rope<true>, 8),
+    METHOD("append_rope", append_rope, 15),
+    METHOD("group_sequences", group_sequences, 3),
+    METHOD("rope_cache", rope_cache, 7),
+    METHOD("decode_shared", decode_shared<false>, 20),
+    METHOD("decode_shared_rope", decode_shared<true>, 20),
+    METHOD("decode_shared_workspace_bytes", decode_shared_workspace_bytes, 9),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -11,13 +11,14 @@ namespace {
 
 constexpr int kTableThreads = 256;
 
-__global__ __launch_bounds__(kTableThreads) void rope_table_kernel(int n_pos, int d, double log2_base,
+// freqs: the pairs' own frequencies, or nullptr: base^(-2i/d)
+__global__ __launch_bounds__(kTableThreads) void rope_table_kernel(int n_pos, int d, double log2_base, const double *__restrict__ freqs,
                                                                   float *__restrict__ table) {
     const int h = d / 2;
     const long item = (long)blockIdx.x * kTableThreads + threadIdx.x;
     if (item >= (long)n_pos * h) return;
     const int pos = (int)(item / h), i = (int)(item % h);
-    const double theta = exp2(-(2.0 * i / d) * log2_base);
+    const double theta = freqs ? freqs[i] : exp2(-(2.0 * i / d) * log2_base);
     double sn, cs;
     sincos((double)pos * theta, &sn, &cs);
     table[(long)pos * d + i] = (float)cs;
@@ -26,12 +27,12 @@ __global__ __launch_bounds__(kTableThreads) void rope_table_kernel(int n_pos, in
 
 }  // namespace
 
-int launch_rope_table(int n_pos, int d, double base, float *table, hipStream_t st) {
+int launch_rope_table(int n_pos, int d, double base, const double *freqs, float *table, hipStream_t st) {
     const long items = (long)n_pos * (d / 2);
     const long blocks = (items + kTableThreads - 1) / kTableThreads;
     if (blocks > 0x7FFFFFFFL) return SEPATTN_ERR_SHAPE;
     ProfScope prof(SEPATTN_K_ROPE_TABLE, st);
-    hipLaunchKernelGGL(rope_table_kernel, dim3((unsigned)blocks), dim3(kTableThreads), 0, st, n_pos, d, log2(base), table);
+    hipLaunchKernelGGL(rope_table_kernel, dim3((unsigned)blocks), dim3(kTableThreads), 0, st, n_pos, d, log2(base), freqs, table);
     return launch_status();
 }
 

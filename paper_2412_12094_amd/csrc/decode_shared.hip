@@ -88,199 +88,446 @@ __device__ inline int query_position(const PrefixArgs &x, int seq, int prefix_en
 }
 
 // ---- bf16 ------------------------------------------------------------------------------------------
-// Four waves: RB row blocks of 32 rows, and KG = 4 / RB groups of waves that take the key tiles in turn.  The waves of a
-// group share its stages of K and V rows in LDS (two, of TK keys).  Operands as in decode_mfma.hip: the cache rows are the A operand, a
-// wave's 32 rows the columns of B, so a row's softmax state is in one lane pair.
-// LO (turned queries): the query is the sum of two bf16 numbers, 16 bits of mantissa, and the scores are two products; rounded
-// to one, lse would be off by 1e-3.
-template <int D, int RB, bool LO>
-__global__ __launch_bounds__(kShThreads, RB == 4 ? 2 : 1) void shared_prefix_kernel(PrefixArgs x) {
-    constexpr int KG = kShWaves / RB, ROWS = 32 * RB, TK = RB == 1 ? 32 : 64;
-    constexpr int CH = D / 8, RPL = 64 / CH;   // 16-byte chunks per cache row, rows per wave-wide load
-    constexpr int NLD = TK / RB / RPL;         // such loads per wave, tensor and tile
-    constexpr int KSTEPS = D / 16, KS2 = KSTEPS / 2, DB = D / 32, REC = kShRecord<D>;
-    __shared__ __attribute__((aligned(1024))) uint16_t smem[KG][2][2][TK * D];  // [group][stage][K, V]
+// One workgroup of four waves: rows (queries that read one KV head) against a slice of one cache, in blocks of 32 keys.  Operands as in
+// decode_wide.hip (v_mfma_f32_16x16x32_bf16, the cache rows as A, 16 queries as the columns of B, score tile t's row 4g+i the block's row
+// 8g+4t+i, so that a lane's probabilities are its operand of the second product); a wave has NB such column blocks, for which it
+// reads the cache's fragments from LDS once.
+//   SPLIT_ROWS: the waves have different rows (64 NB per workgroup) and share the keys, in a ring of four stages of 32 rows of K
+//     and V: three tiles are on their way, one barrier per tile.
+//   otherwise: the waves have the same 16 NB rows and take the blocks in turn, each with a stage of its own, whose K half is refilled
+//     as soon as its fragments are in registers and the V half one step later; no barrier in the loop.  Their states meet in LDS.
+// KROPE (own caches): keys are turned by their distance to the query, as in decode_wide.hip.  LO (prefixes): the query is turned by its
+// position.  Either is then the sum of two bf16 numbers, 16 bits of mantissa, and the scores are two products: rounded to one
+// number, lse would be off by 1e-3.
+template <int D>
+constexpr int kShLds = 4 * 2 * kShBlock * D;  // elements: four stages of K and V
 
+__device__ inline f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+// XOR permutation of the 16-byte chunks of row 8a + 4t + i: see decode_wide.hip
+template <int D>
+__device__ inline int sh_swz(int row) {
+    const int i = row & 3, a = row >> 3;
+    if (D == 128) return (i << 1) | ((a & 1) << 3) | (a >> 1);
+    return (i & 2) | ((a & 1) << 2) | (a >> 1);
+}
+// over the four lane groups
+__device__ inline float groups_max(float x) {
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return pair_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ inline float groups_sum(float x) {
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return pair_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+template <int N>
+__device__ inline void wait_loads() {
+    static_assert(N == 0 || N == 4 || N == 5 || N == 8 || N == 9, "");
+    if constexpr (N == 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if constexpr (N == 4) asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
+    if constexpr (N == 5) asm volatile("s_waitcnt vmcnt(5)" ::: "memory");
+    if constexpr (N == 8) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+    if constexpr (N == 9) asm volatile("s_waitcnt vmcnt(9)" ::: "memory");
+}
+__device__ inline void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+__device__ inline void barrier() {
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Wint-to-pointer-cast"
+__device__ inline f32x4 lds_read_f4(uint32_t addr) { return *(const f32x4 __attribute__((address_space(3))) *)addr; }
+#pragma clang diagnostic pop
+
+// a bf16 number and what it leaves of the sum of the two
+__device__ inline void split_hi_lo(const f32x8 &x, bf16x8 &hi, bf16x8 &lo) {
+    hi = __builtin_convertvector(x, bf16x8);
+    lo = __builtin_convertvector(x - __builtin_convertvector(hi, f32x8), bf16x8);
+}
+
+// What the body needs of its rows: column `col` of block nb.
+struct ShRow {
+    const uint16_t *q;  // its query
+    int position;       // LO: the query's
+    float *record;      // where the slice's record goes, nullptr for a column without a row
+};
+
+// rows: ShRow of (column block, column)
+template <int D, int NB, bool SPLIT_ROWS, bool KROPE, bool LO, typename Rows>
+__device__ __forceinline__ void shared_body(const CacheMap &cm, const uint16_t *__restrict__ Kh, const uint16_t *__restrict__ Vh, int e0, int e1,
+                                            int last /* KROPE: position of the query within the cache */, const float *__restrict__ rope,
+                                            int n_pos, float sl2, uint16_t (&smem)[kShLds<D>], float (&base_s)[kShWaves][2][128], const Rows &rows) {
+    static_assert(!KROPE || (NB == 1 && !SPLIT_ROWS && !LO), "");
+    constexpr int CH = D / 8, RPL = 64 / CH;                         // 16-byte chunks per row, rows per wave-wide load
+    constexpr int NLD = kShBlock / RPL / (SPLIT_ROWS ? kShWaves : 1);  // a wave's loads per block and tensor
+    constexpr int KSTEPS = D / 32, KS2 = KSTEPS / 2, DB = D / 16, TILE = kShBlock * D;
+    constexpr int STAGES = 4;
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int rb = wave % RB, kg = wave / RB, col = lane & 31, hh = lane >> 5;
-    const int kv = blockIdx.x, split = blockIdx.z;
-    Chunk c;
-    if (!find_chunk<ROWS>(x, blockIdx.y, c)) return;
-    const CacheMap cm = cache_map(x.pp, x.prefix_sizes + SEPKV_SIZES_COLS * c.prefix);
-    const int np = entries_of(cm);
-    int e0, e1;
-    if (!slice_of(np, x.nsplit, split, e0, e1)) return;
-    const uint16_t *Kh = static_cast<const uint16_t *>(x.Kp) + ((long)c.prefix * x.p.Hkv + kv) * (long)x.pp.c * D;
-    const uint16_t *Vh = static_cast<const uint16_t *>(x.Vp) + ((long)c.prefix * x.p.Hkv + kv) * (long)x.pp.c * D;
+    const int col = lane & 15, g = lane >> 4;
 
-    const int tiles = (e1 - e0 + TK - 1) / TK, steps = (tiles + KG - 1) / KG;
+    // queries; a turned one in two parts
+    bf16x8 qhi[NB][KSTEPS], qlo[LO ? NB : 1][LO ? KSTEPS : 1];
+    float *record[NB];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+        const ShRow r = rows(SPLIT_ROWS ? wave * NB + nb : nb, col);
+        record[nb] = r.record;
+#pragma unroll
+        for (int ks = 0; ks < KSTEPS; ++ks) qhi[nb][ks] = as_bf16x8(*reinterpret_cast<const u32x4 *>(r.q + 32 * ks + 8 * g));
+        if constexpr (LO) {
+            const float *row = rope + (long)r.position * D + 8 * g;
+#pragma unroll
+            for (int ks = 0; ks < KS2; ++ks) {
+                const f32x8 u = __builtin_convertvector(qhi[nb][ks], f32x8), v = __builtin_convertvector(qhi[nb][ks + KS2], f32x8);
+                f32x8 x, y;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const f32x4 cs = *reinterpret_cast<const f32x4 *>(row + 32 * ks + 4 * h), sn = *reinterpret_cast<const f32x4 *>(row + D / 2 + 32 * ks + 4 * h);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        x[4 * h + e] = fmaf(u[4 * h + e], cs[e], -(v[4 * h + e] * sn[e]));
+                        y[4 * h + e] = fmaf(v[4 * h + e], cs[e], u[4 * h + e] * sn[e]);
+                    }
+                }
+                split_hi_lo(x, qhi[nb][ks], qlo[nb][ks]);
+                split_hi_lo(y, qhi[nb][ks + KS2], qlo[nb][ks + KS2]);
+            }
+        }
+    }
+
+    // loads: the wave's share of block eb's K or V rows into a stage; entries past the end: the last one (masked)
     const int my_pc = lane % CH, my_sub = lane / CH;
-    auto issue = [&](int step) {
-        const int eb = e0 + (step * KG + kg) * TK;
+    const uint32_t lds0 = lds_addr(&smem[0]);
+    const int stage_row0 = SPLIT_ROWS ? wave * (kShBlock / kShWaves) : 0;  // first of the rows that this wave loads
+    uint32_t off[NLD];
+    auto place = [&](int eb) __attribute__((always_inline)) {
         static_for<NLD>([&](auto U) {
-            const int r = (rb * NLD + U) * RPL + my_sub;
-            const uint32_t off = (uint32_t)decode_slot_of(cm, min(eb + r, e1 - 1)) * (uint32_t)(D * 2);
-            dma_to_lds_16(Kh, off + swz_chunk<kSwzRow, D>(my_pc, r) * 16, lds_addr(&smem[kg][step & 1][0][(rb * NLD + U) * RPL * D]));
-            dma_to_lds_16(Vh, off + swz_chunk<kSwzTr, D>(my_pc, r) * 16, lds_addr(&smem[kg][step & 1][1][(rb * NLD + U) * RPL * D]));
+            constexpr int u = U;
+            const int r = stage_row0 + u * RPL + my_sub;
+            off[u] = (uint32_t)decode_slot_of(cm, min(eb + r, e1 - 1)) * (uint32_t)(D * 2) + (uint32_t)((my_pc ^ sh_swz<D>(r)) * 16);
         });
     };
+    auto load_rows = [&](const uint16_t *from, uint32_t stage) __attribute__((always_inline)) {
+        static_for<NLD>([&](auto U) {
+            const uint32_t to = stage + (stage_row0 + U * RPL) * D * 2;
+            if constexpr (SPLIT_ROWS) dma_to_lds_16(from, off[U], to);  // the other chunks of rows read them as well
+            else dma_to_lds_16_nt(from, off[U], to);
+        });
+    };
+    auto k_stage = [&](int i) { return lds0 + (uint32_t)(i * 2 * TILE * 2); };
+    auto v_stage = [&](int i) { return lds0 + (uint32_t)((i * 2 + 1) * TILE * 2); };
 
-    // queries: B operand, column = row of the chunk
-    int seq, head;
-    row_of(x, c, c.row0 + rb * 32 + col, seq, head);
-    const uint16_t *qrow = static_cast<const uint16_t *>(x.q) + ((long)seq * x.p.Hq + kv * x.gq + head) * D + 8 * hh;
-    bf16x8 qhi[KSTEPS], qlo[LO ? KSTEPS : 1];
+    f32x4 oacc[NB][DB];
+    float m_run[NB], l_run[NB];
 #pragma unroll
-    for (int ks = 0; ks < KSTEPS; ++ks) qhi[ks] = as_bf16x8(*reinterpret_cast<const u32x4 *>(qrow + 16 * ks));
-    if constexpr (LO) {
-        const float *row = x.rope + (long)query_position(x, seq, np) * D + 8 * hh;
+    for (int nb = 0; nb < NB; ++nb) {
+        m_run[nb] = -INFINITY, l_run[nb] = 0.f;
 #pragma unroll
-        for (int ks = 0; ks < KS2; ++ks) {
-            const f32x8 u = __builtin_convertvector(qhi[ks], f32x8), v = __builtin_convertvector(qhi[ks + KS2], f32x8);
-            f32x8 cs, sn, a, b;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) cs[e] = row[16 * ks + e], sn[e] = row[D / 2 + 16 * ks + e];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                a[e] = fmaf(u[e], cs[e], -(v[e] * sn[e]));
-                b[e] = fmaf(v[e], cs[e], u[e] * sn[e]);
-            }
-            qhi[ks] = __builtin_convertvector(a, bf16x8);
-            qhi[ks + KS2] = __builtin_convertvector(b, bf16x8);
-            qlo[ks] = __builtin_convertvector(a - __builtin_convertvector(qhi[ks], f32x8), bf16x8);
-            qlo[ks + KS2] = __builtin_convertvector(b - __builtin_convertvector(qhi[ks + KS2], f32x8), bf16x8);
-        }
+        for (int db = 0; db < DB; ++db) oacc[nb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the loop counts its own loads only
-    issue(0);
+    // this lane's fragments in a stage: K row 8 (col/4) + col%4 (+ 4t), chunk 4 ks + g; V rows 8g + col/4 (+ 4), columns 16 db + 4 (col%4)
+    const int krow = 8 * (col >> 2) + (col & 3), vrow = 8 * g + (col >> 2);
+    const uint32_t kswz = sh_swz<D>(krow), vswz = sh_swz<D>(vrow);
+    const uint32_t koff = krow * D * 2, voff = vrow * D * 2 + ((col & 1) << 3);
 
-    const float sl2 = x.p.scale * kLog2e_f;
-    f32x16 oacc[DB];
+    f32x4 s[NB][2];
+    auto clear_scores = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int db = 0; db < DB; ++db)
+        for (int nb = 0; nb < NB; ++nb) s[nb][0] = s[nb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+    };
+    auto key_fragment = [&](uint32_t stage, int t, int ks) __attribute__((always_inline)) {
+        return lds_read_b128_at(stage + koff + 4 * t * D * 2 + (((uint32_t)(4 * ks + g) ^ kswz) << 4));
+    };
+    auto value_fragment = [&](uint32_t stage, int db) __attribute__((always_inline)) {
+        return lds_read_tr_at(stage + voff + (((uint32_t)(2 * db + ((col & 3) >> 1)) ^ vswz) << 4), 4 * D * 2);
+    };
+    // scores -> probabilities of block nb (bf16), maximum, sum and outputs carried on; n_valid >= 1 entries
+    auto softmax = [&](int n_valid, bf16x8 (&pb)[NB]) __attribute__((always_inline)) {
+        float alpha[NB];
+        bool any = false;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) oacc[db][i] = 0.f;
-    float m_run = -INFINITY, l_run = 0.f;
-    const int a_row = pi_row(col);
-
-    for (int step = 0; step < steps; ++step) {
-        if (step + 1 < steps) {
-            issue(step + 1);
-            static_assert(2 * NLD == 16 || 2 * NLD == 8 || 2 * NLD == 4, "wait counts are written for d = 64 and 128");
-            if constexpr (2 * NLD == 16) asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
-            if constexpr (2 * NLD == 8) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
-            if constexpr (2 * NLD == 4) asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
-        } else {
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        }
-        if constexpr (RB > 1) {
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-        }
-        const uint16_t *Kst = smem[kg][step & 1][0], *Vst = smem[kg][step & 1][1];
-        const int eb = e0 + (step * KG + kg) * TK;
+        for (int nb = 0; nb < NB; ++nb) {
+            float x[8] = {s[nb][0][0], s[nb][0][1], s[nb][0][2], s[nb][0][3], s[nb][1][0], s[nb][1][1], s[nb][1][2], s[nb][1][3]};  // rows 8g ..
+            if (n_valid < kShBlock) {
 #pragma unroll
-        for (int blk = 0; blk < TK / 32; ++blk) {
-            const int n_valid = e1 - (eb + 32 * blk);
-            if (n_valid <= 0) continue;
-            f32x16 s;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = 0.f;
-#pragma unroll
-            for (int ks = 0; ks < KSTEPS; ++ks) {
-                const bf16x8 ka = lds_read_a_swz<kSwzRow, D>(Kst + 32 * blk * D, a_row, 2 * ks + hh);
-                s = mfma_bf16(ka, qhi[ks], s);
-                if constexpr (LO) s = mfma_bf16(ka, qlo[ks], s);
+                for (int i = 0; i < 8; ++i) x[i] = 8 * g + i < n_valid ? x[i] : -INFINITY;
             }
-            if (n_valid < 32) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (rho_row(hh, i) >= n_valid) s[i] = -INFINITY;
-            }
-            float m_loc = s[0];
-#pragma unroll
-            for (int i = 1; i < 16; ++i) m_loc = fmaxf(m_loc, s[i]);
-            const float m_new = fmaxf(m_run, pair_max(m_loc * sl2));  // finite: key 0 of the block is valid
-            const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
-            m_run = m_new;
+            const float m_loc = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+            const float m_new = fmaxf(m_run[nb], groups_max(m_loc) * sl2);  // finite: row 0 of a block is valid
+            alpha[nb] = __builtin_amdgcn_exp2f(m_run[nb] - m_new);
+            any |= alpha[nb] != 1.f;
+            m_run[nb] = m_new;
             float psum = 0.f;
+            f32x8 p;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], sl2, -m_new));
-                psum += s[i];
+            for (int i = 0; i < 8; ++i) {
+                p[i] = __builtin_amdgcn_exp2f(fmaf(x[i], sl2, -m_new));
+                psum += p[i];
             }
-            l_run = l_run * alpha + psum;
-            if (__builtin_amdgcn_ballot_w64(alpha != 1.f) != 0ull) {
+            l_run[nb] = l_run[nb] * alpha[nb] + psum;
+            pb[nb] = __builtin_convertvector(p, bf16x8);
+        }
+        if (__builtin_amdgcn_ballot_w64(any) != 0ull) {
 #pragma unroll
-                for (int db = 0; db < DB; ++db)
+            for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) oacc[db][i] *= alpha;
-            }
-            const bf16x8 p0 = pack_bf16x8(s, 0), p1 = pack_bf16x8(s, 8);
+                for (int db = 0; db < DB; ++db) oacc[nb][db] *= alpha[nb];
+        }
+    };
+
+    if constexpr (SPLIT_ROWS) {
+        const int blocks = (e1 - e0 + kShBlock - 1) / kShBlock;
+        // (blocks past the end are loaded as well, the last row over and over: the number of loads on their way stays the same)
+        auto request = [&](int i) __attribute__((always_inline)) {
+            place(e0 + i * kShBlock);
+            load_rows(Kh, k_stage(i % STAGES));
+            load_rows(Vh, v_stage(i % STAGES));
+        };
+        for (int i = 0; i < STAGES - 1; ++i) request(i);
+        for (int i = 0; i < blocks; ++i) {
+            wait_loads<2 * NLD *(STAGES - 2)>();
+            barrier();  // everyone's part of tile i has landed, and everyone is done with tile i - 1
+            request(i + STAGES - 1);
+            const uint32_t ks_ = k_stage(i % STAGES), vs_ = v_stage(i % STAGES);
+            clear_scores();
+#pragma unroll
+            for (int ks = 0; ks < KSTEPS; ++ks)
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const bf16x8 ka = key_fragment(ks_, t, ks);
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) {
+                        s[nb][t] = mfma16(ka, qhi[nb][ks], s[nb][t]);
+                        if constexpr (LO) s[nb][t] = mfma16(ka, qlo[nb][ks], s[nb][t]);
+                    }
+                }
+            bf16x8 pb[NB];
+            softmax(e1 - e0 - i * kShBlock, pb);
 #pragma unroll
             for (int db = 0; db < DB; ++db) {
-                oacc[db] = mfma_bf16(lds_read_a_tr_swz<kSwzTr, D>(Vst + 32 * blk * D, 0, db * 32, lane), p0, oacc[db]);
-                oacc[db] = mfma_bf16(lds_read_a_tr_swz<kSwzTr, D>(Vst + 32 * blk * D, 16, db * 32, lane), p1, oacc[db]);
+                const bf16x8 va = value_fragment(vs_, db);
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) oacc[nb][db] = mfma16(va, pb[nb], oacc[nb][db]);
+            }
+            wait_lds();
+        }
+        wait_loads<0>();
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            const float l = groups_sum(l_run[nb]);
+            if (!record[nb]) continue;
+            if (g == 0) *reinterpret_cast<float2 *>(record[nb]) = float2{m_run[nb], l};
+#pragma unroll
+            for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4 *>(record[nb] + 4 + 16 * db + 4 * g) = oacc[nb][db];
+        }
+    } else {
+        const uint32_t ks_ = k_stage(wave), vs_ = v_stage(wave), bs_ = lds_addr(&base_s[wave][0][0]), ts_ = lds0;
+        auto request_keys = [&](int eb, int par) __attribute__((always_inline)) {
+            place(eb);
+            if constexpr (KROPE) {  // the table row of the first entry's distance
+                if (lane < D / 4) dma_to_lds_16(rope + (long)min(last - eb, n_pos - 1) * D, lane * 16, bs_ + par * D * 4);
+            }
+            load_rows(Kh, ks_);
+        };
+        int eb = e0 + wave * kShBlock;
+        const bool some = eb < e1;
+        // cos / sin of the lane's two rows krow + 4t within a block: table rows 0 .. 31, through LDS, over the V stages of the first waves
+        f32x4 rc[2][KS2][2], rs[2][KS2][2];
+        if constexpr (KROPE) {
+            constexpr int TCH = D / 4, TRPL = 64 / TCH, TLD = kShBlock / TRPL / kShWaves;
+            static_assert(TLD * TRPL * kShWaves == kShBlock, "");
+            // (where row r goes: the V stages lie apart; half a stage holds 16 rows at either d)
+            auto table_row = [&](int r) { return v_stage(r >> 4) + (uint32_t)((r & 15) * D * 4); };
+            static_assert(16 * D * 4 <= 2 * TILE, "");
+            static_for<TLD>([&](auto U) {
+                const int r0 = (wave * TLD + U) * TRPL, r = r0 + lane / TCH;
+                dma_to_lds_16(rope, (uint32_t)(min(r, n_pos - 1) * D * 4) + (uint32_t)(((lane % TCH) ^ sh_swz<128>(r)) * 16), table_row(r0));
+            });
+            if (some) {
+                request_keys(eb, 0);
+                wait_loads<NLD + 1>();
+            } else {
+                wait_loads<0>();
+            }
+            barrier();
+            const uint32_t tswz = sh_swz<128>(krow);
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int ks = 0; ks < KS2; ++ks)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const uint32_t row = table_row(krow + 4 * t);
+                        rc[t][ks][h] = lds_read_f4(row + (((uint32_t)(8 * ks + 2 * g + h) ^ tswz) << 4));
+                        rs[t][ks][h] = lds_read_f4(row + (((uint32_t)(D / 8 + 8 * ks + 2 * g + h) ^ tswz) << 4));
+                    }
+            wait_lds();
+            barrier();
+            if (some) load_rows(Vh, vs_);
+        } else if (some) {
+            request_keys(eb, 0);
+            load_rows(Vh, vs_);
+        }
+        for (int par = 0; eb < e1; eb += kShWaves * kShBlock, par ^= 1) {
+            const bool more = eb + kShWaves * kShBlock < e1;
+            const int n_valid = e1 - eb;
+            wait_loads<NLD>();  // the K rows; the V rows may be in flight
+            bf16x8 ka[2][KSTEPS];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int ks = 0; ks < KSTEPS; ++ks) ka[t][ks] = key_fragment(ks_, t, ks);
+            f32x4 bc[KS2][2], bs[KS2][2];
+            if constexpr (KROPE) {
+#pragma unroll
+                for (int ks = 0; ks < KS2; ++ks)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        bc[ks][h] = lds_read_f4(bs_ + par * D * 4 + (8 * ks + 2 * g + h) * 16);
+                        bs[ks][h] = lds_read_f4(bs_ + par * D * 4 + (D / 8 + 8 * ks + 2 * g + h) * 16);
+                    }
+            }
+            if (more) {
+                wait_lds();
+                request_keys(eb + kShWaves * kShBlock, par ^ 1);
+            }
+            clear_scores();
+            if constexpr (KROPE) {
+                // R(-distance): (x, y) -> (x cos + y sin, y cos - x sin), dimension i with i + D/2; row r's distance is that of the
+                // block's first entry minus r
+#pragma unroll
+                for (int ks = 0; ks < KS2; ++ks)
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        const f32x8 x = __builtin_convertvector(ka[t][ks], f32x8), y = __builtin_convertvector(ka[t][ks + KS2], f32x8);
+                        f32x8 u, v;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const float c0 = bc[ks][e >> 2][e & 3], s0 = bs[ks][e >> 2][e & 3];
+                            const float cr = rc[t][ks][e >> 2][e & 3], sr = rs[t][ks][e >> 2][e & 3];
+                            const float c = fmaf(s0, sr, c0 * cr), sn = fmaf(-c0, sr, s0 * cr);
+                            u[e] = fmaf(y[e], sn, x[e] * c);
+                            v[e] = fmaf(-x[e], sn, y[e] * c);
+                        }
+                        bf16x8 lo;
+                        split_hi_lo(u, ka[t][ks], lo);
+                        s[0][t] = mfma16(lo, qhi[0][ks], s[0][t]);
+                        split_hi_lo(v, ka[t][ks + KS2], lo);
+                        s[0][t] = mfma16(lo, qhi[0][ks + KS2], s[0][t]);
+                    }
+            }
+#pragma unroll
+            for (int ks = 0; ks < KSTEPS; ++ks)
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) {
+                        s[nb][t] = mfma16(ka[t][ks], qhi[nb][ks], s[nb][t]);
+                        if constexpr (LO) s[nb][t] = mfma16(ka[t][ks], qlo[nb][ks], s[nb][t]);
+                    }
+            if (more) wait_loads<NLD + (KROPE ? 1 : 0)>();  // the V rows (only the next block's K rows are in flight)
+            else wait_loads<0>();
+            bf16x8 va[DB];
+#pragma unroll
+            for (int db = 0; db < DB; ++db) va[db] = value_fragment(vs_, db);
+            if (more) {
+                wait_lds();
+                load_rows(Vh, vs_);
+            }
+            bf16x8 pb[NB];
+            softmax(n_valid, pb);
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) oacc[nb][db] = mfma16(va[db], pb[nb], oacc[nb][db]);
+        }
+        // ---- the waves' states meet in LDS, one column block after the other; a thread adds two columns of a row
+        constexpr int REC = kShRecord<D>;
+        static_assert(kShWaves * 16 * REC * sizeof(float) <= kShLds<D> * sizeof(uint16_t), "");
+        float *red = reinterpret_cast<float *>(&smem[0]);  // [wave][row][REC]
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            const float l = groups_sum(l_run[nb]);
+            __syncthreads();
+            float *r = red + (wave * 16 + col) * REC;
+            if (g == 0) *reinterpret_cast<float2 *>(r) = float2{m_run[nb], l};
+#pragma unroll
+            for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4 *>(r + 4 + 16 * db + 4 * g) = oacc[nb][db];
+            __syncthreads();
+            for (int item = threadIdx.x; item < 16 * (D / 2); item += kShThreads) {
+                const int row = item / (D / 2), c2 = item % (D / 2);
+                float *to = rows(nb, row).record;
+                if (!to) continue;
+                float M = -INFINITY, lsum = 0.f, o0 = 0.f, o1 = 0.f;
+#pragma unroll
+                for (int w = 0; w < kShWaves; ++w) M = fmaxf(M, red[(w * 16 + row) * REC]);
+#pragma unroll
+                for (int w = 0; w < kShWaves; ++w) {
+                    const float *x = red + (w * 16 + row) * REC;
+                    const float wgt = __builtin_amdgcn_exp2f(x[0] - M);  // M is finite: the slice has an entry
+                    lsum = fmaf(wgt, x[1], lsum);
+                    o0 = fmaf(wgt, x[4 + 2 * c2], o0);
+                    o1 = fmaf(wgt, x[5 + 2 * c2], o1);
+                }
+                *reinterpret_cast<float2 *>(to + 4 + 2 * c2) = float2{o0, o1};
+                if (c2 == 0) *reinterpret_cast<float2 *>(to) = float2{M, lsum};
             }
         }
-        // everyone has read the stage before the next step's loads overwrite it
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if constexpr (RB > 1) {
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-        }
     }
+}
 
-    // ---- the key groups' states meet in LDS
-    float l_tot = pair_sum(l_run);
-    if constexpr (KG > 1) {
-        __syncthreads();
-        float *red = reinterpret_cast<float *>(smem);  // [row][group][REC]
-        static_assert(sizeof(smem) >= sizeof(float) * ROWS * (KG - 1) * REC, "records fit the stages");
-        if (kg > 0) {
-            float *r = red + ((rb * 32 + col) * (KG - 1) + kg - 1) * REC;
-            if (hh == 0) r[0] = m_run, r[1] = l_tot;
-#pragma unroll
-            for (int db = 0; db < DB; ++db)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    *reinterpret_cast<f32x4 *>(r + 4 + db * 32 + 8 * i + 4 * hh) = f32x4{oacc[db][4 * i], oacc[db][4 * i + 1], oacc[db][4 * i + 2], oacc[db][4 * i + 3]};
-        }
-        __syncthreads();
-        if (kg > 0) return;
-        const float *r = red + (rb * 32 + col) * (KG - 1) * REC;
-        float M = m_run;
-#pragma unroll
-        for (int k = 0; k < KG - 1; ++k) M = fmaxf(M, r[k * REC]);
-        const float own = __builtin_amdgcn_exp2f(m_run - M);  // group 0 has the slice's first tile: m_run is finite
-        l_tot *= own;
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) oacc[db][i] *= own;
-#pragma unroll
-        for (int k = 0; k < KG - 1; ++k) {
-            const float w = __builtin_amdgcn_exp2f(r[k * REC] - M);  // 0 for a group without a tile
-            l_tot = fmaf(w, r[k * REC + 1], l_tot);
-#pragma unroll
-            for (int db = 0; db < DB; ++db)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const f32x4 v = *reinterpret_cast<const f32x4 *>(r + k * REC + 4 + db * 32 + 8 * i + 4 * hh);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) oacc[db][4 * i + j] = fmaf(w, v[j], oacc[db][4 * i + j]);
-                }
-        }
-        m_run = M;
+// Workgroups 0 .. n_prefix_groups - 1: (KV head, chunk of rows, slice of the prefix); the others: (KV head, sequence and chunk of 16 heads, slice of
+// its own cache).  KV heads run fastest, so that with eight of them the workgroups that read the same rows are on one XCD.
+struct SharedArgs {
+    PrefixArgs x;
+    const void *Kc, *Vc;
+    float *own_part;
+    int n_prefix_groups, chunks, n_own, head_chunks;
+};
+template <int D, int NB, bool SPLIT_ROWS, bool ROPE>
+__global__ __launch_bounds__(kShThreads, D == 64 ? 3 : 2) void shared_decode_kernel(SharedArgs a) {
+    constexpr int REC = kShRecord<D>;
+    __shared__ __attribute__((aligned(1024))) uint16_t smem[kShLds<D>];
+    __shared__ __attribute__((aligned(1024))) float base_s[kShWaves][2][128];
+    const PrefixArgs &x = a.x;
+    const float sl2 = x.p.scale * kLog2e_f;
+    const int Hkv = x.p.Hkv;
+    int id = blockIdx.x;
+    if (id < a.n_prefix_groups) {
+        constexpr int ROWS = (SPLIT_ROWS ? kShWaves : 1) * 16 * NB;
+        const int kv = id % Hkv, chunk = id / Hkv % a.chunks, split = id / Hkv / a.chunks;
+        Chunk c;
+        if (!find_chunk<ROWS>(x, chunk, c)) return;
+        const CacheMap cm = cache_map(x.pp, x.prefix_sizes + SEPKV_SIZES_COLS * c.prefix);
+        const int np = entries_of(cm);
+        int e0, e1;
+        if (!slice_of(np, x.nsplit, split, e0, e1)) return;
+        const long head0 = ((long)c.prefix * Hkv + kv) * (long)x.pp.c * D;
+        auto rows = [&](int block, int col) __attribute__((always_inline)) {
+            const int r = c.row0 + block * 16 + col;
+            int seq, head;
+            row_of(x, c, r, seq, head);
+            const long row = (long)seq * x.p.Hq + kv * x.gq + head;
+            return ShRow{static_cast<const uint16_t *>(x.q) + row * D, ROPE ? query_position(x, seq, np) : 0,
+                         r < c.rows ? x.part + (row * x.nsplit + split) * REC : nullptr};
+        };
+        shared_body<D, NB, SPLIT_ROWS, false, ROPE>(cm, static_cast<const uint16_t *>(x.Kp) + head0, static_cast<const uint16_t *>(x.Vp) + head0, e0, e1, 0,
+                                                    x.rope, x.n_pos, sl2, smem, base_s, rows);
+        return;
     }
-    if (c.row0 + rb * 32 + col >= c.rows) return;
-    float *r = x.part + (((long)seq * x.p.Hq + kv * x.gq + head) * x.nsplit + split) * REC;
-    if (hh == 0) *reinterpret_cast<float2 *>(r) = float2{m_run, l_tot};
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            *reinterpret_cast<f32x4 *>(r + 4 + db * 32 + 8 * i + 4 * hh) = f32x4{oacc[db][4 * i], oacc[db][4 * i + 1], oacc[db][4 * i + 2], oacc[db][4 * i + 3]};
+    id -= a.n_prefix_groups;
+    const int kv = id % Hkv, hc = id / Hkv % a.head_chunks, seq = id / Hkv / a.head_chunks % x.p.S, split = id / Hkv / a.head_chunks / x.p.S;
+    const CacheMap cm = cache_map(x.p, x.sizes + SEPKV_SIZES_COLS * seq);
+    const int nv = entries_of(cm);
+    int e0, e1;
+    if (!slice_of(nv, a.n_own, split, e0, e1)) return;
+    const long head0 = ((long)seq * Hkv + kv) * (long)x.p.c * D;
+    auto rows = [&](int, int col) __attribute__((always_inline)) {
+        const int head = hc * 16 + col;
+        const long row = (long)seq * x.p.Hq + kv * x.gq + min(head, x.gq - 1);
+        return ShRow{static_cast<const uint16_t *>(x.q) + row * D, 0, head < x.gq ? a.own_part + (row * a.n_own + split) * REC : nullptr};
+    };
+    shared_body<D, 1, false, ROPE, false>(cm, static_cast<const uint16_t *>(a.Kc) + head0, static_cast<const uint16_t *>(a.Vc) + head0, e0, e1, nv - 1, x.rope,
+                                          x.n_pos, sl2, smem, base_s, rows);
 }
 
 // ---- fp32 ------------------------------------------------------------------------------------------
@@ -375,69 +622,105 @@ __global__ __launch_bounds__(kShThreads) void shared_prefix_fp32_kernel(PrefixAr
     for (int db = 0; db < D / 16; ++db) *reinterpret_cast<f4 *>(r + 4 + 16 * db + 4 * g) = o[db];
 }
 
-// ---- the slices' sum: one wave per (sequence, head), prefix slices first, then the own cache's, in order ------------
-template <typename T, int D>
-__global__ __launch_bounds__(kShThreads) void shared_merge_kernel(sepkv_params p, sepkv_params pp, int n_prefix, int n_own,
+// ---- the slices' sum: a workgroup per (sequence, head), prefix slices first, then the own cache's; wave w takes slices w, w + 4, ... of
+// both, eight records in one round trip, and the waves' sums are added in wave order --------------------------------
+// OWN: floats of an own record, whose outputs are its last D
+template <typename T, int D, int OWN>
+__global__ __launch_bounds__(kShThreads) void shared_merge_kernel(sepkv_params p, sepkv_params pp, int n_prefix, int n_own, const int32_t *__restrict__ sizes,
                                                                   const int32_t *__restrict__ prefix_sizes, const int32_t *__restrict__ prefix_of,
                                                                   const float *__restrict__ prefix_part, const float *__restrict__ own_part,
                                                                   T *__restrict__ out, float *__restrict__ lse) {
-    constexpr int REC = kShRecord<D>, OWN = D + 2, C = D / kWave;
-    const int lane = threadIdx.x % kWave;
-    const long row = (long)blockIdx.x * kShWaves + threadIdx.x / kWave;
-    if (row >= (long)p.S * p.Hq) return;
-    const int of = prefix_of[row / p.Hq];
+    constexpr int REC = kShRecord<D>, C = D / kWave, NR = 8;
+    __shared__ float state[kShWaves][D + 2];
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const long row = blockIdx.x;
+    const int seq = (int)(row / p.Hq), of = prefix_of[seq];
     const int np = of >= 0 && of < pp.S ? slices_in_use(entries_of(cache_map(pp, prefix_sizes + SEPKV_SIZES_COLS * of)), n_prefix) : 0;
-    const int total = np + n_own;
+    const int total = np + (OWN == REC ? slices_in_use(entries_of(cache_map(p, sizes + SEPKV_SIZES_COLS * seq)), n_own) : n_own);
     const float *pre = prefix_part + row * n_prefix * REC, *own = own_part + row * n_own * OWN;
-    auto record = [&](int k) { return k < np ? pre + k * REC : own + (k - np) * OWN; };
-    float M = -INFINITY;
-    for (int k = lane; k < total; k += kWave) M = fmaxf(M, record(k)[0]);
+    float M = -INFINITY, l = 0.f, o[C] = {};
+    for (int k0 = wave; k0 < total; k0 += kShWaves * NR) {
+        float m[NR], ls[NR], os[NR][C];
 #pragma unroll
-    for (int o = 1; o < kWave; o *= 2) M = fmaxf(M, __shfl_xor(M, o));
-    float l = 0.f, o[C] = {};
-    for (int k0 = 0; k0 < total; k0 += kWave) {
-        const int n = min(kWave, total - k0);
-        float w = 0.f, ml = 0.f;
-        if (lane < n) {
-            const float *r = record(k0 + lane);
-            w = r[0] == -INFINITY ? 0.f : exp2f(r[0] - M);
-            ml = r[1];
+        for (int i = 0; i < NR; ++i) {
+            const int k = min(k0 + kShWaves * i, total - 1);  // past the last one: that again, with weight 0
+            const float *r = k < np ? pre + k * REC : own + (k - np) * OWN, *v = r + (k < np ? REC : OWN) - D + C * lane;
+            m[i] = r[0], ls[i] = r[1];
+#pragma unroll
+            for (int j = 0; j < C; ++j) os[i][j] = v[j];
         }
-        for (int k = 0; k < n; ++k) {
-            const float wk = __shfl(w, k);
-            const float *r = record(k0 + k) + (k0 + k < np ? 4 : 2) + C * lane;
-            l = fmaf(wk, __shfl(ml, k), l);
+        float Mn = M;
 #pragma unroll
-            for (int i = 0; i < C; ++i) o[i] = fmaf(wk, r[i], o[i]);
+        for (int i = 0; i < NR; ++i) {
+            if (k0 + kShWaves * i >= total) m[i] = -INFINITY;
+            Mn = fmaxf(Mn, m[i]);
+        }
+        if (Mn == -INFINITY) continue;  // slices without an entry
+        const float keep = exp2f(M - Mn);
+        M = Mn;
+        l *= keep;
+#pragma unroll
+        for (int j = 0; j < C; ++j) o[j] *= keep;
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+            const float w = exp2f(m[i] - M);
+            l = fmaf(w, ls[i], l);
+#pragma unroll
+            for (int j = 0; j < C; ++j) o[j] = fmaf(w, os[i][j], o[j]);
         }
     }
+    if (lane == 0) state[wave][D] = M, state[wave][D + 1] = l;
 #pragma unroll
-    for (int i = 0; i < C; ++i) {
-        const float v = l > 0.f ? o[i] / l : 0.f;
-        if constexpr (sizeof(T) == 2) out[row * D + C * lane + i] = decode_f32_to_bf16(v);
-        else out[row * D + C * lane + i] = v;
+    for (int j = 0; j < C; ++j) state[wave][C * lane + j] = o[j];
+    __syncthreads();
+    const int c = threadIdx.x;
+    if (c >= D) return;
+    M = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kShWaves; ++w) M = fmaxf(M, state[w][D]);
+    float lsum = 0.f, v = 0.f;
+#pragma unroll
+    for (int w = 0; w < kShWaves; ++w) {
+        const float wgt = state[w][D] == -INFINITY ? 0.f : exp2f(state[w][D] - M);
+        lsum = fmaf(wgt, state[w][D + 1], lsum);
+        v = fmaf(wgt, state[w][c], v);
     }
-    if (lse && lane == 0) lse[row] = l > 0.f ? (M + log2f(l)) * kLn2_f : -INFINITY;
+    v = lsum > 0.f ? v / lsum : 0.f;
+    if constexpr (sizeof(T) == 2) out[row * D + c] = decode_f32_to_bf16(v);
+    else out[row * D + c] = v;
+    if (lse && c == 0) lse[row] = lsum > 0.f ? (M + log2f(lsum)) * kLn2_f : -INFINITY;
 }
 
 // ---- host ------------------------------------------------------------------------------------------
 struct SharedShape {
-    int rb;        // bf16: row blocks per workgroup
-    int chunks;    // of rows, all prefixes together, at most
-    int n_prefix;  // slices per prefix
-    int n_own;     // slices per own cache
+    bool split_rows;  // bf16: what shared_body's waves share
+    int nb;           // bf16: column blocks of a wave
+    int chunks;       // of rows, all prefixes together, at most
+    int n_prefix;     // slices per prefix
+    int n_own;        // slices per own cache
+    int record;       // floats of an own cache's record
 };
 SharedShape shared_shape(const sepkv_params &p, const sepkv_params &pp) {
     SharedShape s;
     const long gq = p.Hq / p.Hkv, all = p.S * gq, per_prefix = (all + pp.S - 1) / pp.S;
-    s.rb = per_prefix <= 32 ? 1 : per_prefix <= 64 ? 2 : 4;
-    const long rows = p.dtype == SEPATTN_FP32 ? 64 : 32 * s.rb;
+    s.split_rows = per_prefix > 32;
+    s.nb = s.split_rows ? (per_prefix <= 64 ? 1 : per_prefix <= 128 ? 2 : 3) : (per_prefix <= 16 ? 1 : 2);
+    const long rows = p.dtype == SEPATTN_FP32 ? 64 : (s.split_rows ? 64 : 16) * s.nb;
     s.chunks = (int)(pp.S == 1 ? (all + rows - 1) / rows : all / rows + (pp.S < p.S ? pp.S : p.S));
-    const long nb = (pp.c + kShBlock - 1) / kShBlock, groups = (long)p.Hkv * s.chunks;
-    long ns = (2L * compute_units() + groups - 1) / groups;
+    const long nb = (pp.c + kShBlock - 1) / kShBlock, groups = (long)p.Hkv * s.chunks, units = compute_units();
+    long ns = (units + groups - 1) / groups;
     if (ns > nb / 4) ns = nb / 4;
     s.n_prefix = (int)(ns < 1 ? 1 : ns > 64 ? 64 : ns);
-    s.n_own = decode_record_slices(p);
+    if (p.dtype == SEPATTN_FP32) {
+        s.n_own = decode_record_slices(p);
+        s.record = p.d + 2;
+    } else {
+        const long own_groups = (long)p.S * p.Hkv * ((gq + 15) / 16), own_nb = (p.c + kShBlock - 1) / kShBlock;
+        long no = units / own_groups;
+        if (no > own_nb / 4) no = own_nb / 4;
+        s.n_own = (int)(no < 1 ? 1 : no > 64 ? 64 : no);
+        s.record = p.d + 4;
+    }
     return s;
 }
 size_t prefix_record_bytes(const sepkv_params &p, const SharedShape &s) {
@@ -448,42 +731,52 @@ size_t prefix_record_bytes(const sepkv_params &p, const SharedShape &s) {
 
 size_t decode_shared_workspace(const sepkv_params &p, const sepkv_params &pp) {
     const SharedShape s = shared_shape(p, pp);
-    return prefix_record_bytes(p, s) + align_up((size_t)p.S * p.Hq * s.n_own * (p.d + 2) * sizeof(float), 256);
+    return prefix_record_bytes(p, s) + align_up((size_t)p.S * p.Hq * s.n_own * s.record * sizeof(float), 256);
 }
 
 int launch_decode_shared(const SharedDecode &x, hipStream_t st) {
     const SharedShape s = shared_shape(x.p, x.pp);
     float *const own_part = x.part + prefix_record_bytes(x.p, s) / sizeof(float);
-    const PrefixArgs a = {x.p, x.pp, x.p.Hq / x.p.Hkv, s.n_prefix, x.q, x.Kp, x.Vp, x.sizes, x.prefix_sizes, x.group_start, x.group_seq,
+    const int gq = x.p.Hq / x.p.Hkv;
+    const PrefixArgs a = {x.p, x.pp, gq, s.n_prefix, x.q, x.Kp, x.Vp, x.sizes, x.prefix_sizes, x.group_start, x.group_seq,
                           x.rope, x.n_pos, x.part};
-    const dim3 grid(x.p.Hkv, s.chunks, s.n_prefix), block(kShThreads);
-    {
+    const dim3 block(kShThreads);
+    if (x.p.dtype == SEPATTN_FP32) {
+        {
+            ProfScope prof(SEPATTN_K_DECODE_SPLIT, st);
+            const dim3 grid(x.p.Hkv, s.chunks, s.n_prefix);
+            if (x.p.d == 64) hipLaunchKernelGGL((shared_prefix_fp32_kernel<64>), grid, block, 0, st, a);
+            else hipLaunchKernelGGL((shared_prefix_fp32_kernel<128>), grid, block, 0, st, a);
+        }
+        int rc = launch_status();
+        if (rc == SEPATTN_OK) rc = launch_decode_records(x.p, s.n_own, x.q, x.Kc, x.Vc, x.sizes, x.rope, x.n_pos, own_part, st);
+        if (rc != SEPATTN_OK) return rc;
+    } else {
+        const int head_chunks = (gq + 15) / 16;
+        const long n_prefix_groups = (long)x.p.Hkv * s.chunks * s.n_prefix, n = n_prefix_groups + (long)x.p.Hkv * head_chunks * x.p.S * s.n_own;
+        if (n > 0x7FFFFFFFL) return SEPATTN_ERR_SHAPE;
+        const SharedArgs all = {a, x.Kc, x.Vc, own_part, (int)n_prefix_groups, s.chunks, s.n_own, head_chunks};
         ProfScope prof(SEPATTN_K_DECODE_SPLIT, st);
-        auto go = [&](auto D_) {
-            constexpr int D = decltype(D_)::value;
-            if (x.p.dtype == SEPATTN_FP32) {
-                hipLaunchKernelGGL((shared_prefix_fp32_kernel<D>), grid, block, 0, st, a);
-                return;
-            }
-            auto rows = [&](auto RB_) {
-                constexpr int RB = decltype(RB_)::value;
-                if (x.rope) hipLaunchKernelGGL((shared_prefix_kernel<D, RB, true>), grid, block, 0, st, a);
-                else hipLaunchKernelGGL((shared_prefix_kernel<D, RB, false>), grid, block, 0, st, a);
-            };
-            s.rb == 1 ? rows(IntC<1>{}) : s.rb == 2 ? rows(IntC<2>{}) : rows(IntC<4>{});
+        auto go = [&](auto D_, auto NB_, auto ROWS_) {
+            constexpr int D = decltype(D_)::value, NB = decltype(NB_)::value;
+            constexpr bool ROWS = decltype(ROWS_)::value != 0;
+            if (x.rope) hipLaunchKernelGGL((shared_decode_kernel<D, NB, ROWS, true>), dim3((unsigned)n), block, 0, st, all);
+            else hipLaunchKernelGGL((shared_decode_kernel<D, NB, ROWS, false>), dim3((unsigned)n), block, 0, st, all);
         };
-        x.p.d == 64 ? go(IntC<64>{}) : go(IntC<128>{});
+        auto shape = [&](auto D_) {
+            if (s.split_rows) s.nb == 1 ? go(D_, IntC<1>{}, IntC<1>{}) : s.nb == 2 ? go(D_, IntC<2>{}, IntC<1>{}) : go(D_, IntC<3>{}, IntC<1>{});
+            else s.nb == 1 ? go(D_, IntC<1>{}, IntC<0>{}) : go(D_, IntC<2>{}, IntC<0>{});
+        };
+        x.p.d == 64 ? shape(IntC<64>{}) : shape(IntC<128>{});
+        const int rc = launch_status();
+        if (rc != SEPATTN_OK) return rc;
     }
-    int rc = launch_status();
-    if (rc != SEPATTN_OK) return rc;
-    rc = launch_decode_records(x.p, s.n_own, x.q, x.Kc, x.Vc, x.sizes, x.rope, x.n_pos, own_part, st);
-    if (rc != SEPATTN_OK) return rc;
     ProfScope prof(SEPATTN_K_DECODE_MERGE, st);
-    const dim3 merge(((unsigned)(x.p.S * x.p.Hq) + kShWaves - 1) / kShWaves);
     auto go = [&](auto T_, auto D_) {
         using T = decltype(T_);
-        hipLaunchKernelGGL((shared_merge_kernel<T, decltype(D_)::value>), merge, block, 0, st, x.p, x.pp, s.n_prefix, s.n_own, x.prefix_sizes,
-                           x.prefix_of, x.part, own_part, static_cast<T *>(x.out), x.lse);
+        constexpr int D = decltype(D_)::value;
+        hipLaunchKernelGGL((shared_merge_kernel<T, D, sizeof(T) == 2 ? D + 4 : D + 2>), dim3(x.p.S * x.p.Hq), block, 0, st, x.p, x.pp, s.n_prefix, s.n_own,
+                           x.sizes, x.prefix_sizes, x.prefix_of, x.part, own_part, static_cast<T *>(x.out), x.lse);
     };
     if (x.p.dtype == SEPATTN_BF16) x.p.d == 64 ? go(uint16_t{}, IntC<64>{}) : go(uint16_t{}, IntC<128>{});
     else x.p.d == 64 ? go(float{}, IntC<64>{}) : go(float{}, IntC<128>{});

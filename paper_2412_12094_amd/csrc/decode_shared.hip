@@ -10,11 +10,14 @@
 #include "decode_common.h"
 #include "mfma_common.h"
 
+#include <algorithm>
+#include <cmath>
+
 namespace sepattn {
 
 namespace {
 
-constexpr int kShThreads = 256, kShWaves = 4;
+constexpr int kShThreads = 256, kShWaves = 4;         // of the fp32 kernel and of the sum
 constexpr int kShBlock = 32;  // keys per block; slices are whole blocks
 
 // records of the prefixes' slices, [sequence][head][slice]: max (log2 domain), sum, 2 unused, D unnormalised outputs
@@ -65,13 +68,17 @@ __device__ inline bool find_chunk(const PrefixArgs &x, int chunk, Chunk &c) {
 // entries [e0, e1) of a slice; false if it has none
 __device__ inline bool slice_of(int entries, int nsplit, int split, int &e0, int &e1) {
     const int nb = (entries + kShBlock - 1) / kShBlock, per = (nb + nsplit - 1) / nsplit * kShBlock;
-    e0 = min(split * per, entries);
-    e1 = min(entries, e0 + per);
+    e0 = __builtin_amdgcn_readfirstlane(min(split * per, entries));
+    e1 = __builtin_amdgcn_readfirstlane(min(entries, e0 + per));
     return e0 < e1;
 }
-__device__ inline int slices_in_use(int entries, int nsplit) {
-    const int nb = (entries + kShBlock - 1) / kShBlock, per = (nb + nsplit - 1) / nsplit;
-    return per ? (nb + per - 1) / per : 0;
+// the record of a slice without an entry: its outputs are not looked at
+__device__ inline void mark_empty(float *record) { *reinterpret_cast<float2 *>(record) = float2{-INFINITY, 0.f}; }
+// the map of one cache, which is the same in every lane, in scalar registers
+__device__ inline CacheMap uniform_map(const sepkv_params &p, const int32_t *__restrict__ sizes, long cache) {
+    CacheMap m = cache_map(p, sizes + SEPKV_SIZES_COLS * cache);
+    for (int *x : {&m.n_init, &m.n_sep, &m.n_past, &m.n_loc, &m.sep_head, &m.win_head}) *x = __builtin_amdgcn_readfirstlane(*x);
+    return m;
 }
 __device__ inline int entries_of(const CacheMap &m) { return m.n_init + m.n_sep + m.n_past + m.n_loc; }
 
@@ -88,19 +95,21 @@ __device__ inline int query_position(const PrefixArgs &x, int seq, int prefix_en
 }
 
 // ---- bf16 ------------------------------------------------------------------------------------------
-// One workgroup of four waves: rows (queries that read one KV head) against a slice of one cache, in blocks of 32 keys.  Operands as in
+// One workgroup of eight waves: rows (queries that read one KV head) against a slice of one cache, in blocks of 32 keys.  Operands as in
 // decode_wide.hip (v_mfma_f32_16x16x32_bf16, the cache rows as A, 16 queries as the columns of B, score tile t's row 4g+i the block's row
 // 8g+4t+i, so that a lane's probabilities are its operand of the second product); a wave has NB such column blocks, for which it
 // reads the cache's fragments from LDS once.
-//   SPLIT_ROWS: the waves have different rows (64 NB per workgroup) and share the keys, in a ring of four stages of 32 rows of K
-//     and V: three tiles are on their way, one barrier per tile.
+//   SPLIT_ROWS: four waves have different rows (64 NB per workgroup), and two groups of four take the slice's blocks in turn.  A group
+//     shares a ring of four stages of 32 rows of K and V: three tiles are on their way, one barrier per tile.  (With one group per workgroup a
+//     SIMD has one wave of it, nothing of whose waits is hidden; two workgroups per compute unit leave twice as many records.)
 //   otherwise: the waves have the same 16 NB rows and take the blocks in turn, each with a stage of its own, whose K half is refilled
-//     as soon as its fragments are in registers and the V half one step later; no barrier in the loop.  Their states meet in LDS.
+//     as soon as its fragments are in registers and the V half one step later; no barrier in the loop.
+// The groups' or waves' states meet in LDS.
 // KROPE (own caches): keys are turned by their distance to the query, as in decode_wide.hip.  LO (prefixes): the query is turned by its
 // position.  Either is then the sum of two bf16 numbers, 16 bits of mantissa, and the scores are two products: rounded to one
 // number, lse would be off by 1e-3.
-template <int D>
-constexpr int kShLds = 4 * 2 * kShBlock * D;  // elements: four stages of K and V
+template <int D, int NW>
+constexpr int kShLds = NW * 2 * kShBlock * D;  // elements: a stage of K and V per wave
 
 __device__ inline f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 // XOR permutation of the 16-byte chunks of row 8a + 4t + i: see decode_wide.hip
@@ -121,10 +130,12 @@ __device__ inline float groups_sum(float x) {
 }
 template <int N>
 __device__ inline void wait_loads() {
-    static_assert(N == 0 || N == 4 || N == 5 || N == 8 || N == 9, "");
+    static_assert(N == 0 || N == 4 || N == 5 || N == 6 || N == 8 || N == 9 || N == 12, "");
     if constexpr (N == 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     if constexpr (N == 4) asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
     if constexpr (N == 5) asm volatile("s_waitcnt vmcnt(5)" ::: "memory");
+    if constexpr (N == 6) asm volatile("s_waitcnt vmcnt(6)" ::: "memory");
+    if constexpr (N == 12) asm volatile("s_waitcnt vmcnt(12)" ::: "memory");
     if constexpr (N == 8) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
     if constexpr (N == 9) asm volatile("s_waitcnt vmcnt(9)" ::: "memory");
 }
@@ -137,6 +148,22 @@ __device__ inline void barrier() {
 #pragma clang diagnostic ignored "-Wint-to-pointer-cast"
 __device__ inline f32x4 lds_read_f4(uint32_t addr) { return *(const f32x4 __attribute__((address_space(3))) *)addr; }
 #pragma clang diagnostic pop
+
+// decode_slot_of without branches
+__device__ inline int slot_of(const CacheMap &m, int e) {
+    const int k = e - m.n_init, u = k - m.n_sep;
+    const int sep = m.sep_head + k, win = m.win_head + u;
+    const int in_sep = m.a + (sep >= m.s ? sep - m.s : sep), in_win = m.a + m.s + (win >= m.wcap ? win - m.wcap : win);
+    return k < 0 ? e : u < 0 ? in_sep : in_win;
+}
+
+// slot of entry e, and the first entry behind e that does not lie in the slots next to it
+__device__ inline void run_of(const CacheMap &m, int e, int &slot, int &end) {
+    slot = slot_of(m, e);
+    const int k = e - m.n_init, u = k - m.n_sep;
+    const int sep = min(m.n_sep, m.s - m.sep_head), win = min(m.n_past + m.n_loc, m.wcap - m.win_head);  // entries in front of the rings' wraps
+    end = k < 0 ? m.n_init : u < 0 ? m.n_init + (k < sep ? sep : m.n_sep) : m.n_init + m.n_sep + (u < win ? win : m.n_past + m.n_loc);
+}
 
 // a bf16 number and what it leaves of the sum of the two
 __device__ inline void split_hi_lo(const f32x8 &x, bf16x8 &hi, bf16x8 &lo) {
@@ -152,25 +179,24 @@ struct ShRow {
 };
 
 // rows: ShRow of (column block, column)
-template <int D, int NB, bool SPLIT_ROWS, bool KROPE, bool LO, typename Rows>
+template <int D, int NW, int NB, bool SPLIT_ROWS, bool KROPE, bool LO, typename Rows>
 __device__ __forceinline__ void shared_body(const CacheMap &cm, const uint16_t *__restrict__ Kh, const uint16_t *__restrict__ Vh, int e0, int e1,
                                             int last /* KROPE: position of the query within the cache */, const float *__restrict__ rope,
-                                            int n_pos, float sl2, uint16_t (&smem)[kShLds<D>], float (&base_s)[kShWaves][2][128], const Rows &rows) {
+                                            int n_pos, float sl2, uint16_t (&smem)[kShLds<D, NW>], float (&base_s)[NW][2][128], const Rows &rows) {
     static_assert(!KROPE || (NB == 1 && !SPLIT_ROWS && !LO), "");
     constexpr int CH = D / 8, RPL = 64 / CH;                         // 16-byte chunks per row, rows per wave-wide load
-    constexpr int NLD = kShBlock / RPL / (SPLIT_ROWS ? kShWaves : 1);  // a wave's loads per block and tensor
+    constexpr int RW = 4, KG = NW / RW;                       // SPLIT_ROWS: waves per group, groups
+    constexpr int NLD = kShBlock / RPL / (SPLIT_ROWS ? RW : 1);  // a wave's loads per block and tensor
     constexpr int KSTEPS = D / 32, KS2 = KSTEPS / 2, DB = D / 16, TILE = kShBlock * D;
     constexpr int STAGES = 4;
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int col = lane & 15, g = lane >> 4;
+    const int col = lane & 15, g = lane >> 4, rw = wave % RW, kg = wave / RW;
 
     // queries; a turned one in two parts
     bf16x8 qhi[NB][KSTEPS], qlo[LO ? NB : 1][LO ? KSTEPS : 1];
-    float *record[NB];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-        const ShRow r = rows(SPLIT_ROWS ? wave * NB + nb : nb, col);
-        record[nb] = r.record;
+        const ShRow r = rows(SPLIT_ROWS ? rw * NB + nb : nb, col);
 #pragma unroll
         for (int ks = 0; ks < KSTEPS; ++ks) qhi[nb][ks] = as_bf16x8(*reinterpret_cast<const u32x4 *>(r.q + 32 * ks + 8 * g));
         if constexpr (LO) {
@@ -194,23 +220,53 @@ __device__ __forceinline__ void shared_body(const CacheMap &cm, const uint16_t *
         }
     }
 
+    // The queries have arrived: without this the compiler waits for them, and with them for every row on its way, in each round of the loop.
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int ks = 0; ks < KSTEPS; ++ks) asm volatile("" : "+v"(qhi[nb][ks]));
+
     // loads: the wave's share of block eb's K or V rows into a stage; entries past the end: the last one (masked)
     const int my_pc = lane % CH, my_sub = lane / CH;
     const uint32_t lds0 = lds_addr(&smem[0]);
-    const int stage_row0 = SPLIT_ROWS ? wave * (kShBlock / kShWaves) : 0;  // first of the rows that this wave loads
-    uint32_t off[NLD];
-    auto place = [&](int eb) __attribute__((always_inline)) {
-        static_for<NLD>([&](auto U) {
-            constexpr int u = U;
-            const int r = stage_row0 + u * RPL + my_sub;
-            off[u] = (uint32_t)decode_slot_of(cm, min(eb + r, e1 - 1)) * (uint32_t)(D * 2) + (uint32_t)((my_pc ^ sh_swz<D>(r)) * 16);
-        });
+    const int stage_row0 = SPLIT_ROWS ? rw * (kShBlock / RW) : 0;  // first of the rows that this wave loads
+    // Where a block's rows lie: nearly always in one run of slots, whose lanes' offsets never change; else a slot per row.
+    uint32_t run_off[NLD];
+#pragma unroll
+    for (int u = 0; u < NLD; ++u) {
+        const int r = stage_row0 + u * RPL + my_sub;
+        run_off[u] = (uint32_t)(r * D * 2) + (uint32_t)((my_pc ^ sh_swz<D>(r)) * 16);
+    }
+    struct Place {
+        int first;          // slot that the offsets count from
+        uint32_t off[NLD];
     };
-    auto load_rows = [&](const uint16_t *from, uint32_t stage) __attribute__((always_inline)) {
+    int run_slot = 0, run_e = 0, run_end = 0;  // entry run_e lies in run_slot, those from there to run_end behind it
+    auto place = [&](int eb) __attribute__((always_inline)) {
+        Place at;
+        if (eb + kShBlock <= run_end) {
+            at.first = run_slot + (eb - run_e);
+#pragma unroll
+            for (int u = 0; u < NLD; ++u) at.off[u] = run_off[u];
+        } else {
+            at.first = 0;
+#pragma unroll
+            for (int u = 0; u < NLD; ++u) {
+                const int r = stage_row0 + u * RPL + my_sub;
+                at.off[u] = (uint32_t)slot_of(cm, min(eb + r, e1 - 1)) * (uint32_t)(D * 2) + (uint32_t)((my_pc ^ sh_swz<D>(r)) * 16);
+            }
+            run_e = min(eb + kShBlock, e1);
+            run_of(cm, run_e, run_slot, run_end);
+            run_end = min(run_end, e1);
+        }
+        return at;
+    };
+    auto load_rows = [&](const uint16_t *from, const Place &at, uint32_t stage) __attribute__((always_inline)) {
+        from += (long)__builtin_amdgcn_readfirstlane(at.first) * D;
         static_for<NLD>([&](auto U) {
             const uint32_t to = stage + (stage_row0 + U * RPL) * D * 2;
-            if constexpr (SPLIT_ROWS) dma_to_lds_16(from, off[U], to);  // the other chunks of rows read them as well
-            else dma_to_lds_16_nt(from, off[U], to);
+            if constexpr (SPLIT_ROWS) dma_to_lds_16(from, at.off[U], to);  // the other chunks of rows read them as well
+            else dma_to_lds_16_nt(from, at.off[U], to);
         });
     };
     auto k_stage = [&](int i) { return lds0 + (uint32_t)(i * 2 * TILE * 2); };
@@ -229,112 +285,214 @@ __device__ __forceinline__ void shared_body(const CacheMap &cm, const uint16_t *
     const uint32_t kswz = sh_swz<D>(krow), vswz = sh_swz<D>(vrow);
     const uint32_t koff = krow * D * 2, voff = vrow * D * 2 + ((col & 1) << 3);
 
-    f32x4 s[NB][2];
-    auto clear_scores = [&]() __attribute__((always_inline)) {
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) s[nb][0] = s[nb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-    };
     auto key_fragment = [&](uint32_t stage, int t, int ks) __attribute__((always_inline)) {
         return lds_read_b128_at(stage + koff + 4 * t * D * 2 + (((uint32_t)(4 * ks + g) ^ kswz) << 4));
     };
     auto value_fragment = [&](uint32_t stage, int db) __attribute__((always_inline)) {
         return lds_read_tr_at(stage + voff + (((uint32_t)(2 * db + ((col & 3) >> 1)) ^ vswz) << 4), 4 * D * 2);
     };
-    // scores -> probabilities of block nb (bf16), maximum, sum and outputs carried on; n_valid >= 1 entries
-    auto softmax = [&](int n_valid, bf16x8 (&pb)[NB]) __attribute__((always_inline)) {
-        float alpha[NB];
-        bool any = false;
+    // Scores of column block nb -> its probabilities against the maximum so far.  That one is raised only where a lane's probabilities sum to
+    // more than 2^8 (or there is none yet): a sum in fp32 and a product of bf16 numbers are as exact with a factor, and looking for every
+    // block's maximum is a third of the vector instructions.  Entries past the slice's end: minus infinity.
+    constexpr float kMost = 256.f;
+    auto exponentials = [&](const f32x4 (&s)[2], int nb, f32x8 &p) __attribute__((always_inline)) {
+        float psum = 0.f;
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-            float x[8] = {s[nb][0][0], s[nb][0][1], s[nb][0][2], s[nb][0][3], s[nb][1][0], s[nb][1][1], s[nb][1][2], s[nb][1][3]};  // rows 8g ..
-            if (n_valid < kShBlock) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = 8 * g + i < n_valid ? x[i] : -INFINITY;
-            }
-            const float m_loc = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-            const float m_new = fmaxf(m_run[nb], groups_max(m_loc) * sl2);  // finite: row 0 of a block is valid
-            alpha[nb] = __builtin_amdgcn_exp2f(m_run[nb] - m_new);
-            any |= alpha[nb] != 1.f;
-            m_run[nb] = m_new;
-            float psum = 0.f;
-            f32x8 p;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                p[i] = __builtin_amdgcn_exp2f(fmaf(x[i], sl2, -m_new));
-                psum += p[i];
-            }
-            l_run[nb] = l_run[nb] * alpha[nb] + psum;
-            pb[nb] = __builtin_convertvector(p, bf16x8);
+        for (int i = 0; i < 8; ++i) {
+            p[i] = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], sl2, -m_run[nb]));
+            psum += p[i];
         }
-        if (__builtin_amdgcn_ballot_w64(any) != 0ull) {
+        return psum;
+    };
+    auto mask_tail = [&](f32x4 (&s)[2], int n_valid) __attribute__((always_inline)) {
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
+        for (int i = 0; i < 8; ++i) s[i >> 2][i & 3] = 8 * g + i < n_valid ? s[i >> 2][i & 3] : -INFINITY;
+    };
+    auto raise = [&](const f32x4 (&s)[2], int nb, f32x8 &p) __attribute__((always_inline)) {
+        float m = s[0][0];
 #pragma unroll
-                for (int db = 0; db < DB; ++db) oacc[nb][db] *= alpha[nb];
-        }
+        for (int i = 1; i < 8; ++i) m = fmaxf(m, s[i >> 2][i & 3]);
+        m = fmaxf(m_run[nb], groups_max(m) * sl2);  // finite: row 0 of a block is valid
+        const float alpha = __builtin_amdgcn_exp2f(m_run[nb] - m);
+        m_run[nb] = m;
+        l_run[nb] *= alpha;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) oacc[nb][db] *= alpha;
+        return exponentials(s, nb, p);
     };
 
     if constexpr (SPLIT_ROWS) {
-        const int blocks = (e1 - e0 + kShBlock - 1) / kShBlock;
-        // (blocks past the end are loaded as well, the last row over and over: the number of loads on their way stays the same)
-        auto request = [&](int i) __attribute__((always_inline)) {
-            place(e0 + i * kShBlock);
-            load_rows(Kh, k_stage(i % STAGES));
-            load_rows(Vh, v_stage(i % STAGES));
-        };
-        for (int i = 0; i < STAGES - 1; ++i) request(i);
-        for (int i = 0; i < blocks; ++i) {
-            wait_loads<2 * NLD *(STAGES - 2)>();
-            barrier();  // everyone's part of tile i has landed, and everyone is done with tile i - 1
-            request(i + STAGES - 1);
-            const uint32_t ks_ = k_stage(i % STAGES), vs_ = v_stage(i % STAGES);
-            clear_scores();
+        const int blocks = ((e1 - e0 + kShBlock - 1) / kShBlock + KG - 1) / KG;  // of a group
+        const int stage0 = kg * STAGES;
+        // Where the registers allow it, a wave reads a tile's K fragments one tile ahead and its V fragments in front of the exponentials, so
+        // that neither is waited for; K then runs one tile ahead of V through the ring.  (Blocks past the end are loaded as
+        // well, the last row over and over: the number of loads on their way stays the same.)
+        constexpr bool AHEAD = D == 64 || NB * (LO ? 2 : 1) <= 2, EARLY_V = D == 64 || NB <= 2;
+        auto where = [&](int i) __attribute__((always_inline)) { return place(e0 + (i * KG + kg) * kShBlock); };
+        auto request_k = [&](int i, const Place &at) __attribute__((always_inline)) { load_rows(Kh, at, k_stage(stage0 + i % STAGES)); };
+        auto request_v = [&](int i, const Place &at) __attribute__((always_inline)) { load_rows(Vh, at, v_stage(stage0 + i % STAGES)); };
+        bf16x8 ka[2][KSTEPS];
+        auto read_keys = [&](int i) __attribute__((always_inline)) {
 #pragma unroll
             for (int ks = 0; ks < KSTEPS; ++ks)
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    const bf16x8 ka = key_fragment(ks_, t, ks);
+                for (int t = 0; t < 2; ++t) ka[t][ks] = key_fragment(k_stage(stage0 + i % STAGES), t, ks);
+        };
+        Place at = where(0);
+        request_k(0, at);
+        if constexpr (!AHEAD) request_v(0, at);
+        for (int i = 1; i < STAGES - (AHEAD ? 0 : 1); ++i) {
+            const Place next = where(i);
+            request_k(i, next);
+            request_v(AHEAD ? i - 1 : i, AHEAD ? at : next);
+            at = next;
+        }
+        if constexpr (AHEAD) {
+            wait_loads<2 * NLD *(STAGES - 1)>();
+            barrier();
+            read_keys(0);
+        }
+        for (int i = 0; i < blocks; ++i) {
+            wait_loads<2 * NLD *(STAGES - 2)>();
+            if constexpr (AHEAD) wait_lds();
+            barrier();  // everyone's part of V tile i and of K tile i (AHEAD: i + 1) has landed, and everyone has read what lay where the next ones go
+            const int n_valid = e1 - e0 - (i * KG + kg) * kShBlock;
+            const uint32_t k_at = k_stage(stage0 + i % STAGES), v_at = v_stage(stage0 + i % STAGES);
+            // (else two steps' fragments in front of their use, which the scheduling fences keep there)
+            constexpr int EARLY = 2;
+            auto read_step = [&](int ks) __attribute__((always_inline)) {
 #pragma unroll
-                    for (int nb = 0; nb < NB; ++nb) {
-                        s[nb][t] = mfma16(ka, qhi[nb][ks], s[nb][t]);
-                        if constexpr (LO) s[nb][t] = mfma16(ka, qlo[nb][ks], s[nb][t]);
-                    }
-                }
-            bf16x8 pb[NB];
-            softmax(e1 - e0 - i * kShBlock, pb);
+                for (int t = 0; t < 2; ++t) ka[t][ks] = key_fragment(k_at, t, ks);
+            };
+            if constexpr (!AHEAD) {
 #pragma unroll
-            for (int db = 0; db < DB; ++db) {
-                const bf16x8 va = value_fragment(vs_, db);
-#pragma unroll
-                for (int nb = 0; nb < NB; ++nb) oacc[nb][db] = mfma16(va, pb[nb], oacc[nb][db]);
+                for (int ks = 0; ks < EARLY; ++ks) read_step(ks);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            wait_lds();
+            {
+                const Place next = where(i + STAGES - (AHEAD ? 0 : 1));
+                request_k(i + STAGES - (AHEAD ? 0 : 1), next);
+                request_v(i + STAGES - 1, AHEAD ? at : next);
+                at = next;
+            }
+            if (n_valid > 0) {  // (the second group's last block may be past the end)
+                f32x4 s[NB][2];
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) s[nb][0] = s[nb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+                static_for<KSTEPS>([&](auto KS) __attribute__((always_inline)) {
+                    constexpr int ks = KS;
+                    if constexpr (!AHEAD && ks + EARLY < KSTEPS) {
+                        read_step(ks + EARLY);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+#pragma unroll
+                        for (int nb = 0; nb < NB; ++nb) {
+                            s[nb][t] = mfma16(ka[t][ks], qhi[nb][ks], s[nb][t]);
+                            if constexpr (LO) s[nb][t] = mfma16(ka[t][ks], qlo[nb][ks], s[nb][t]);
+                        }
+                });
+                bf16x8 va[DB];
+#pragma unroll
+                for (int db = 0; db < (EARLY_V ? DB : EARLY); ++db) va[db] = value_fragment(v_at, db);
+                if constexpr (AHEAD) read_keys(i + 1);
+                if constexpr (!EARLY_V) __builtin_amdgcn_sched_barrier(0);
+                if (n_valid < kShBlock) {
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) mask_tail(s[nb], n_valid);
+                }
+                f32x8 p[NB];
+                float psum[NB];
+                bool over = false;
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    psum[nb] = exponentials(s[nb], nb, p[nb]);
+                    over |= !(psum[nb] <= kMost);
+                }
+                if (__builtin_amdgcn_ballot_w64(over) != 0ull) {
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) psum[nb] = raise(s[nb], nb, p[nb]);
+                }
+                bf16x8 pb[NB];
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    l_run[nb] += psum[nb];
+                    pb[nb] = __builtin_convertvector(p[nb], bf16x8);
+                }
+                static_for<DB>([&](auto DBI) __attribute__((always_inline)) {
+                    constexpr int db = DBI;
+                    if constexpr (!EARLY_V && db + EARLY < DB) {
+                        va[db + EARLY] = value_fragment(v_at, db + EARLY);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) oacc[nb][db] = mfma16(va[db], pb[nb], oacc[nb][db]);
+                    if constexpr (!EARLY_V) __builtin_amdgcn_sched_barrier(0);
+                });
+            }
+            if constexpr (!AHEAD) wait_lds();
         }
         wait_loads<0>();
+        // ---- the second group's states meet the first's
+        constexpr int REC = kShRecord<D>;
+        static_assert(KG == 1 || KG == 2 && RW * NB * 16 * REC * sizeof(float) <= kShLds<D, NW> * sizeof(uint16_t), "");
+        float *const red = reinterpret_cast<float *>(&smem[0]) + (rw * NB * 16 + col) * REC;
+        if constexpr (KG > 1) __syncthreads();
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-            const float l = groups_sum(l_run[nb]);
-            if (!record[nb]) continue;
-            if (g == 0) *reinterpret_cast<float2 *>(record[nb]) = float2{m_run[nb], l};
+            l_run[nb] = groups_sum(l_run[nb]);
+            if (KG == 1 || kg == 0) continue;
+            float *const r = red + nb * 16 * REC;
+            if (g == 0) *reinterpret_cast<float2 *>(r) = float2{m_run[nb], l_run[nb]};
 #pragma unroll
-            for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4 *>(record[nb] + 4 + 16 * db + 4 * g) = oacc[nb][db];
+            for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4 *>(r + 4 + 16 * db + 4 * g) = oacc[nb][db];
+        }
+        if constexpr (KG > 1) {
+            __syncthreads();
+            if (kg > 0) return;
+        }
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            float *const to = rows(rw * NB + nb, col).record;
+            if (!to) continue;
+            if constexpr (KG == 1) {
+                if (g == 0) *reinterpret_cast<float2 *>(to) = float2{m_run[nb], l_run[nb]};
+#pragma unroll
+                for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4 *>(to + 4 + 16 * db + 4 * g) = oacc[nb][db];
+                continue;
+            }
+            const float *r = red + nb * 16 * REC;
+            const float2 ml = *reinterpret_cast<const float2 *>(r);
+            const float M = fmaxf(m_run[nb], ml.x);  // finite: the slice's first block is this group's
+            const float mine = __builtin_amdgcn_exp2f(m_run[nb] - M), other = __builtin_amdgcn_exp2f(ml.x - M);
+            if (g == 0) *reinterpret_cast<float2 *>(to) = float2{M, fmaf(other, ml.y, mine * l_run[nb])};
+#pragma unroll
+            for (int db = 0; db < DB; ++db) {
+                const f32x4 o = *reinterpret_cast<const f32x4 *>(r + 4 + 16 * db + 4 * g);
+                f32x4 v;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = fmaf(other, o[i], mine * oacc[nb][db][i]);
+                *reinterpret_cast<f32x4 *>(to + 4 + 16 * db + 4 * g) = v;
+            }
         }
     } else {
         const uint32_t ks_ = k_stage(wave), vs_ = v_stage(wave), bs_ = lds_addr(&base_s[wave][0][0]), ts_ = lds0;
+        Place at;
         auto request_keys = [&](int eb, int par) __attribute__((always_inline)) {
-            place(eb);
+            at = place(eb);
             if constexpr (KROPE) {  // the table row of the first entry's distance
                 if (lane < D / 4) dma_to_lds_16(rope + (long)min(last - eb, n_pos - 1) * D, lane * 16, bs_ + par * D * 4);
             }
-            load_rows(Kh, ks_);
+            load_rows(Kh, at, ks_);
         };
         int eb = e0 + wave * kShBlock;
         const bool some = eb < e1;
         // cos / sin of the lane's two rows krow + 4t within a block: table rows 0 .. 31, through LDS, over the V stages of the first waves
         f32x4 rc[2][KS2][2], rs[2][KS2][2];
         if constexpr (KROPE) {
-            constexpr int TCH = D / 4, TRPL = 64 / TCH, TLD = kShBlock / TRPL / kShWaves;
-            static_assert(TLD * TRPL * kShWaves == kShBlock, "");
+            constexpr int TCH = D / 4, TRPL = 64 / TCH, TLD = kShBlock / TRPL / NW;
+            static_assert(TLD >= 1 && TLD * TRPL * NW == kShBlock, "");
             // (where row r goes: the V stages lie apart; half a stage holds 16 rows at either d)
             auto table_row = [&](int r) { return v_stage(r >> 4) + (uint32_t)((r & 15) * D * 4); };
             static_assert(16 * D * 4 <= 2 * TILE, "");
@@ -362,13 +520,13 @@ __device__ __forceinline__ void shared_body(const CacheMap &cm, const uint16_t *
                     }
             wait_lds();
             barrier();
-            if (some) load_rows(Vh, vs_);
+            if (some) load_rows(Vh, at, vs_);
         } else if (some) {
             request_keys(eb, 0);
-            load_rows(Vh, vs_);
+            load_rows(Vh, at, vs_);
         }
-        for (int par = 0; eb < e1; eb += kShWaves * kShBlock, par ^= 1) {
-            const bool more = eb + kShWaves * kShBlock < e1;
+        for (int par = 0; eb < e1; eb += NW * kShBlock, par ^= 1) {
+            const bool more = eb + NW * kShBlock < e1;
             const int n_valid = e1 - eb;
             wait_loads<NLD>();  // the K rows; the V rows may be in flight
             bf16x8 ka[2][KSTEPS];
@@ -388,9 +546,11 @@ __device__ __forceinline__ void shared_body(const CacheMap &cm, const uint16_t *
             }
             if (more) {
                 wait_lds();
-                request_keys(eb + kShWaves * kShBlock, par ^ 1);
+                request_keys(eb + NW * kShBlock, par ^ 1);
             }
-            clear_scores();
+            f32x4 s[NB][2];
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) s[nb][0] = s[nb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
             if constexpr (KROPE) {
                 // R(-distance): (x, y) -> (x cos + y sin, y cos - x sin), dimension i with i + D/2; row r's distance is that of the
                 // block's first entry minus r
@@ -431,10 +591,18 @@ __device__ __forceinline__ void shared_body(const CacheMap &cm, const uint16_t *
             for (int db = 0; db < DB; ++db) va[db] = value_fragment(vs_, db);
             if (more) {
                 wait_lds();
-                load_rows(Vh, vs_);
+                load_rows(Vh, at, vs_);
             }
             bf16x8 pb[NB];
-            softmax(n_valid, pb);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                f32x8 p;
+                if (n_valid < kShBlock) mask_tail(s[nb], n_valid);
+                float psum = exponentials(s[nb], nb, p);
+                if (__builtin_amdgcn_ballot_w64(!(psum <= kMost)) != 0ull) psum = raise(s[nb], nb, p);
+                l_run[nb] += psum;
+                pb[nb] = __builtin_convertvector(p, bf16x8);
+            }
 #pragma unroll
             for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -442,7 +610,7 @@ __device__ __forceinline__ void shared_body(const CacheMap &cm, const uint16_t *
         }
         // ---- the waves' states meet in LDS, one column block after the other; a thread adds two columns of a row
         constexpr int REC = kShRecord<D>;
-        static_assert(kShWaves * 16 * REC * sizeof(float) <= kShLds<D> * sizeof(uint16_t), "");
+        static_assert(NW * 16 * REC * sizeof(float) <= kShLds<D, NW> * sizeof(uint16_t), "");
         float *red = reinterpret_cast<float *>(&smem[0]);  // [wave][row][REC]
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
@@ -453,15 +621,15 @@ __device__ __forceinline__ void shared_body(const CacheMap &cm, const uint16_t *
 #pragma unroll
             for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4 *>(r + 4 + 16 * db + 4 * g) = oacc[nb][db];
             __syncthreads();
-            for (int item = threadIdx.x; item < 16 * (D / 2); item += kShThreads) {
+            for (int item = threadIdx.x; item < 16 * (D / 2); item += (64 * NW)) {
                 const int row = item / (D / 2), c2 = item % (D / 2);
                 float *to = rows(nb, row).record;
                 if (!to) continue;
                 float M = -INFINITY, lsum = 0.f, o0 = 0.f, o1 = 0.f;
 #pragma unroll
-                for (int w = 0; w < kShWaves; ++w) M = fmaxf(M, red[(w * 16 + row) * REC]);
+                for (int w = 0; w < NW; ++w) M = fmaxf(M, red[(w * 16 + row) * REC]);
 #pragma unroll
-                for (int w = 0; w < kShWaves; ++w) {
+                for (int w = 0; w < NW; ++w) {
                     const float *x = red + (w * 16 + row) * REC;
                     const float wgt = __builtin_amdgcn_exp2f(x[0] - M);  // M is finite: the slice has an entry
                     lsum = fmaf(wgt, x[1], lsum);
@@ -483,24 +651,31 @@ struct SharedArgs {
     float *own_part;
     int n_prefix_groups, chunks, n_own, head_chunks;
 };
-template <int D, int NB, bool SPLIT_ROWS, bool ROPE>
-__global__ __launch_bounds__(kShThreads, D == 64 ? 3 : 2) void shared_decode_kernel(SharedArgs a) {
+template <int D, int NW, int NB, bool SPLIT_ROWS, bool ROPE>
+__global__ __launch_bounds__(64 * NW, 8 / NW) void shared_decode_kernel(SharedArgs a) {
     constexpr int REC = kShRecord<D>;
-    __shared__ __attribute__((aligned(1024))) uint16_t smem[kShLds<D>];
-    __shared__ __attribute__((aligned(1024))) float base_s[kShWaves][2][128];
+    __shared__ __attribute__((aligned(1024))) uint16_t smem[kShLds<D, NW>];
+    __shared__ __attribute__((aligned(1024))) float base_s[NW][2][128];
     const PrefixArgs &x = a.x;
     const float sl2 = x.p.scale * kLog2e_f;
     const int Hkv = x.p.Hkv;
     int id = blockIdx.x;
     if (id < a.n_prefix_groups) {
-        constexpr int ROWS = (SPLIT_ROWS ? kShWaves : 1) * 16 * NB;
+        constexpr int ROWS = (SPLIT_ROWS ? 4 : 1) * 16 * NB;
         const int kv = id % Hkv, chunk = id / Hkv % a.chunks, split = id / Hkv / a.chunks;
         Chunk c;
         if (!find_chunk<ROWS>(x, chunk, c)) return;
-        const CacheMap cm = cache_map(x.pp, x.prefix_sizes + SEPKV_SIZES_COLS * c.prefix);
+        const CacheMap cm = uniform_map(x.pp, x.prefix_sizes, c.prefix);
         const int np = entries_of(cm);
         int e0, e1;
-        if (!slice_of(np, x.nsplit, split, e0, e1)) return;
+        if (!slice_of(np, x.nsplit, split, e0, e1)) {
+            if (threadIdx.x < ROWS && c.row0 + (int)threadIdx.x < c.rows) {
+                int seq, head;
+                row_of(x, c, c.row0 + threadIdx.x, seq, head);
+                mark_empty(x.part + (((long)seq * x.p.Hq + kv * x.gq + head) * x.nsplit + split) * REC);
+            }
+            return;
+        }
         const long head0 = ((long)c.prefix * Hkv + kv) * (long)x.pp.c * D;
         auto rows = [&](int block, int col) __attribute__((always_inline)) {
             const int r = c.row0 + block * 16 + col;
@@ -510,23 +685,27 @@ __global__ __launch_bounds__(kShThreads, D == 64 ? 3 : 2) void shared_decode_ker
             return ShRow{static_cast<const uint16_t *>(x.q) + row * D, ROPE ? query_position(x, seq, np) : 0,
                          r < c.rows ? x.part + (row * x.nsplit + split) * REC : nullptr};
         };
-        shared_body<D, NB, SPLIT_ROWS, false, ROPE>(cm, static_cast<const uint16_t *>(x.Kp) + head0, static_cast<const uint16_t *>(x.Vp) + head0, e0, e1, 0,
+        shared_body<D, NW, NB, SPLIT_ROWS, false, ROPE>(cm, static_cast<const uint16_t *>(x.Kp) + head0, static_cast<const uint16_t *>(x.Vp) + head0, e0, e1, 0,
                                                     x.rope, x.n_pos, sl2, smem, base_s, rows);
         return;
     }
     id -= a.n_prefix_groups;
     const int kv = id % Hkv, hc = id / Hkv % a.head_chunks, seq = id / Hkv / a.head_chunks % x.p.S, split = id / Hkv / a.head_chunks / x.p.S;
-    const CacheMap cm = cache_map(x.p, x.sizes + SEPKV_SIZES_COLS * seq);
+    const CacheMap cm = uniform_map(x.p, x.sizes, seq);
     const int nv = entries_of(cm);
     int e0, e1;
-    if (!slice_of(nv, a.n_own, split, e0, e1)) return;
+    if (!slice_of(nv, a.n_own, split, e0, e1)) {
+        const int head = hc * 16 + threadIdx.x;
+        if (threadIdx.x < 16 && head < x.gq) mark_empty(a.own_part + (((long)seq * x.p.Hq + kv * x.gq + head) * a.n_own + split) * REC);
+        return;
+    }
     const long head0 = ((long)seq * Hkv + kv) * (long)x.p.c * D;
     auto rows = [&](int, int col) __attribute__((always_inline)) {
         const int head = hc * 16 + col;
         const long row = (long)seq * x.p.Hq + kv * x.gq + min(head, x.gq - 1);
         return ShRow{static_cast<const uint16_t *>(x.q) + row * D, 0, head < x.gq ? a.own_part + (row * a.n_own + split) * REC : nullptr};
     };
-    shared_body<D, 1, false, ROPE, false>(cm, static_cast<const uint16_t *>(a.Kc) + head0, static_cast<const uint16_t *>(a.Vc) + head0, e0, e1, nv - 1, x.rope,
+    shared_body<D, NW, 1, false, ROPE, false>(cm, static_cast<const uint16_t *>(a.Kc) + head0, static_cast<const uint16_t *>(a.Vc) + head0, e0, e1, nv - 1, x.rope,
                                           x.n_pos, sl2, smem, base_s, rows);
 }
 
@@ -547,7 +726,14 @@ __global__ __launch_bounds__(kShThreads) void shared_prefix_fp32_kernel(PrefixAr
     const CacheMap cm = cache_map(x.pp, x.prefix_sizes + SEPKV_SIZES_COLS * c.prefix);
     const int np = entries_of(cm);
     int e0, e1;
-    if (!slice_of(np, x.nsplit, split, e0, e1)) return;
+    if (!slice_of(np, x.nsplit, split, e0, e1)) {
+        if (threadIdx.x < ROWS && c.row0 + (int)threadIdx.x < c.rows) {
+            int seq, head;
+            row_of(x, c, c.row0 + threadIdx.x, seq, head);
+            mark_empty(x.part + (((long)seq * x.p.Hq + kv * x.gq + head) * x.nsplit + split) * REC);
+        }
+        return;
+    }
     const float *Kh = static_cast<const float *>(x.Kp) + ((long)c.prefix * x.p.Hkv + kv) * (long)x.pp.c * D;
     const float *Vh = static_cast<const float *>(x.Vp) + ((long)c.prefix * x.p.Hkv + kv) * (long)x.pp.c * D;
     int seq, head;
@@ -623,20 +809,21 @@ __global__ __launch_bounds__(kShThreads) void shared_prefix_fp32_kernel(PrefixAr
 }
 
 // ---- the slices' sum: a workgroup per (sequence, head), prefix slices first, then the own cache's; wave w takes slices w, w + 4, ... of
-// both, eight records in one round trip, and the waves' sums are added in wave order --------------------------------
+// both, eight records in one round trip, and the waves' sums are added in wave order.  Nothing but the records has to be read for that (a
+// slice without an entry says so in its own; those of a prefix that the sequence does not have are skipped), so that the kernel is one
+// round trip and its launch --------------------------------
 // OWN: floats of an own record, whose outputs are its last D
 template <typename T, int D, int OWN>
-__global__ __launch_bounds__(kShThreads) void shared_merge_kernel(sepkv_params p, sepkv_params pp, int n_prefix, int n_own, const int32_t *__restrict__ sizes,
-                                                                  const int32_t *__restrict__ prefix_sizes, const int32_t *__restrict__ prefix_of,
-                                                                  const float *__restrict__ prefix_part, const float *__restrict__ own_part,
-                                                                  T *__restrict__ out, float *__restrict__ lse) {
+__global__ __launch_bounds__(kShThreads) void shared_merge_kernel(sepkv_params p, int n_prefixes, int n_prefix, int n_own,
+                                                                  const int32_t *__restrict__ prefix_of, const float *__restrict__ prefix_part,
+                                                                  const float *__restrict__ own_part, T *__restrict__ out, float *__restrict__ lse) {
     constexpr int REC = kShRecord<D>, C = D / kWave, NR = 8;
     __shared__ float state[kShWaves][D + 2];
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const long row = blockIdx.x;
-    const int seq = (int)(row / p.Hq), of = prefix_of[seq];
-    const int np = of >= 0 && of < pp.S ? slices_in_use(entries_of(cache_map(pp, prefix_sizes + SEPKV_SIZES_COLS * of)), n_prefix) : 0;
-    const int total = np + (OWN == REC ? slices_in_use(entries_of(cache_map(p, sizes + SEPKV_SIZES_COLS * seq)), n_own) : n_own);
+    const int head = blockIdx.x, seq = blockIdx.y;
+    const long row = (long)seq * p.Hq + head;
+    const int of = prefix_of[seq];
+    const int total = n_prefix + n_own;
     const float *pre = prefix_part + row * n_prefix * REC, *own = own_part + row * n_own * OWN;
     float M = -INFINITY, l = 0.f, o[C] = {};
     for (int k0 = wave; k0 < total; k0 += kShWaves * NR) {
@@ -644,15 +831,18 @@ __global__ __launch_bounds__(kShThreads) void shared_merge_kernel(sepkv_params p
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
             const int k = min(k0 + kShWaves * i, total - 1);  // past the last one: that again, with weight 0
-            const float *r = k < np ? pre + k * REC : own + (k - np) * OWN, *v = r + (k < np ? REC : OWN) - D + C * lane;
-            m[i] = r[0], ls[i] = r[1];
+            const float *r = k < n_prefix ? pre + k * REC : own + (k - n_prefix) * OWN, *v = r + (k < n_prefix ? REC : OWN) - D + C * lane;
+            const float2 ml = *reinterpret_cast<const float2 *>(r);
+            m[i] = ml.x, ls[i] = ml.y;
 #pragma unroll
             for (int j = 0; j < C; ++j) os[i][j] = v[j];
         }
+        const bool shares = of >= 0 && of < n_prefixes;
         float Mn = M;
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
-            if (k0 + kShWaves * i >= total) m[i] = -INFINITY;
+            const int k = k0 + kShWaves * i;
+            if (k >= total || (k < n_prefix && !shares)) m[i] = -INFINITY;
             Mn = fmaxf(Mn, m[i]);
         }
         if (Mn == -INFINITY) continue;  // slices without an entry
@@ -663,10 +853,11 @@ __global__ __launch_bounds__(kShThreads) void shared_merge_kernel(sepkv_params p
         for (int j = 0; j < C; ++j) o[j] *= keep;
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
-            const float w = exp2f(m[i] - M);
-            l = fmaf(w, ls[i], l);
+            const bool used = m[i] != -INFINITY;  // (else the rest of the record is whatever the memory held)
+            const float w = used ? exp2f(m[i] - M) : 0.f;
+            l = fmaf(w, used ? ls[i] : 0.f, l);
 #pragma unroll
-            for (int j = 0; j < C; ++j) o[j] = fmaf(w, os[i][j], o[j]);
+            for (int j = 0; j < C; ++j) o[j] = fmaf(w, used ? os[i][j] : 0.f, o[j]);
         }
     }
     if (lane == 0) state[wave][D] = M, state[wave][D + 1] = l;
@@ -695,47 +886,85 @@ __global__ __launch_bounds__(kShThreads) void shared_merge_kernel(sepkv_params p
 struct SharedShape {
     bool split_rows;  // bf16: what shared_body's waves share
     int nb;           // bf16: column blocks of a wave
+    int waves;        // bf16: per workgroup
     int chunks;       // of rows, all prefixes together, at most
     int n_prefix;     // slices per prefix
     int n_own;        // slices per own cache
     int record;       // floats of an own cache's record
 };
-SharedShape shared_shape(const sepkv_params &p, const sepkv_params &pp) {
-    SharedShape s;
-    const long gq = p.Hq / p.Hkv, all = p.S * gq, per_prefix = (all + pp.S - 1) / pp.S;
-    s.split_rows = per_prefix > 32;
-    s.nb = s.split_rows ? (per_prefix <= 64 ? 1 : per_prefix <= 128 ? 2 : 3) : (per_prefix <= 16 ? 1 : 2);
-    const long rows = p.dtype == SEPATTN_FP32 ? 64 : (s.split_rows ? 64 : 16) * s.nb;
-    s.chunks = (int)(pp.S == 1 ? (all + rows - 1) / rows : all / rows + (pp.S < p.S ? pp.S : p.S));
-    const long nb = (pp.c + kShBlock - 1) / kShBlock, groups = (long)p.Hkv * s.chunks, units = compute_units();
-    long ns = (units + groups - 1) / groups;
-    if (ns > nb / 4) ns = nb / 4;
-    s.n_prefix = (int)(ns < 1 ? 1 : ns > 64 ? 64 : ns);
+// Host estimate in microseconds, from the capacities (the device alone knows how much of them is in use).  `bytes_us`: what reading every cache once
+// takes.  A prefix is cut so finely that a workgroup's walk through its slice, at `step` per 32 keys while the memory is busy, ends
+// well before that, and at least so finely that half of the places that the chip has for workgroups are taken; finer, and a slice more costs a
+// record per row, written and read again.
+SharedShape shared_shape(const sepkv_params &p, const sepkv_params &pp, bool rope) {
+    SharedShape s = {};
+    const long gq = p.Hq / p.Hkv, all = p.S * gq, per_prefix = (all + pp.S - 1) / pp.S, units = compute_units();
+    const long nb = (pp.c + kShBlock - 1) / kShBlock, own_nb = (p.c + kShBlock - 1) / kShBlock;
+    auto chunks_of = [&](long rows) { return pp.S == 1 ? (all + rows - 1) / rows : all / rows + (pp.S < p.S ? pp.S : p.S); };
+    s.waves = 4;
     if (p.dtype == SEPATTN_FP32) {
+        s.chunks = (int)chunks_of(64);
+        s.n_prefix = (int)std::clamp(2 * units / ((long)p.Hkv * s.chunks), 1L, std::min(nb, 64L));
         s.n_own = decode_record_slices(p);
         s.record = p.d + 2;
-    } else {
-        const long own_groups = (long)p.S * p.Hkv * ((gq + 15) / 16), own_nb = (p.c + kShBlock - 1) / kShBlock;
-        long no = units / own_groups;
-        if (no > own_nb / 4) no = own_nb / 4;
-        s.n_own = (int)(no < 1 ? 1 : no > 64 ? 64 : no);
-        s.record = p.d + 4;
+        return s;
     }
+    s.record = p.d + 4;
+    const long slots = (p.d == 64 ? 3 : 2) * units, own_groups = (long)p.S * p.Hkv * ((gq + 15) / 16);
+    const double own_rows = (double)p.S * p.c, prefix_rows = (double)pp.S * pp.c, bytes_us = 4.0 * p.d * p.Hkv * (own_rows + prefix_rows) / 5.3e6;
+    const double most_us = std::max(5.0, bytes_us * (0.4 + 0.5 * prefix_rows / (own_rows + prefix_rows)));
+    auto cut = [&](double step) {
+        const long groups = (long)p.Hkv * s.chunks, finest = std::clamp(nb / (nb > 64 ? 8 : 4), 1L, 64L), room = (slots - own_groups) / groups;
+        long ns = std::max((long)std::ceil(nb * step * (p.d == 64 ? 0.6 : 1.0) / most_us), (slots / 2 - own_groups) / groups);
+        // no second round of workgroups for a few slices
+        if (ns > room && room * 10 >= ns * 6) ns = room;
+        else if (ns > slots / groups && slots / groups * 10 >= ns * 7) ns = slots / groups;
+        return (int)std::clamp(ns, 1L, finest);
+    };
+    if (per_prefix <= 32) {
+        s.nb = per_prefix <= 16 ? 1 : 2;
+        s.chunks = (int)chunks_of(16 * s.nb);
+        s.n_prefix = cut(s.nb == 1 ? 0.35 : 0.45);
+    } else {
+        s.split_rows = true;
+        static const double step[2][3] = {{0.75, 0.85, 1.05}, {0.95, 1.1, 0.}};
+        s.nb = per_prefix <= 64 ? 1 : per_prefix <= 128 ? 2 : 3;
+        // three column blocks where they waste no more rows than two (turned queries at d = 128 have no registers for them)
+        if (s.nb == 3 && ((rope && p.d == 128) || (per_prefix + 191) / 192 * 3 > (per_prefix + 127) / 128 * 2)) s.nb = 2;
+        for (;; --s.nb) {  // fewer rows per workgroup, and more workgroups, where a slice would be a few steps
+            s.chunks = (int)chunks_of(64 * s.nb);
+            s.n_prefix = cut(step[rope && p.d == 128][s.nb - 1]);
+            if (s.nb == 1 || nb / s.n_prefix >= 16) break;
+        }
+        if (p.d == 128 && !rope && s.nb > 1 && s.n_prefix >= 24) {
+            s.waves = 8;
+            s.n_prefix = (s.n_prefix * 7 + 5) / 10;
+        }
+    }
+    const long no = (slots / 2) / own_groups;
+    s.n_own = (int)std::clamp(no, 1L, std::clamp(own_nb / 4, 1L, 64L));
     return s;
 }
 size_t prefix_record_bytes(const sepkv_params &p, const SharedShape &s) {
     return align_up((size_t)p.S * p.Hq * s.n_prefix * (p.d + 4) * sizeof(float), 256);
 }
+size_t own_record_bytes(const sepkv_params &p, const SharedShape &s) {
+    return align_up((size_t)p.S * p.Hq * s.n_own * s.record * sizeof(float), 256);
+}
 
 }  // namespace
 
 size_t decode_shared_workspace(const sepkv_params &p, const sepkv_params &pp) {
-    const SharedShape s = shared_shape(p, pp);
-    return prefix_record_bytes(p, s) + align_up((size_t)p.S * p.Hq * s.n_own * s.record * sizeof(float), 256);
+    size_t most = 0;
+    for (const bool rope : {false, true}) {  // one size for calls with and without positions
+        const SharedShape s = shared_shape(p, pp, rope);
+        most = std::max(most, prefix_record_bytes(p, s) + own_record_bytes(p, s));
+    }
+    return most;
 }
 
 int launch_decode_shared(const SharedDecode &x, hipStream_t st) {
-    const SharedShape s = shared_shape(x.p, x.pp);
+    const SharedShape s = shared_shape(x.p, x.pp, x.rope != nullptr);
     float *const own_part = x.part + prefix_record_bytes(x.p, s) / sizeof(float);
     const int gq = x.p.Hq / x.p.Hkv;
     const PrefixArgs a = {x.p, x.pp, gq, s.n_prefix, x.q, x.Kp, x.Vp, x.sizes, x.prefix_sizes, x.group_start, x.group_seq,
@@ -757,17 +986,28 @@ int launch_decode_shared(const SharedDecode &x, hipStream_t st) {
         if (n > 0x7FFFFFFFL) return SEPATTN_ERR_SHAPE;
         const SharedArgs all = {a, x.Kc, x.Vc, own_part, (int)n_prefix_groups, s.chunks, s.n_own, head_chunks};
         ProfScope prof(SEPATTN_K_DECODE_SPLIT, st);
-        auto go = [&](auto D_, auto NB_, auto ROWS_) {
-            constexpr int D = decltype(D_)::value, NB = decltype(NB_)::value;
-            constexpr bool ROWS = decltype(ROWS_)::value != 0;
-            if (x.rope) hipLaunchKernelGGL((shared_decode_kernel<D, NB, ROWS, true>), dim3((unsigned)n), block, 0, st, all);
-            else hipLaunchKernelGGL((shared_decode_kernel<D, NB, ROWS, false>), dim3((unsigned)n), block, 0, st, all);
+        auto go = [&](auto D_, auto NW_, auto NB_, auto ROWS_, auto ROPE_) {
+            constexpr int D = decltype(D_)::value, NW = decltype(NW_)::value, NB = decltype(NB_)::value;
+            constexpr bool ROWS = decltype(ROWS_)::value != 0, ROPE = decltype(ROPE_)::value != 0;
+            hipLaunchKernelGGL((shared_decode_kernel<D, NW, NB, ROWS, ROPE>), dim3((unsigned)n), dim3(64 * NW), 0, st, all);
         };
-        auto shape = [&](auto D_) {
-            if (s.split_rows) s.nb == 1 ? go(D_, IntC<1>{}, IntC<1>{}) : s.nb == 2 ? go(D_, IntC<2>{}, IntC<1>{}) : go(D_, IntC<3>{}, IntC<1>{});
-            else s.nb == 1 ? go(D_, IntC<1>{}, IntC<0>{}) : go(D_, IntC<2>{}, IntC<0>{});
+        using N1 = IntC<1>;
+        using N2 = IntC<2>;
+        using N3 = IntC<3>;
+        using W4 = IntC<4>;
+        using W8 = IntC<8>;
+        auto shape = [&](auto D_, auto ROPE_) {
+            constexpr int D = decltype(D_)::value;
+            constexpr bool ROPE = decltype(ROPE_)::value != 0;
+            if (!s.split_rows) return s.nb == 1 ? go(D_, W4{}, N1{}, IntC<0>{}, ROPE_) : go(D_, W4{}, N2{}, IntC<0>{}, ROPE_);
+            if constexpr (D == 128 && !ROPE)
+                if (s.waves == 8) return s.nb == 2 ? go(D_, W8{}, N2{}, N1{}, ROPE_) : go(D_, W8{}, N3{}, N1{}, ROPE_);
+            if constexpr (D == 64 || !ROPE)
+                if (s.nb == 3) return go(D_, W4{}, N3{}, N1{}, ROPE_);
+            s.nb == 1 ? go(D_, W4{}, N1{}, N1{}, ROPE_) : go(D_, W4{}, N2{}, N1{}, ROPE_);
         };
-        x.p.d == 64 ? shape(IntC<64>{}) : shape(IntC<128>{});
+        if (x.p.d == 64) x.rope ? shape(IntC<64>{}, N1{}) : shape(IntC<64>{}, IntC<0>{});
+        else x.rope ? shape(IntC<128>{}, N1{}) : shape(IntC<128>{}, IntC<0>{});
         const int rc = launch_status();
         if (rc != SEPATTN_OK) return rc;
     }
@@ -775,8 +1015,8 @@ int launch_decode_shared(const SharedDecode &x, hipStream_t st) {
     auto go = [&](auto T_, auto D_) {
         using T = decltype(T_);
         constexpr int D = decltype(D_)::value;
-        hipLaunchKernelGGL((shared_merge_kernel<T, D, sizeof(T) == 2 ? D + 4 : D + 2>), dim3(x.p.S * x.p.Hq), block, 0, st, x.p, x.pp, s.n_prefix, s.n_own,
-                           x.sizes, x.prefix_sizes, x.prefix_of, x.part, own_part, static_cast<T *>(x.out), x.lse);
+        hipLaunchKernelGGL((shared_merge_kernel<T, D, sizeof(T) == 2 ? D + 4 : D + 2>), dim3(x.p.Hq, x.p.S), block, 0, st, x.p, x.pp.S, s.n_prefix, s.n_own,
+                           x.prefix_of, x.part, own_part, static_cast<T *>(x.out), x.lse);
     };
     if (x.p.dtype == SEPATTN_BF16) x.p.d == 64 ? go(uint16_t{}, IntC<64>{}) : go(uint16_t{}, IntC<128>{});
     else x.p.d == 64 ? go(float{}, IntC<64>{}) : go(float{}, IntC<128>{});

@@ -77,16 +77,18 @@ __global__ __launch_bounds__(kAppendThreads) void cache_append_rope_kernel(
     T *__restrict__ Vc, uint8_t *__restrict__ win_is_sep, int32_t *__restrict__ sizes) {
     const long sq = blockIdx.x;
     const int group = threadIdx.x & ((1 << log_groups) - 1), row = threadIdx.x >> log_groups, rows = kAppendThreads >> log_groups;
-    const bool turned = group * Angles<T>::E < n_pairs;
+    constexpr int E = Angles<T, LAYOUT>::E;
+    const int half = p.d / 2;
+    const bool turned = has_turned<LAYOUT, E>(group, n_pairs);
     const int t = positions[sq];
-    Angles<T> w;
+    Angles<T, LAYOUT> w;
     if (blockIdx.y == 1) {  // the query
-        if (turned) w.form(freqs, n_pairs, group, t, 1.f);
+        if (turned) w.form(freqs, n_pairs, half, group, t, 1.f);
         for (int h = row; h < p.Hq; h += rows) {
-            Pairs<T> x;
-            x.template load<LAYOUT>(q + (sq * p.Hq + h) * p.d, group, n_pairs);
-            if (turned) x.template turn<LAYOUT>(w, group, n_pairs);
-            x.template store<LAYOUT>(q_out + (sq * p.Hq + h) * p.d, group, n_pairs);
+            Pairs<T, LAYOUT> x;
+            x.load(q + (sq * p.Hq + h) * p.d, group, n_pairs, half);
+            if (turned) x.turn(w, group, n_pairs, half);
+            x.store(q_out + (sq * p.Hq + h) * p.d, group, n_pairs, half);
         }
         return;
     }
@@ -98,14 +100,14 @@ __global__ __launch_bounds__(kAppendThreads) void cache_append_rope_kernel(
     if (cm.n_init < p.a) slot = cm.n_init;
     else if (u < cm.wcap) slot = p.a + p.s + win_index(cm, u);
     else return;  // window region full (uniform over the workgroup)
-    if (turned) w.form(freqs, n_pairs, group, t, 1.f);
+    if (turned) w.form(freqs, n_pairs, half, group, t, 1.f);
     for (int i = row; i < 2 * p.Hkv; i += rows) {
         const bool value = i >= p.Hkv;
         const int h = value ? i - p.Hkv : i;
-        Pairs<T> x;
-        x.template load<LAYOUT>((value ? v_new : k_new) + (sq * p.Hkv + h) * p.d, group, n_pairs);
-        if (turned && !value) x.template turn<LAYOUT>(w, group, n_pairs);
-        x.template store<LAYOUT>((value ? Vc : Kc) + ((sq * p.Hkv + h) * p.c + slot) * p.d, group, n_pairs);
+        Pairs<T, LAYOUT> x;
+        x.load((value ? v_new : k_new) + (sq * p.Hkv + h) * p.d, group, n_pairs, half);
+        if (turned && !value) x.turn(w, group, n_pairs, half);
+        x.store((value ? Vc : Kc) + ((sq * p.Hkv + h) * p.c + slot) * p.d, group, n_pairs, half);
     }
     if (threadIdx.x == 0) count_appended(p, cm, sq, is_sep_new[sq], win_is_sep, sz);
 }

@@ -28,7 +28,7 @@ struct RopeTensors {
 
 // Threads of a workgroup: group of pairs (fastest), `tokens` tokens, head slots; grid (token tiles, head chunks, B).  A thread walks through the
 // heads  slot, slot + slots, ...  of its chunk.
-template <typename T, PairLayout LAYOUT>
+template <typename T, PairLayout LAYOUT, bool STREAM>
 __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeTensors x, int L, int n_pairs, int log_groups, int log_tokens, int chunk,
                                                              float sign, const double *__restrict__ freqs,
                                                              const int32_t *__restrict__ positions, const int32_t *__restrict__ doc_start) {
@@ -40,9 +40,11 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeTensors x, int L
     const long at = (long)b * L + l;
     const int t = positions ? positions[at] : l - (doc_start ? doc_start[at] : 0);
     const int h0 = blockIdx.y * chunk, all = x.heads[0] + x.heads[1] + x.heads[2], h1 = min(h0 + chunk, all);
-    const bool turned = group * Angles<T>::E < n_pairs;
-    Angles<T> w;
-    if (turned && h0 < x.heads[0] + x.heads[1]) w.form(freqs, n_pairs, group, t, sign);
+    constexpr int E = Angles<T, LAYOUT>::E;
+    const int half = E << log_groups;
+    const bool turned = has_turned<LAYOUT, E>(group, n_pairs);
+    Angles<T, LAYOUT> w;
+    if (turned && h0 < x.heads[0] + x.heads[1]) w.form(freqs, n_pairs, half, group, t, sign);
     int before = 0;
 #pragma unroll
     for (int which = 0; which < 3; ++which) {  // q, k, v
@@ -52,15 +54,15 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeTensors x, int L
         const int lo = max(h0 - before, 0), hi = min(h1 - before, x.heads[which]);
         constexpr int N = 4;
         for (int h = lo + slot; h < hi; h += N * slots) {
-            Pairs<T> row[N];
+            Pairs<T, LAYOUT> row[N];
 #pragma unroll
             for (int n = 0; n < N; ++n)
-                if (h + n * slots < hi) row[n].template load<LAYOUT>(src + (h + n * slots) * from.h, group, n_pairs);
+                if (h + n * slots < hi) row[n].template load<STREAM>(src + (h + n * slots) * from.h, group, n_pairs, half);
 #pragma unroll
             for (int n = 0; n < N; ++n)
                 if (h + n * slots < hi) {
-                    if (which < 2 && turned) row[n].template turn<LAYOUT>(w, group, n_pairs);
-                    row[n].template store<LAYOUT>(dst + (h + n * slots) * to.h, group, n_pairs);
+                    if (which < 2 && turned) row[n].turn(w, group, n_pairs, half);
+                    row[n].store(dst + (h + n * slots) * to.h, group, n_pairs, half);
                 }
         }
         before += x.heads[which];
@@ -73,29 +75,29 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeTensors x, int L
 template <typename T, int D>
 __global__ __launch_bounds__(kRopeThreads) void rope_cache_kernel(sepkv_params p, int chunk, const int32_t *__restrict__ sizes,
                                                                    const float *__restrict__ rope, int n_pos, const T *Kc, T *K_out) {
-    constexpr int GROUPS = D / (2 * Angles<T>::E), SLOTS = kRopeThreads / GROUPS, E = Angles<T>::E;
+    constexpr int GROUPS = D / (2 * Angles<T, kHalves>::E), SLOTS = kRopeThreads / GROUPS, E = Angles<T, kHalves>::E;
     const int group = threadIdx.x % GROUPS, slot = blockIdx.x * SLOTS + threadIdx.x / GROUPS;
     const long cache = blockIdx.z;
     if (slot >= p.c) return;
     const int e = rank_of_slot(cache_map(p, sizes + SEPKV_SIZES_COLS * cache), slot);
     if (e < 0) return;
-    Angles<T> w;
+    Angles<T, kHalves> w;
     const float *row = rope + (long)min(e, n_pos - 1) * D + group * E;
 #pragma unroll
     for (int i = 0; i < E; ++i) w.cs[i] = row[i], w.sn[i] = row[D / 2 + i];
     const int h0 = blockIdx.y * chunk, h1 = min(h0 + chunk, p.Hkv);
     constexpr int N = 4;
     for (int h = h0; h < h1; h += N) {
-        Pairs<T> x[N];
+        Pairs<T, kHalves> x[N];
         const long at = ((cache * p.Hkv + h) * p.c + slot) * D, pitch = (long)p.c * D;
 #pragma unroll
         for (int n = 0; n < N; ++n)
-            if (h + n < h1) x[n].template load<kHalves>(Kc + at + n * pitch, group, D / 2);
+            if (h + n < h1) x[n].load(Kc + at + n * pitch, group, D / 2, D / 2);
 #pragma unroll
         for (int n = 0; n < N; ++n)
             if (h + n < h1) {
-                x[n].template turn<kHalves>(w, group, D / 2);
-                x[n].template store<kHalves>(K_out + at + n * pitch, group, D / 2);
+                x[n].turn(w, group, D / 2, D / 2);
+                x[n].store(K_out + at + n * pitch, group, D / 2, D / 2);
             }
     }
 }
@@ -147,8 +149,15 @@ int launch_rope(const sepattn_rope_params &p, const double *freqs, const int32_t
     while ((1 << log_groups) < groups) ++log_groups;
     while ((1 << log_tokens) < p.L && (1 << (log_groups + log_tokens)) < kRopeThreads) ++log_tokens;
     const int tiles = (p.L + (1 << log_tokens) - 1) >> log_tokens, slots = kRopeThreads >> (log_groups + log_tokens);
-    // as many chunks of heads as fill the chip with eight workgroups per compute unit, of whole rounds of the head slots
-    const long want = (8L * compute_units() + (long)tiles * p.B - 1) / ((long)tiles * p.B);
+    // More than half of the last cache level (256 MB) passes through: the rows are read with the non-temporal hint, if an instruction covers whole
+    // cache lines of them (rows of 256 bytes and more; rows of 128 lose 2 us of 31), so that the results find room there (microseconds without
+    // / with it, 32/8 heads, d = 128: 8192 tokens 45 / 36, backward 43 / 35, fp32 42 / 34; 3 x 700 tokens 10.4 / 12.0).  Chunks of heads: as many as make
+    // this many workgroups per compute unit (4 / 8 / 32: with the hint 36.2 / 37.0 / 39.2; 3 x 700 tokens 10.4 / 10.7 / 12.3; 8 x 12/12 heads, d = 64,
+    // 2048 tokens 31.1 / 31.6 / 28.3).
+    const long row_bytes = p.d * (p.dtype == SEPATTN_BF16 ? 2 : 4);
+    const bool large = 2 * row_bytes * p.B * p.L * heads > 128L << 20, stream = large && row_bytes >= 256;
+    const long per_unit = stream ? 4 : large ? 32 : 8;
+    const long want = (per_unit * compute_units() + (long)tiles * p.B - 1) / ((long)tiles * p.B);
     int chunk = (int)((heads + want - 1) / want);
     chunk = (chunk + slots - 1) / slots * slots;
     const dim3 grid(tiles, (heads + chunk - 1) / chunk, p.B);
@@ -156,12 +165,12 @@ int launch_rope(const sepattn_rope_params &p, const double *freqs, const int32_t
     auto go = [&](auto T_) {
         using T = decltype(T_);
         const int layout = pair_layout<T>(p.rotary_dim, p.interleaved);
-#define ROPE(LAYOUT)                                                                                                         \
-    hipLaunchKernelGGL((rope_kernel<T, LAYOUT>), grid, dim3(kRopeThreads), 0, st, x, p.L, p.rotary_dim / 2, log_groups, log_tokens, \
+#define ROPE(LAYOUT, STREAM)                                                                                                 \
+    hipLaunchKernelGGL((rope_kernel<T, LAYOUT, STREAM>), grid, dim3(kRopeThreads), 0, st, x, p.L, p.rotary_dim / 2, log_groups, log_tokens, \
                        chunk, sign, freqs, positions, doc_start)
-        if (layout == kNeighbours) ROPE(kNeighbours);
-        else if (layout == kHalves) ROPE(kHalves);
-        else ROPE(kHalvesOdd);
+        if (layout == kNeighbours) { if (stream) ROPE(kNeighbours, true); else ROPE(kNeighbours, false); }
+        else if (layout == kHalves) { if (stream) ROPE(kHalves, true); else ROPE(kHalves, false); }
+        else ROPE(kHalvesOdd, false);
 #undef ROPE
     };
     if (p.dtype == SEPATTN_BF16) go(uint16_t{});

@@ -1,9 +1,8 @@
 // Pieces shared by the kernels that turn pairs of dimensions by positions (rope.hip, cache_append.hip).
 //
-// A row of d values is cut into groups of 16 bytes worth of pairs: group j holds pairs E j .. E j + E - 1 (E = 8 in bf16, 4 in
-// fp32), every group is one lane's, and a lane reads both members of its pairs before it writes any, so a turn may be in place.
-// Pair p of the first rotary_dim / 2 is (p, p + rotary_dim/2), or (2p, 2p+1) where interleaved; the others are the values
-// 2p, 2p+1, which are copied bit for bit.
+// A row of d values is cut into groups of two pieces of 16 bytes, E pairs (E = 8 in bf16, 4 in fp32); every group is one lane's, and a lane
+// reads both members of its pairs before it writes any, so a turn may be in place.  Pair p of the first rotary_dim / 2 is
+// (p, p + rotary_dim/2), or (2p, 2p+1) where interleaved; the others are the values 2p, 2p+1, which are copied bit for bit.
 #pragma once
 
 #include "common.h"
@@ -11,8 +10,8 @@
 namespace sepattn {
 
 enum PairLayout {
-    kNeighbours,  // (2p, 2p+1): a group is 32 contiguous bytes
-    kHalves,      // (p, p + rotary_dim/2), rotary_dim/2 a multiple of E: a group is two runs of 16 bytes
+    kNeighbours,  // (2p, 2p+1): a lane's pieces are the same place in the two halves of the row, so that a load instruction covers half a row
+    kHalves,      // (p, p + rotary_dim/2), rotary_dim/2 a multiple of E: a piece of first members, the piece of their partners
     kHalvesOdd,   // the same with any even rotary_dim: value by value
 };
 template <typename T>
@@ -38,97 +37,101 @@ __device__ inline void angle_of(int t, double f, float &cs, float &sn) {
     sincospif((float)(turns + turns), &sn, &cs);
 }
 
+// Which pair element e of a group is; `half` = d / 2
+template <PairLayout LAYOUT, int E>
+__device__ inline int pair_of(int group, int e, int half) {
+    if (LAYOUT == kNeighbours) return (e < E / 2 ? group * (E / 2) : half / 2 + group * (E / 2) - E / 2) + e;
+    return group * E + e;
+}
+// whether a group has a pair that is turned
+template <PairLayout LAYOUT, int E>
+__device__ inline bool has_turned(int group, int n_pairs) { return pair_of<LAYOUT, E>(group, 0, 0) < n_pairs; }
+
 // cos / sin of the E pairs of a group at one position
-template <typename T>
+template <typename T, PairLayout LAYOUT>
 struct Angles {
     static constexpr int E = 16 / (int)sizeof(T);
     float cs[E], sn[E];
     // sign -1: the opposite angles.  Pairs from n_pairs on are not looked at later.
-    __device__ void form(const double *__restrict__ freqs, int n_pairs, int group, int t, float sign) {
+    __device__ void form(const double *__restrict__ freqs, int n_pairs, int half, int group, int t, float sign) {
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            angle_of(t, freqs[min(group * E + e, n_pairs - 1)], cs[e], sn[e]);
+            angle_of(t, freqs[min(pair_of<LAYOUT, E>(group, e, half), n_pairs - 1)], cs[e], sn[e]);
             sn[e] *= sign;
         }
     }
 };
 
-// the 2 E values of a group: x[e], y[e] are pair e's
-template <typename T>
+// the 2 E values of a group
+template <typename T, PairLayout LAYOUT>
 struct Pairs {
     static constexpr int E = 16 / (int)sizeof(T);
     typedef T Run __attribute__((ext_vector_type(16 / sizeof(T))));
-    Run a, b;  // as they lie: two runs of 16 bytes (kHalves: the first and the second members; else neighbouring values)
+    Run a, b;  // kNeighbours: pieces of whole pairs; else first and second members
 
-    template <PairLayout LAYOUT>
-    __device__ static int first(int group, int n_pairs, int e) {  // place of pair e's first member
-        const int p = group * E + e;
-        return LAYOUT != kNeighbours && p < n_pairs ? p : 2 * p;
+    static __device__ int second_piece(int group, int n_pairs, int half, int &first) {
+        if (LAYOUT == kNeighbours) {
+            first = group * E;
+            return first + half;
+        }
+        const bool turned = group * E < n_pairs;
+        first = turned ? group * E : 2 * group * E;
+        return first + (turned ? n_pairs : E);
     }
-    template <PairLayout LAYOUT>
-    __device__ void load(const T *row, int group, int n_pairs) {
+    // STREAM: the non-temporal hint, for rows whose pieces one instruction reads by whole cache lines
+    template <bool STREAM = false>
+    __device__ void load(const T *row, int group, int n_pairs, int half) {
         if constexpr (LAYOUT == kHalvesOdd) {
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                const int at = first<LAYOUT>(group, n_pairs, e);
-                a[e] = row[at];
-                b[e] = row[group * E + e < n_pairs ? at + n_pairs : at + 1];
+                const int p = group * E + e;
+                a[e] = row[p < n_pairs ? p : 2 * p];
+                b[e] = row[p < n_pairs ? p + n_pairs : 2 * p + 1];
             }
         } else {
-            const bool halves = LAYOUT == kHalves && group * E < n_pairs;
-            const T *p = row + (halves ? group * E : 2 * group * E);
-            a = *reinterpret_cast<const Run *>(p);
-            b = *reinterpret_cast<const Run *>(p + (halves ? n_pairs : E));
+            int first;
+            const int second = second_piece(group, n_pairs, half, first);
+            const Run *pa = reinterpret_cast<const Run *>(row + first), *pb = reinterpret_cast<const Run *>(row + second);
+            a = STREAM ? __builtin_nontemporal_load(pa) : *pa;
+            b = STREAM ? __builtin_nontemporal_load(pb) : *pb;
         }
     }
-    template <PairLayout LAYOUT>
-    __device__ void store(T *row, int group, int n_pairs) const {
+    __device__ void store(T *row, int group, int n_pairs, int half) const {
         if constexpr (LAYOUT == kHalvesOdd) {
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                const int at = first<LAYOUT>(group, n_pairs, e);
-                row[at] = a[e];
-                row[group * E + e < n_pairs ? at + n_pairs : at + 1] = b[e];
+                const int p = group * E + e;
+                row[p < n_pairs ? p : 2 * p] = a[e];
+                row[p < n_pairs ? p + n_pairs : 2 * p + 1] = b[e];
             }
         } else {
-            const bool halves = LAYOUT == kHalves && group * E < n_pairs;
-            T *p = row + (halves ? group * E : 2 * group * E);
-            *reinterpret_cast<Run *>(p) = a;
-            *reinterpret_cast<Run *>(p + (halves ? n_pairs : E)) = b;
+            int first;
+            const int second = second_piece(group, n_pairs, half, first);
+            *reinterpret_cast<Run *>(row + first) = a;
+            *reinterpret_cast<Run *>(row + second) = b;
         }
     }
-    template <PairLayout LAYOUT>
-    __device__ void turn(const Angles<T> &w, int group, int n_pairs) {
-        Run x = a, y = b;
-        if constexpr (LAYOUT == kNeighbours) {
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                x[e] = 2 * e < E ? a[(2 * e) % E] : b[(2 * e) % E];
-                y[e] = 2 * e < E ? a[(2 * e + 1) % E] : b[(2 * e + 1) % E];
+    __device__ void turn(const Angles<T, LAYOUT> &w, int group, int n_pairs, int half) {
+        auto one = [&](int e, T &x, T &y) {
+            const float u = widened(x), v = widened(y);
+            // (a select, not an angle of 0: 0 times an infinity next to it would be NaN)
+            if (pair_of<LAYOUT, E>(group, e, half) < n_pairs) {
+                x = narrowed<T>(fmaf(u, w.cs[e], -(v * w.sn[e])));
+                y = narrowed<T>(fmaf(v, w.cs[e], u * w.sn[e]));
             }
-        }
+        };
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const float u = widened((T)x[e]), v = widened((T)y[e]);
-            // (a select, not an angle of 0: 0 times an infinity next to it would be NaN)
-            if (group * E + e < n_pairs) {
-                x[e] = narrowed<T>(fmaf(u, w.cs[e], -(v * w.sn[e])));
-                y[e] = narrowed<T>(fmaf(v, w.cs[e], u * w.sn[e]));
+            if constexpr (LAYOUT == kNeighbours) {
+                Run &r = e < E / 2 ? a : b;
+                T x = r[2 * e % E], y = r[2 * e % E + 1];
+                one(e, x, y);
+                r[2 * e % E] = x, r[2 * e % E + 1] = y;
+            } else {
+                T x = a[e], y = b[e];
+                one(e, x, y);
+                a[e] = x, b[e] = y;
             }
-        }
-        if constexpr (LAYOUT == kNeighbours) {
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                if (2 * e < E) {
-                    a[(2 * e) % E] = x[e];
-                    a[(2 * e + 1) % E] = y[e];
-                } else {
-                    b[(2 * e) % E] = x[e];
-                    b[(2 * e + 1) % E] = y[e];
-                }
-            }
-        } else {
-            a = x, b = y;
         }
     }
 };

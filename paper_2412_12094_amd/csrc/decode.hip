@@ -292,10 +292,11 @@ int pick_nsplit(const sepkv_params &p) {
 }
 
 template <typename T, int D, bool ROPE>
-int launch_split_t(const sepkv_params &p, int nsplit, const T *q, const T *Kc, const T *Vc, const int32_t *sizes, const float *rope,
-                   int n_pos, float *part, hipStream_t st) {
-    int G = p.Hq / p.Hkv, GT = pick_gt(G);
+int launch_decode_t(const sepkv_params &p, const T *q, const T *Kc, const T *Vc, const int32_t *sizes,
+                    const float *rope, int n_pos, T *out, float *lse, float *part, hipStream_t st) {
+    int G = p.Hq / p.Hkv, GT = pick_gt(G), nsplit = pick_nsplit(p);
     dim3 grid(nsplit, p.S * p.Hkv * (G / GT)), block(kDecodeThreads);
+    {
     ProfScope prof(SEPATTN_K_DECODE_SPLIT, st);
     if (GT == 4)
         hipLaunchKernelGGL((decode_split_kernel<T, D, 4, ROPE>), grid, block, 0, st, p, nsplit, q, Kc, Vc, sizes, rope, n_pos, part);
@@ -303,39 +304,14 @@ int launch_split_t(const sepkv_params &p, int nsplit, const T *q, const T *Kc, c
         hipLaunchKernelGGL((decode_split_kernel<T, D, 2, ROPE>), grid, block, 0, st, p, nsplit, q, Kc, Vc, sizes, rope, n_pos, part);
     else
         hipLaunchKernelGGL((decode_split_kernel<T, D, 1, ROPE>), grid, block, 0, st, p, nsplit, q, Kc, Vc, sizes, rope, n_pos, part);
-    return launch_status();
-}
-
-template <typename T, int D, bool ROPE>
-int launch_decode_t(const sepkv_params &p, const T *q, const T *Kc, const T *Vc, const int32_t *sizes,
-                    const float *rope, int n_pos, T *out, float *lse, float *part, hipStream_t st) {
-    const int nsplit = pick_nsplit(p);
-    const int rc = launch_split_t<T, D, ROPE>(p, nsplit, q, Kc, Vc, sizes, rope, n_pos, part, st);
-    if (rc != SEPATTN_OK) return rc;
+    }
+    if (hipGetLastError() != hipSuccess) return SEPATTN_ERR_HIP;
     ProfScope prof(SEPATTN_K_DECODE_MERGE, st);
     hipLaunchKernelGGL((decode_merge_kernel<T, D>), dim3(p.S * p.Hq), dim3(D), 0, st, nsplit, part, out, lse);
     return launch_status();
 }
 
 }  // namespace
-
-int decode_record_slices(const sepkv_params &p) { return pick_nsplit(p); }
-
-template <typename T>
-int launch_records_t(const sepkv_params &p, int nsplit, const void *q, const void *Kc, const void *Vc, const int32_t *sizes,
-                     const float *rope, int n_pos, float *part, hipStream_t st) {
-    const T *q_ = (const T *)q, *K_ = (const T *)Kc, *V_ = (const T *)Vc;
-    if (p.d == 64 && rope) return launch_split_t<T, 64, true>(p, nsplit, q_, K_, V_, sizes, rope, n_pos, part, st);
-    if (p.d == 64) return launch_split_t<T, 64, false>(p, nsplit, q_, K_, V_, sizes, rope, n_pos, part, st);
-    if (rope) return launch_split_t<T, 128, true>(p, nsplit, q_, K_, V_, sizes, rope, n_pos, part, st);
-    return launch_split_t<T, 128, false>(p, nsplit, q_, K_, V_, sizes, rope, n_pos, part, st);
-}
-
-int launch_decode_records(const sepkv_params &p, int nsplit, const void *q, const void *Kc, const void *Vc, const int32_t *sizes,
-                          const float *rope, int n_pos, float *part, hipStream_t st) {
-    if (p.dtype == SEPATTN_BF16) return launch_records_t<uint16_t>(p, nsplit, q, Kc, Vc, sizes, rope, n_pos, part, st);
-    return launch_records_t<float>(p, nsplit, q, Kc, Vc, sizes, rope, n_pos, part, st);
-}
 
 size_t decode_workspace(const sepkv_params &p) {
     int nsplit;

@@ -59,12 +59,6 @@ __device__ inline uint16_t decode_f32_to_bf16(float f) {
     return (uint16_t)(u >> 16);
 }
 
-// The vector-ALU kernel of decode.hip without the sum over the slices: records of d + 2 floats (max, sum, unnormalised outputs),
-// [sequence][head][slice]
-int decode_record_slices(const sepkv_params &p);
-int launch_decode_records(const sepkv_params &p, int nsplit, const void *q, const void *Kc, const void *Vc, const int32_t *sizes,
-                          const float *rope, int n_pos, float *part, hipStream_t st);
-
 bool decode_mfma_applicable(const sepkv_params &p);
 int decode_mfma_nsplit(const sepkv_params &p);
 // rope: table of cos / sin by position [n_pos][2][d/2], or nullptr for keys that carry their encoding

@@ -94,6 +94,106 @@ __device__ inline int query_position(const PrefixArgs &x, int seq, int prefix_en
     return min(max(prefix_entries + entries_of(cache_map(x.p, x.sizes + SEPKV_SIZES_COLS * seq)) - 1, 0), x.n_pos - 1);
 }
 
+// What a workgroup has to do.  Workgroups 0 .. n_prefix_groups - 1: (KV head, chunk of rows, slice of the prefix); the others: (KV head, sequence and
+// chunk of 16 heads, slice of its own cache).  KV heads run fastest, so that with eight of them the workgroups that read the same rows are on
+// one XCD.
+struct SharedArgs {
+    PrefixArgs x;
+    const void *Kc, *Vc;
+    float *own_part;
+    int n_prefix_groups, chunks, n_own, head_chunks;
+};
+template <typename T>
+struct SliceWork {
+    CacheMap cm;
+    int entries, e0, e1;  // of the cache, of the slice
+    int kv, split;
+    Chunk c;              // a prefix's
+    int seq, head0;       // an own cache's: first head of the chunk, within the KV head's
+    const T *K, *V;
+};
+// One row of the product: its query, the query's position (turned queries), where the slice's record goes (nullptr for a column without a row)
+template <typename T>
+struct SliceRow {
+    const T *q;
+    int position;
+    float *record;
+};
+template <int D, bool ROPE, typename T>
+__device__ __forceinline__ SliceRow<T> prefix_row(const SharedArgs &a, const SliceWork<T> &w, int block, int col) {
+    const PrefixArgs &x = a.x;
+    const int r = w.c.row0 + block * 16 + col;
+    int seq, head;
+    row_of(x, w.c, r, seq, head);
+    const long row = (long)seq * x.p.Hq + w.kv * x.gq + head;
+    return {static_cast<const T *>(x.q) + row * D, ROPE ? query_position(x, seq, w.entries) : 0,
+            r < w.c.rows ? x.part + (row * x.nsplit + w.split) * kShRecord<D> : nullptr};
+}
+template <int D, typename T>
+__device__ __forceinline__ SliceRow<T> own_row(const SharedArgs &a, const SliceWork<T> &w, int col) {
+    const PrefixArgs &x = a.x;
+    const int head = w.head0 + col;
+    const long row = (long)w.seq * x.p.Hq + w.kv * x.gq + min(head, x.gq - 1);
+    return {static_cast<const T *>(x.q) + row * D, 0, head < x.gq ? a.own_part + (row * a.n_own + w.split) * kShRecord<D> : nullptr};
+}
+// false: nothing to do (a slice without an entry has been marked as such)
+template <int D, int ROWS, bool ROPE, typename T>
+__device__ __forceinline__ bool prefix_work(const SharedArgs &a, int id, SliceWork<T> &w) {
+    const PrefixArgs &x = a.x;
+    const int Hkv = x.p.Hkv, chunk = id / Hkv % a.chunks;
+    w.kv = id % Hkv, w.split = id / Hkv / a.chunks;
+    if (!find_chunk<ROWS>(x, chunk, w.c)) return false;
+    w.cm = uniform_map(x.pp, x.prefix_sizes, w.c.prefix);
+    w.entries = entries_of(w.cm);
+    if (!slice_of(w.entries, x.nsplit, w.split, w.e0, w.e1)) {
+        if (threadIdx.x < ROWS)
+            if (float *r = prefix_row<D, false>(a, w, threadIdx.x / 16, threadIdx.x % 16).record) mark_empty(r);
+        return false;
+    }
+    const long head0 = ((long)w.c.prefix * Hkv + w.kv) * (long)x.pp.c * D;
+    w.K = static_cast<const T *>(x.Kp) + head0, w.V = static_cast<const T *>(x.Vp) + head0;
+    return true;
+}
+template <int D, typename T>
+__device__ __forceinline__ bool own_work(const SharedArgs &a, int id, SliceWork<T> &w) {
+    const PrefixArgs &x = a.x;
+    const int Hkv = x.p.Hkv;
+    w.kv = id % Hkv, w.head0 = id / Hkv % a.head_chunks * 16, w.seq = id / Hkv / a.head_chunks % x.p.S, w.split = id / Hkv / a.head_chunks / x.p.S;
+    w.cm = uniform_map(x.p, x.sizes, w.seq);
+    w.entries = entries_of(w.cm);
+    if (!slice_of(w.entries, a.n_own, w.split, w.e0, w.e1)) {
+        if (threadIdx.x < 16)
+            if (float *r = own_row<D>(a, w, threadIdx.x).record) mark_empty(r);
+        return false;
+    }
+    const long head0 = ((long)w.seq * Hkv + w.kv) * (long)x.p.c * D;
+    w.K = static_cast<const T *>(a.Kc) + head0, w.V = static_cast<const T *>(a.Vc) + head0;
+    return true;
+}
+// The states of NW waves that had the same 16 rows, [wave][row][record] in LDS, added in wave order and written; two columns per thread.
+template <int D, int NW, typename Rows>
+__device__ __forceinline__ void add_wave_states(const float *states, const Rows &rows, int block) {
+    constexpr int REC = kShRecord<D>;
+    for (int item = threadIdx.x; item < 16 * (D / 2); item += 64 * NW) {
+        const int row = item / (D / 2), c2 = item % (D / 2);
+        float *const to = rows(block, row).record;
+        if (!to) continue;
+        float M = -INFINITY, lsum = 0.f, o0 = 0.f, o1 = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) M = fmaxf(M, states[(w * 16 + row) * REC]);
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const float *x = states + (w * 16 + row) * REC;
+            const float wgt = __builtin_amdgcn_exp2f(x[0] - M);  // M is finite: the slice has an entry
+            lsum = fmaf(wgt, x[1], lsum);
+            o0 = fmaf(wgt, x[4 + 2 * c2], o0);
+            o1 = fmaf(wgt, x[5 + 2 * c2], o1);
+        }
+        *reinterpret_cast<float2 *>(to + 4 + 2 * c2) = float2{o0, o1};
+        if (c2 == 0) *reinterpret_cast<float2 *>(to) = float2{M, lsum};
+    }
+}
+
 // ---- bf16 ------------------------------------------------------------------------------------------
 // One workgroup of eight waves: rows (queries that read one KV head) against a slice of one cache, in blocks of 32 keys.  Operands as in
 // decode_wide.hip (v_mfma_f32_16x16x32_bf16, the cache rows as A, 16 queries as the columns of B, score tile t's row 4g+i the block's row
@@ -171,14 +271,7 @@ __device__ inline void split_hi_lo(const f32x8 &x, bf16x8 &hi, bf16x8 &lo) {
     lo = __builtin_convertvector(x - __builtin_convertvector(hi, f32x8), bf16x8);
 }
 
-// What the body needs of its rows: column `col` of block nb.
-struct ShRow {
-    const uint16_t *q;  // its query
-    int position;       // LO: the query's
-    float *record;      // where the slice's record goes, nullptr for a column without a row
-};
-
-// rows: ShRow of (column block, column)
+// rows: SliceRow of (column block, column)
 template <int D, int NW, int NB, bool SPLIT_ROWS, bool KROPE, bool LO, typename Rows>
 __device__ __forceinline__ void shared_body(const CacheMap &cm, const uint16_t *__restrict__ Kh, const uint16_t *__restrict__ Vh, int e0, int e1,
                                             int last /* KROPE: position of the query within the cache */, const float *__restrict__ rope,
@@ -196,7 +289,7 @@ __device__ __forceinline__ void shared_body(const CacheMap &cm, const uint16_t *
     bf16x8 qhi[NB][KSTEPS], qlo[LO ? NB : 1][LO ? KSTEPS : 1];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-        const ShRow r = rows(SPLIT_ROWS ? rw * NB + nb : nb, col);
+        const SliceRow<uint16_t> r = rows(SPLIT_ROWS ? rw * NB + nb : nb, col);
 #pragma unroll
         for (int ks = 0; ks < KSTEPS; ++ks) qhi[nb][ks] = as_bf16x8(*reinterpret_cast<const u32x4 *>(r.q + 32 * ks + 8 * g));
         if constexpr (LO) {
@@ -621,167 +714,124 @@ __device__ __forceinline__ void shared_body(const CacheMap &cm, const uint16_t *
 #pragma unroll
             for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4 *>(r + 4 + 16 * db + 4 * g) = oacc[nb][db];
             __syncthreads();
-            for (int item = threadIdx.x; item < 16 * (D / 2); item += (64 * NW)) {
-                const int row = item / (D / 2), c2 = item % (D / 2);
-                float *to = rows(nb, row).record;
-                if (!to) continue;
-                float M = -INFINITY, lsum = 0.f, o0 = 0.f, o1 = 0.f;
-#pragma unroll
-                for (int w = 0; w < NW; ++w) M = fmaxf(M, red[(w * 16 + row) * REC]);
-#pragma unroll
-                for (int w = 0; w < NW; ++w) {
-                    const float *x = red + (w * 16 + row) * REC;
-                    const float wgt = __builtin_amdgcn_exp2f(x[0] - M);  // M is finite: the slice has an entry
-                    lsum = fmaf(wgt, x[1], lsum);
-                    o0 = fmaf(wgt, x[4 + 2 * c2], o0);
-                    o1 = fmaf(wgt, x[5 + 2 * c2], o1);
-                }
-                *reinterpret_cast<float2 *>(to + 4 + 2 * c2) = float2{o0, o1};
-                if (c2 == 0) *reinterpret_cast<float2 *>(to) = float2{M, lsum};
-            }
+            add_wave_states<D, NW>(red, rows, nb);
         }
     }
 }
 
-// Workgroups 0 .. n_prefix_groups - 1: (KV head, chunk of rows, slice of the prefix); the others: (KV head, sequence and chunk of 16 heads, slice of
-// its own cache).  KV heads run fastest, so that with eight of them the workgroups that read the same rows are on one XCD.
-struct SharedArgs {
-    PrefixArgs x;
-    const void *Kc, *Vc;
-    float *own_part;
-    int n_prefix_groups, chunks, n_own, head_chunks;
-};
 template <int D, int NW, int NB, bool SPLIT_ROWS, bool ROPE>
 __global__ __launch_bounds__(64 * NW, 8 / NW) void shared_decode_kernel(SharedArgs a) {
-    constexpr int REC = kShRecord<D>;
     __shared__ __attribute__((aligned(1024))) uint16_t smem[kShLds<D, NW>];
     __shared__ __attribute__((aligned(1024))) float base_s[NW][2][128];
     const PrefixArgs &x = a.x;
     const float sl2 = x.p.scale * kLog2e_f;
-    const int Hkv = x.p.Hkv;
-    int id = blockIdx.x;
-    if (id < a.n_prefix_groups) {
-        constexpr int ROWS = (SPLIT_ROWS ? 4 : 1) * 16 * NB;
-        const int kv = id % Hkv, chunk = id / Hkv % a.chunks, split = id / Hkv / a.chunks;
-        Chunk c;
-        if (!find_chunk<ROWS>(x, chunk, c)) return;
-        const CacheMap cm = uniform_map(x.pp, x.prefix_sizes, c.prefix);
-        const int np = entries_of(cm);
-        int e0, e1;
-        if (!slice_of(np, x.nsplit, split, e0, e1)) {
-            if (threadIdx.x < ROWS && c.row0 + (int)threadIdx.x < c.rows) {
-                int seq, head;
-                row_of(x, c, c.row0 + threadIdx.x, seq, head);
-                mark_empty(x.part + (((long)seq * x.p.Hq + kv * x.gq + head) * x.nsplit + split) * REC);
-            }
-            return;
-        }
-        const long head0 = ((long)c.prefix * Hkv + kv) * (long)x.pp.c * D;
-        auto rows = [&](int block, int col) __attribute__((always_inline)) {
-            const int r = c.row0 + block * 16 + col;
-            int seq, head;
-            row_of(x, c, r, seq, head);
-            const long row = (long)seq * x.p.Hq + kv * x.gq + head;
-            return ShRow{static_cast<const uint16_t *>(x.q) + row * D, ROPE ? query_position(x, seq, np) : 0,
-                         r < c.rows ? x.part + (row * x.nsplit + split) * REC : nullptr};
-        };
-        shared_body<D, NW, NB, SPLIT_ROWS, false, ROPE>(cm, static_cast<const uint16_t *>(x.Kp) + head0, static_cast<const uint16_t *>(x.Vp) + head0, e0, e1, 0,
-                                                    x.rope, x.n_pos, sl2, smem, base_s, rows);
-        return;
+    SliceWork<uint16_t> w;
+    if ((int)blockIdx.x < a.n_prefix_groups) {
+        if (!prefix_work<D, (SPLIT_ROWS ? 4 : 1) * 16 * NB, ROPE>(a, blockIdx.x, w)) return;
+        shared_body<D, NW, NB, SPLIT_ROWS, false, ROPE>(w.cm, w.K, w.V, w.e0, w.e1, 0, x.rope, x.n_pos, sl2, smem, base_s,
+                                                        [&](int block, int col) { return prefix_row<D, ROPE>(a, w, block, col); });
+    } else {
+        if (!own_work<D>(a, blockIdx.x - a.n_prefix_groups, w)) return;
+        shared_body<D, NW, 1, false, ROPE, false>(w.cm, w.K, w.V, w.e0, w.e1, w.entries - 1, x.rope, x.n_pos, sl2, smem, base_s,
+                                                  [&](int, int col) { return own_row<D>(a, w, col); });
     }
-    id -= a.n_prefix_groups;
-    const int kv = id % Hkv, hc = id / Hkv % a.head_chunks, seq = id / Hkv / a.head_chunks % x.p.S, split = id / Hkv / a.head_chunks / x.p.S;
-    const CacheMap cm = uniform_map(x.p, x.sizes, seq);
-    const int nv = entries_of(cm);
-    int e0, e1;
-    if (!slice_of(nv, a.n_own, split, e0, e1)) {
-        const int head = hc * 16 + threadIdx.x;
-        if (threadIdx.x < 16 && head < x.gq) mark_empty(a.own_part + (((long)seq * x.p.Hq + kv * x.gq + head) * a.n_own + split) * REC);
-        return;
-    }
-    const long head0 = ((long)seq * Hkv + kv) * (long)x.p.c * D;
-    auto rows = [&](int, int col) __attribute__((always_inline)) {
-        const int head = hc * 16 + col;
-        const long row = (long)seq * x.p.Hq + kv * x.gq + min(head, x.gq - 1);
-        return ShRow{static_cast<const uint16_t *>(x.q) + row * D, 0, head < x.gq ? a.own_part + (row * a.n_own + split) * REC : nullptr};
-    };
-    shared_body<D, NW, 1, false, ROPE, false>(cm, static_cast<const uint16_t *>(a.Kc) + head0, static_cast<const uint16_t *>(a.Vc) + head0, e0, e1, nv - 1, x.rope,
-                                          x.n_pos, sl2, smem, base_s, rows);
 }
 
 // ---- fp32 ------------------------------------------------------------------------------------------
-// Four waves of 16 rows each, tiles of 32 keys in LDS, v_mfma_f32_16x16x4_f32 with fp32 operands.  Lane l, group g = l / 16.  Scores: A = K, row
-// l%16 = key, B = queries, column l%16; the four k-slots of step 4 S + i are dimensions 16 S + 4 g + i, so that a lane's
-// operands are pieces of 16 bytes.  C: column l%16 = query, rows 4 g + i = keys.  Output: O^T += V^T P^T, the k-slots of step i
-// are keys 4 g + i, which the lane group holds.
+// The same division into prefixes and own caches with fp32 operands, v_mfma_f32_16x16x4_f32.  Four waves, tiles of 64 keys in LDS; the next tile's
+// rows are on their way in registers meanwhile.  SPLIT_ROWS: each wave has 16 rows of its own and takes every key; otherwise all
+// have the same 16 rows and a quarter of the tile's keys each, and their states meet in LDS.
+// Lane l, group g = l / 16.  Scores: A = K, row l%16 = key, B = queries, column l%16; the four k-slots of step 4 S + i are dimensions 16 S + 4 g + i,
+// so that a lane's operands are pieces of 16 bytes.  C: column l%16 = query, rows 4 g + i = keys.  Output: O^T += V^T P^T, the k-slots
+// of step i are keys 4 g + i, which the lane group holds.
+// KROPE (own caches): a key is turned by its distance to the query on its way into LDS, by the thread that holds both of a pair.
 typedef float f4 __attribute__((ext_vector_type(4)));
+constexpr int kFpKeys = 64;
 template <int D>
-__global__ __launch_bounds__(kShThreads) void shared_prefix_fp32_kernel(PrefixArgs x) {
-    constexpr int ROWS = 16 * kShWaves, TK = kShBlock, PITCH = D + 4, REC = kShRecord<D>;
-    __shared__ __attribute__((aligned(16))) float ks[TK * PITCH], vs[TK * PITCH];
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, col = lane & 15, g = lane >> 4;
-    const int kv = blockIdx.x, split = blockIdx.z;
-    Chunk c;
-    if (!find_chunk<ROWS>(x, blockIdx.y, c)) return;
-    const CacheMap cm = cache_map(x.pp, x.prefix_sizes + SEPKV_SIZES_COLS * c.prefix);
-    const int np = entries_of(cm);
-    int e0, e1;
-    if (!slice_of(np, x.nsplit, split, e0, e1)) {
-        if (threadIdx.x < ROWS && c.row0 + (int)threadIdx.x < c.rows) {
-            int seq, head;
-            row_of(x, c, c.row0 + threadIdx.x, seq, head);
-            mark_empty(x.part + (((long)seq * x.p.Hq + kv * x.gq + head) * x.nsplit + split) * REC);
-        }
-        return;
-    }
-    const float *Kh = static_cast<const float *>(x.Kp) + ((long)c.prefix * x.p.Hkv + kv) * (long)x.pp.c * D;
-    const float *Vh = static_cast<const float *>(x.Vp) + ((long)c.prefix * x.p.Hkv + kv) * (long)x.pp.c * D;
-    int seq, head;
-    row_of(x, c, c.row0 + wave * 16 + col, seq, head);
-    const float *qrow = static_cast<const float *>(x.q) + ((long)seq * x.p.Hq + kv * x.gq + head) * D + 4 * g;
+constexpr int kFpPitch = D + 4;  // floats per row in LDS
+
+template <int D, bool SPLIT_ROWS, bool KROPE, bool LO, typename Rows>
+__device__ __forceinline__ void shared_fp32_body(const CacheMap &cm, const float *__restrict__ Kh, const float *__restrict__ Vh, int e0, int e1, int last,
+                                                 const float *__restrict__ rope, int n_pos, float sl2, float (&smem)[2 * kFpKeys * kFpPitch<D>],
+                                                 const Rows &rows) {
+    constexpr int PITCH = kFpPitch<D>, REC = kShRecord<D>, ITEMS = kFpKeys * (D / 8) / kShThreads;
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), col = lane & 15, g = lane >> 4;
+    float *const ks = smem, *const vs = smem + kFpKeys * PITCH;
     f4 q[D / 16];
+    {
+        const auto r = rows(SPLIT_ROWS ? wave : 0, col);
 #pragma unroll
-    for (int s = 0; s < D / 16; ++s) q[s] = *reinterpret_cast<const f4 *>(qrow + 16 * s);
-    if (x.rope) {
-        const float *row = x.rope + (long)query_position(x, seq, np) * D + 4 * g;
+        for (int s = 0; s < D / 16; ++s) q[s] = *reinterpret_cast<const f4 *>(r.q + 16 * s + 4 * g);
+        if constexpr (LO) {
+            const float *row = rope + (long)r.position * D + 4 * g;
 #pragma unroll
-        for (int s = 0; s < D / 32; ++s) {
-            const f4 cs = *reinterpret_cast<const f4 *>(row + 16 * s), sn = *reinterpret_cast<const f4 *>(row + D / 2 + 16 * s);
-            const f4 u = q[s], v = q[s + D / 32];
-            q[s] = u * cs - v * sn;
-            q[s + D / 32] = v * cs + u * sn;
+            for (int s = 0; s < D / 32; ++s) {
+                const f4 cs = *reinterpret_cast<const f4 *>(row + 16 * s), sn = *reinterpret_cast<const f4 *>(row + D / 2 + 16 * s);
+                const f4 u = q[s], v = q[s + D / 32];
+                q[s] = u * cs - v * sn;
+                q[s + D / 32] = v * cs + u * sn;
+            }
         }
     }
-    const float sl2 = x.p.scale * kLog2e_f;
+    // a thread's pieces of a tile: columns pc .. pc + 3 and their partners D/2 on
+    f4 kr[ITEMS][2], vr[ITEMS][2], cs[KROPE ? ITEMS : 1], sn[KROPE ? ITEMS : 1];
+    auto fetch = [&](int eb) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const int item = threadIdx.x + i * kShThreads, pc = item % (D / 8) * 4, e = min(eb + item / (D / 8), e1 - 1);
+            const long off = (long)slot_of(cm, e) * D + pc;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                kr[i][h] = *reinterpret_cast<const f4 *>(Kh + off + h * (D / 2));
+                vr[i][h] = *reinterpret_cast<const f4 *>(Vh + off + h * (D / 2));
+            }
+            if constexpr (KROPE) {
+                const float *row = rope + (long)min(last - e, n_pos - 1) * D + pc;
+                cs[i] = *reinterpret_cast<const f4 *>(row);
+                sn[i] = *reinterpret_cast<const f4 *>(row + D / 2);
+            }
+        }
+    };
+    auto stage = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const int item = threadIdx.x + i * kShThreads, at = item / (D / 8) * PITCH + item % (D / 8) * 4;
+            f4 x = kr[i][0], y = kr[i][1];
+            if constexpr (KROPE) {  // R(-distance)
+                x = kr[i][0] * cs[i] + kr[i][1] * sn[i];
+                y = kr[i][1] * cs[i] - kr[i][0] * sn[i];
+            }
+            *reinterpret_cast<f4 *>(ks + at) = x;
+            *reinterpret_cast<f4 *>(ks + at + D / 2) = y;
+            *reinterpret_cast<f4 *>(vs + at) = vr[i][0];
+            *reinterpret_cast<f4 *>(vs + at + D / 2) = vr[i][1];
+        }
+    };
     f4 o[D / 16];
 #pragma unroll
     for (int db = 0; db < D / 16; ++db) o[db] = f4{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
-    for (int eb = e0; eb < e1; eb += TK) {
+    fetch(e0);
+    for (int eb = e0; eb < e1; eb += kFpKeys) {
         __syncthreads();
-        for (int i = threadIdx.x; i < TK * (D / 4); i += kShThreads) {
-            const int r = i / (D / 4), pc = i % (D / 4) * 4;
-            const long off = (long)decode_slot_of(cm, min(eb + r, e1 - 1)) * D + pc;
-            *reinterpret_cast<f4 *>(ks + r * PITCH + pc) = *reinterpret_cast<const f4 *>(Kh + off);
-            *reinterpret_cast<f4 *>(vs + r * PITCH + pc) = *reinterpret_cast<const f4 *>(Vh + off);
-        }
+        stage();
         __syncthreads();
-#pragma unroll
-        for (int blk = 0; blk < TK / 16; ++blk) {
+        if (eb + kFpKeys < e1) fetch(eb + kFpKeys);
+#pragma unroll 1
+        for (int blk = SPLIT_ROWS ? 0 : wave; blk < (SPLIT_ROWS ? kFpKeys / 16 : wave + 1); ++blk) {
             const int n_valid = e1 - eb - 16 * blk;
-            if (n_valid <= 0) continue;
+            if (n_valid <= 0) break;
+            const float *const kb = ks + 16 * blk * PITCH, *const vb = vs + 16 * blk * PITCH;
             f4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int st = 0; st < D / 16; ++st) {
-                const f4 k = *reinterpret_cast<const f4 *>(ks + (16 * blk + col) * PITCH + 16 * st + 4 * g);
+                const f4 k = *reinterpret_cast<const f4 *>(kb + col * PITCH + 16 * st + 4 * g);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k[i], q[st][i], s, 0, 0, 0);
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) s[i] = 4 * g + i < n_valid ? s[i] * sl2 : -INFINITY;
-            float m_new = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
-            m_new = fmaxf(m_new, __shfl_xor(m_new, 16));
-            m_new = fmaxf(m, fmaxf(m_new, __shfl_xor(m_new, 32)));  // finite: key 0 of the block is valid
+            const float m_new = fmaxf(m, groups_max(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]))));  // finite: key 0 of the block is valid
             const float alpha = exp2f(m - m_new);
             m = m_new;
             l *= alpha;
@@ -794,26 +844,50 @@ __global__ __launch_bounds__(kShThreads) void shared_prefix_fp32_kernel(PrefixAr
             for (int db = 0; db < D / 16; ++db) {
                 o[db] *= alpha;
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    o[db] = __builtin_amdgcn_mfma_f32_16x16x4f32(vs[(16 * blk + 4 * g + i) * PITCH + 16 * db + col], s[i], o[db], 0, 0, 0);
+                for (int i = 0; i < 4; ++i) o[db] = __builtin_amdgcn_mfma_f32_16x16x4f32(vb[(4 * g + i) * PITCH + 16 * db + col], s[i], o[db], 0, 0, 0);
             }
         }
     }
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
-    if (c.row0 + wave * 16 + col >= c.rows) return;
-    float *r = x.part + (((long)seq * x.p.Hq + kv * x.gq + head) * x.nsplit + split) * REC;
-    if (g == 0) r[0] = m, r[1] = l;
+    l = groups_sum(l);
+    if constexpr (SPLIT_ROWS) {
+        float *const to = rows(wave, col).record;
+        if (!to) return;
+        if (g == 0) *reinterpret_cast<float2 *>(to) = float2{m, l};
 #pragma unroll
-    for (int db = 0; db < D / 16; ++db) *reinterpret_cast<f4 *>(r + 4 + 16 * db + 4 * g) = o[db];
+        for (int db = 0; db < D / 16; ++db) *reinterpret_cast<f4 *>(to + 4 + 16 * db + 4 * g) = o[db];
+    } else {
+        static_assert(kShWaves * 16 * REC <= 2 * kFpKeys * PITCH, "the waves' states fit the tiles");
+        __syncthreads();
+        float *const r = smem + (wave * 16 + col) * REC;
+        if (g == 0) *reinterpret_cast<float2 *>(r) = float2{m, l};
+#pragma unroll
+        for (int db = 0; db < D / 16; ++db) *reinterpret_cast<f4 *>(r + 4 + 16 * db + 4 * g) = o[db];
+        __syncthreads();
+        add_wave_states<D, kShWaves>(smem, rows, 0);
+    }
+}
+
+template <int D, bool SPLIT_ROWS, bool ROPE>
+__global__ __launch_bounds__(kShThreads, 2) void shared_decode_fp32_kernel(SharedArgs a) {
+    constexpr int ROWS = (SPLIT_ROWS ? kShWaves : 1) * 16;
+    __shared__ __attribute__((aligned(16))) float smem[2 * kFpKeys * kFpPitch<D>];
+    const PrefixArgs &x = a.x;
+    const float sl2 = x.p.scale * kLog2e_f;
+    SliceWork<float> w;
+    if ((int)blockIdx.x < a.n_prefix_groups) {
+        if (!prefix_work<D, ROWS, ROPE>(a, blockIdx.x, w)) return;
+        shared_fp32_body<D, SPLIT_ROWS, false, ROPE>(w.cm, w.K, w.V, w.e0, w.e1, 0, x.rope, x.n_pos, sl2, smem, [&](int block, int col) { return prefix_row<D, ROPE>(a, w, block, col); });
+    } else {
+        if (!own_work<D>(a, blockIdx.x - a.n_prefix_groups, w)) return;
+        shared_fp32_body<D, false, ROPE, false>(w.cm, w.K, w.V, w.e0, w.e1, w.entries - 1, x.rope, x.n_pos, sl2, smem, [&](int, int col) { return own_row<D>(a, w, col); });
+    }
 }
 
 // ---- the slices' sum: a workgroup per (sequence, head), prefix slices first, then the own cache's; wave w takes slices w, w + 4, ... of
 // both, eight records in one round trip, and the waves' sums are added in wave order.  Nothing but the records has to be read for that (a
 // slice without an entry says so in its own; those of a prefix that the sequence does not have are skipped), so that the kernel is one
 // round trip and its launch --------------------------------
-// OWN: floats of an own record, whose outputs are its last D
-template <typename T, int D, int OWN>
+template <typename T, int D>
 __global__ __launch_bounds__(kShThreads) void shared_merge_kernel(sepkv_params p, int n_prefixes, int n_prefix, int n_own,
                                                                   const int32_t *__restrict__ prefix_of, const float *__restrict__ prefix_part,
                                                                   const float *__restrict__ own_part, T *__restrict__ out, float *__restrict__ lse) {
@@ -824,14 +898,14 @@ __global__ __launch_bounds__(kShThreads) void shared_merge_kernel(sepkv_params p
     const long row = (long)seq * p.Hq + head;
     const int of = prefix_of[seq];
     const int total = n_prefix + n_own;
-    const float *pre = prefix_part + row * n_prefix * REC, *own = own_part + row * n_own * OWN;
+    const float *pre = prefix_part + row * n_prefix * REC, *own = own_part + row * n_own * REC;
     float M = -INFINITY, l = 0.f, o[C] = {};
     for (int k0 = wave; k0 < total; k0 += kShWaves * NR) {
         float m[NR], ls[NR], os[NR][C];
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
             const int k = min(k0 + kShWaves * i, total - 1);  // past the last one: that again, with weight 0
-            const float *r = k < n_prefix ? pre + k * REC : own + (k - n_prefix) * OWN, *v = r + (k < n_prefix ? REC : OWN) - D + C * lane;
+            const float *r = k < n_prefix ? pre + k * REC : own + (k - n_prefix) * REC, *v = r + 4 + C * lane;
             const float2 ml = *reinterpret_cast<const float2 *>(r);
             m[i] = ml.x, ls[i] = ml.y;
 #pragma unroll
@@ -890,7 +964,6 @@ struct SharedShape {
     int chunks;       // of rows, all prefixes together, at most
     int n_prefix;     // slices per prefix
     int n_own;        // slices per own cache
-    int record;       // floats of an own cache's record
 };
 // Host estimate in microseconds, from the capacities (the device alone knows how much of them is in use).  `bytes_us`: what reading every cache once
 // takes.  A prefix is cut so finely that a workgroup's walk through its slice, at `step` per 32 keys while the memory is busy, ends
@@ -902,16 +975,9 @@ SharedShape shared_shape(const sepkv_params &p, const sepkv_params &pp, bool rop
     const long nb = (pp.c + kShBlock - 1) / kShBlock, own_nb = (p.c + kShBlock - 1) / kShBlock;
     auto chunks_of = [&](long rows) { return pp.S == 1 ? (all + rows - 1) / rows : all / rows + (pp.S < p.S ? pp.S : p.S); };
     s.waves = 4;
-    if (p.dtype == SEPATTN_FP32) {
-        s.chunks = (int)chunks_of(64);
-        s.n_prefix = (int)std::clamp(2 * units / ((long)p.Hkv * s.chunks), 1L, std::min(nb, 64L));
-        s.n_own = decode_record_slices(p);
-        s.record = p.d + 2;
-        return s;
-    }
-    s.record = p.d + 4;
+    const bool fp32 = p.dtype == SEPATTN_FP32;
     const long slots = (p.d == 64 ? 3 : 2) * units, own_groups = (long)p.S * p.Hkv * ((gq + 15) / 16);
-    const double own_rows = (double)p.S * p.c, prefix_rows = (double)pp.S * pp.c, bytes_us = 4.0 * p.d * p.Hkv * (own_rows + prefix_rows) / 5.3e6;
+    const double own_rows = (double)p.S * p.c, prefix_rows = (double)pp.S * pp.c, bytes_us = (fp32 ? 8.0 : 4.0) * p.d * p.Hkv * (own_rows + prefix_rows) / 5.3e6;
     const double most_us = std::max(5.0, bytes_us * (0.4 + 0.5 * prefix_rows / (own_rows + prefix_rows)));
     auto cut = [&](double step) {
         const long groups = (long)p.Hkv * s.chunks, finest = std::clamp(nb / (nb > 64 ? 8 : 4), 1L, 64L), room = (slots - own_groups) / groups;
@@ -921,7 +987,11 @@ SharedShape shared_shape(const sepkv_params &p, const sepkv_params &pp, bool rop
         else if (ns > slots / groups && slots / groups * 10 >= ns * 7) ns = slots / groups;
         return (int)std::clamp(ns, 1L, finest);
     };
-    if (per_prefix <= 32) {
+    if (fp32) {
+        s.split_rows = per_prefix > 16;
+        s.chunks = (int)chunks_of(s.split_rows ? 64 : 16);
+        s.n_prefix = cut(s.split_rows ? 1.6 : 0.8);
+    } else if (per_prefix <= 32) {
         s.nb = per_prefix <= 16 ? 1 : 2;
         s.chunks = (int)chunks_of(16 * s.nb);
         s.n_prefix = cut(s.nb == 1 ? 0.35 : 0.45);
@@ -949,7 +1019,7 @@ size_t prefix_record_bytes(const sepkv_params &p, const SharedShape &s) {
     return align_up((size_t)p.S * p.Hq * s.n_prefix * (p.d + 4) * sizeof(float), 256);
 }
 size_t own_record_bytes(const sepkv_params &p, const SharedShape &s) {
-    return align_up((size_t)p.S * p.Hq * s.n_own * s.record * sizeof(float), 256);
+    return align_up((size_t)p.S * p.Hq * s.n_own * (p.d + 4) * sizeof(float), 256);
 }
 
 }  // namespace
@@ -970,22 +1040,18 @@ int launch_decode_shared(const SharedDecode &x, hipStream_t st) {
     const PrefixArgs a = {x.p, x.pp, gq, s.n_prefix, x.q, x.Kp, x.Vp, x.sizes, x.prefix_sizes, x.group_start, x.group_seq,
                           x.rope, x.n_pos, x.part};
     const dim3 block(kShThreads);
-    if (x.p.dtype == SEPATTN_FP32) {
-        {
-            ProfScope prof(SEPATTN_K_DECODE_SPLIT, st);
-            const dim3 grid(x.p.Hkv, s.chunks, s.n_prefix);
-            if (x.p.d == 64) hipLaunchKernelGGL((shared_prefix_fp32_kernel<64>), grid, block, 0, st, a);
-            else hipLaunchKernelGGL((shared_prefix_fp32_kernel<128>), grid, block, 0, st, a);
-        }
-        int rc = launch_status();
-        if (rc == SEPATTN_OK) rc = launch_decode_records(x.p, s.n_own, x.q, x.Kc, x.Vc, x.sizes, x.rope, x.n_pos, own_part, st);
-        if (rc != SEPATTN_OK) return rc;
-    } else {
+    {
         const int head_chunks = (gq + 15) / 16;
         const long n_prefix_groups = (long)x.p.Hkv * s.chunks * s.n_prefix, n = n_prefix_groups + (long)x.p.Hkv * head_chunks * x.p.S * s.n_own;
         if (n > 0x7FFFFFFFL) return SEPATTN_ERR_SHAPE;
         const SharedArgs all = {a, x.Kc, x.Vc, own_part, (int)n_prefix_groups, s.chunks, s.n_own, head_chunks};
         ProfScope prof(SEPATTN_K_DECODE_SPLIT, st);
+        auto fp32 = [&](auto D_, auto ROWS_) {
+            constexpr int D = decltype(D_)::value;
+            constexpr bool ROWS = decltype(ROWS_)::value != 0;
+            if (x.rope) hipLaunchKernelGGL((shared_decode_fp32_kernel<D, ROWS, true>), dim3((unsigned)n), block, 0, st, all);
+            else hipLaunchKernelGGL((shared_decode_fp32_kernel<D, ROWS, false>), dim3((unsigned)n), block, 0, st, all);
+        };
         auto go = [&](auto D_, auto NW_, auto NB_, auto ROWS_, auto ROPE_) {
             constexpr int D = decltype(D_)::value, NW = decltype(NW_)::value, NB = decltype(NB_)::value;
             constexpr bool ROWS = decltype(ROWS_)::value != 0, ROPE = decltype(ROPE_)::value != 0;
@@ -1006,7 +1072,10 @@ int launch_decode_shared(const SharedDecode &x, hipStream_t st) {
                 if (s.nb == 3) return go(D_, W4{}, N3{}, N1{}, ROPE_);
             s.nb == 1 ? go(D_, W4{}, N1{}, N1{}, ROPE_) : go(D_, W4{}, N2{}, N1{}, ROPE_);
         };
-        if (x.p.d == 64) x.rope ? shape(IntC<64>{}, N1{}) : shape(IntC<64>{}, IntC<0>{});
+        if (x.p.dtype == SEPATTN_FP32) {
+            if (x.p.d == 64) s.split_rows ? fp32(IntC<64>{}, N1{}) : fp32(IntC<64>{}, IntC<0>{});
+            else s.split_rows ? fp32(IntC<128>{}, N1{}) : fp32(IntC<128>{}, IntC<0>{});
+        } else if (x.p.d == 64) x.rope ? shape(IntC<64>{}, N1{}) : shape(IntC<64>{}, IntC<0>{});
         else x.rope ? shape(IntC<128>{}, N1{}) : shape(IntC<128>{}, IntC<0>{});
         const int rc = launch_status();
         if (rc != SEPATTN_OK) return rc;
@@ -1015,7 +1084,7 @@ int launch_decode_shared(const SharedDecode &x, hipStream_t st) {
     auto go = [&](auto T_, auto D_) {
         using T = decltype(T_);
         constexpr int D = decltype(D_)::value;
-        hipLaunchKernelGGL((shared_merge_kernel<T, D, sizeof(T) == 2 ? D + 4 : D + 2>), dim3(x.p.Hq, x.p.S), block, 0, st, x.p, x.pp.S, s.n_prefix, s.n_own,
+        hipLaunchKernelGGL((shared_merge_kernel<T, D>), dim3(x.p.Hq, x.p.S), block, 0, st, x.p, x.pp.S, s.n_prefix, s.n_own,
                            x.prefix_of, x.part, own_part, static_cast<T *>(x.out), x.lse);
     };
     if (x.p.dtype == SEPATTN_BF16) x.p.d == 64 ? go(uint16_t{}, IntC<64>{}) : go(uint16_t{}, IntC<128>{});

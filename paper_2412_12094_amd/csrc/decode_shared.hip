@@ -883,28 +883,30 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_decode_fp32_kernel(Share
     }
 }
 
-// ---- the slices' sum: a workgroup per (sequence, head), prefix slices first, then the own cache's; wave w takes slices w, w + 4, ... of
-// both, eight records in one round trip, and the waves' sums are added in wave order.  Nothing but the records has to be read for that (a
-// slice without an entry says so in its own; those of a prefix that the sequence does not have are skipped), so that the kernel is one
-// round trip and its launch --------------------------------
-template <typename T, int D>
+// ---- the slices' sum ------------------------------------------------------------------------------
+// WPR waves per (sequence, head), prefix slices first, then the own cache's; wave w takes slices w, w + WPR, ... of both, eight records in one
+// round trip, and the waves' sums are added in wave order.  Nothing but the records has to be read for that (a slice without an entry
+// says so in its own; those of a prefix that the sequence does not have are skipped), so that the kernel is one round trip and its
+// launch: 3 us for a few rows, 5 for 1024 rows of 17 records, 10 for 1536 rows of 49.
+template <typename T, int D, int WPR>
 __global__ __launch_bounds__(kShThreads) void shared_merge_kernel(sepkv_params p, int n_prefixes, int n_prefix, int n_own,
                                                                   const int32_t *__restrict__ prefix_of, const float *__restrict__ prefix_part,
                                                                   const float *__restrict__ own_part, T *__restrict__ out, float *__restrict__ lse) {
     constexpr int REC = kShRecord<D>, C = D / kWave, NR = 8;
-    __shared__ float state[kShWaves][D + 2];
-    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int head = blockIdx.x, seq = blockIdx.y;
+    __shared__ float state[WPR][D + 2];
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), w0 = WPR == 1 ? 0 : wave;
+    const int head = WPR == 1 ? blockIdx.x * kShWaves + wave : blockIdx.x, seq = blockIdx.y;
+    if (head >= p.Hq) return;
     const long row = (long)seq * p.Hq + head;
     const int of = prefix_of[seq];
     const int total = n_prefix + n_own;
     const float *pre = prefix_part + row * n_prefix * REC, *own = own_part + row * n_own * REC;
     float M = -INFINITY, l = 0.f, o[C] = {};
-    for (int k0 = wave; k0 < total; k0 += kShWaves * NR) {
+    for (int k0 = w0; k0 < total; k0 += WPR * NR) {
         float m[NR], ls[NR], os[NR][C];
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
-            const int k = min(k0 + kShWaves * i, total - 1);  // past the last one: that again, with weight 0
+            const int k = min(k0 + WPR * i, total - 1);  // past the last one: that again, with weight 0
             const float *r = k < n_prefix ? pre + k * REC : own + (k - n_prefix) * REC, *v = r + 4 + C * lane;
             const float2 ml = *reinterpret_cast<const float2 *>(r);
             m[i] = ml.x, ls[i] = ml.y;
@@ -915,7 +917,7 @@ __global__ __launch_bounds__(kShThreads) void shared_merge_kernel(sepkv_params p
         float Mn = M;
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
-            const int k = k0 + kShWaves * i;
+            const int k = k0 + WPR * i;
             if (k >= total || (k < n_prefix && !shares)) m[i] = -INFINITY;
             Mn = fmaxf(Mn, m[i]);
         }
@@ -934,6 +936,17 @@ __global__ __launch_bounds__(kShThreads) void shared_merge_kernel(sepkv_params p
             for (int j = 0; j < C; ++j) o[j] = fmaf(w, used ? os[i][j] : 0.f, o[j]);
         }
     }
+    auto write = [&](int c, float v, float lsum) {
+        v = lsum > 0.f ? v / lsum : 0.f;
+        if constexpr (sizeof(T) == 2) out[row * D + c] = decode_f32_to_bf16(v);
+        else out[row * D + c] = v;
+        if (lse && c == 0) lse[row] = lsum > 0.f ? (M + log2f(lsum)) * kLn2_f : -INFINITY;
+    };
+    if constexpr (WPR == 1) {
+#pragma unroll
+        for (int j = 0; j < C; ++j) write(C * lane + j, o[j], l);
+        return;
+    }
     if (lane == 0) state[wave][D] = M, state[wave][D + 1] = l;
 #pragma unroll
     for (int j = 0; j < C; ++j) state[wave][C * lane + j] = o[j];
@@ -942,18 +955,15 @@ __global__ __launch_bounds__(kShThreads) void shared_merge_kernel(sepkv_params p
     if (c >= D) return;
     M = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < kShWaves; ++w) M = fmaxf(M, state[w][D]);
+    for (int w = 0; w < WPR; ++w) M = fmaxf(M, state[w][D]);
     float lsum = 0.f, v = 0.f;
 #pragma unroll
-    for (int w = 0; w < kShWaves; ++w) {
+    for (int w = 0; w < WPR; ++w) {
         const float wgt = state[w][D] == -INFINITY ? 0.f : exp2f(state[w][D] - M);
         lsum = fmaf(wgt, state[w][D + 1], lsum);
         v = fmaf(wgt, state[w][c], v);
     }
-    v = lsum > 0.f ? v / lsum : 0.f;
-    if constexpr (sizeof(T) == 2) out[row * D + c] = decode_f32_to_bf16(v);
-    else out[row * D + c] = v;
-    if (lse && c == 0) lse[row] = lsum > 0.f ? (M + log2f(lsum)) * kLn2_f : -INFINITY;
+    write(c, v, lsum);
 }
 
 // ---- host ------------------------------------------------------------------------------------------
@@ -980,8 +990,8 @@ SharedShape shared_shape(const sepkv_params &p, const sepkv_params &pp, bool rop
     const double own_rows = (double)p.S * p.c, prefix_rows = (double)pp.S * pp.c, bytes_us = (fp32 ? 8.0 : 4.0) * p.d * p.Hkv * (own_rows + prefix_rows) / 5.3e6;
     const double most_us = std::max(5.0, bytes_us * (0.4 + 0.5 * prefix_rows / (own_rows + prefix_rows)));
     auto cut = [&](double step) {
-        const long groups = (long)p.Hkv * s.chunks, finest = std::clamp(nb / (nb > 64 ? 8 : 4), 1L, 64L), room = (slots - own_groups) / groups;
-        long ns = std::max((long)std::ceil(nb * step * (p.d == 64 ? 0.6 : 1.0) / most_us), (slots / 2 - own_groups) / groups);
+        const long groups = (long)p.Hkv * s.chunks, finest = std::clamp(nb / (fp32 ? 2 : nb > 64 ? 8 : 4), 1L, 64L), room = (slots - own_groups) / groups;
+        long ns = std::max((long)std::ceil(nb * step * (p.d == 64 ? 0.6 : 1.0) / most_us - 0.25), (slots / 2 - own_groups) / groups);
         // no second round of workgroups for a few slices
         if (ns > room && room * 10 >= ns * 6) ns = room;
         else if (ns > slots / groups && slots / groups * 10 >= ns * 7) ns = slots / groups;
@@ -990,7 +1000,7 @@ SharedShape shared_shape(const sepkv_params &p, const sepkv_params &pp, bool rop
     if (fp32) {
         s.split_rows = per_prefix > 16;
         s.chunks = (int)chunks_of(s.split_rows ? 64 : 16);
-        s.n_prefix = cut(s.split_rows ? 1.6 : 0.8);
+        s.n_prefix = cut(s.split_rows ? 1.9 : 0.5);
     } else if (per_prefix <= 32) {
         s.nb = per_prefix <= 16 ? 1 : 2;
         s.chunks = (int)chunks_of(16 * s.nb);
@@ -1001,10 +1011,10 @@ SharedShape shared_shape(const sepkv_params &p, const sepkv_params &pp, bool rop
         s.nb = per_prefix <= 64 ? 1 : per_prefix <= 128 ? 2 : 3;
         // three column blocks where they waste no more rows than two (turned queries at d = 128 have no registers for them)
         if (s.nb == 3 && ((rope && p.d == 128) || (per_prefix + 191) / 192 * 3 > (per_prefix + 127) / 128 * 2)) s.nb = 2;
-        for (;; --s.nb) {  // fewer rows per workgroup, and more workgroups, where a slice would be a few steps
+        for (;; --s.nb) {  // fewer rows per workgroup, and more workgroups, where a slice would be a few steps and there is room
             s.chunks = (int)chunks_of(64 * s.nb);
             s.n_prefix = cut(step[rope && p.d == 128][s.nb - 1]);
-            if (s.nb == 1 || nb / s.n_prefix >= 16) break;
+            if (s.nb == 1 || nb / s.n_prefix >= 16 || own_groups + (long)p.Hkv * ((all + 64 * s.nb - 1) / (64 * s.nb)) * s.n_prefix >= slots) break;
         }
         if (p.d == 128 && !rope && s.nb > 1 && s.n_prefix >= 24) {
             s.waves = 8;
@@ -1084,8 +1094,14 @@ int launch_decode_shared(const SharedDecode &x, hipStream_t st) {
     auto go = [&](auto T_, auto D_) {
         using T = decltype(T_);
         constexpr int D = decltype(D_)::value;
-        hipLaunchKernelGGL((shared_merge_kernel<T, D>), dim3(x.p.Hq, x.p.S), block, 0, st, x.p, x.pp.S, s.n_prefix, s.n_own,
-                           x.prefix_of, x.part, own_part, static_cast<T *>(x.out), x.lse);
+        auto rows = [&](auto WPR_) {
+            constexpr int WPR = decltype(WPR_)::value;
+            const dim3 grid(WPR == 1 ? (x.p.Hq + kShWaves - 1) / kShWaves : x.p.Hq, x.p.S);
+            hipLaunchKernelGGL((shared_merge_kernel<T, D, WPR>), grid, block, 0, st, x.p, x.pp.S, s.n_prefix, s.n_own, x.prefix_of, x.part,
+                               own_part, static_cast<T *>(x.out), x.lse);
+        };
+        // one round trip of one wave where the records are few
+        s.n_prefix + s.n_own <= 8 ? rows(IntC<1>{}) : rows(IntC<kShWaves>{});
     };
     if (x.p.dtype == SEPATTN_BF16) x.p.d == 64 ? go(uint16_t{}, IntC<64>{}) : go(uint16_t{}, IntC<128>{});
     else x.p.d == 64 ? go(float{}, IntC<64>{}) : go(float{}, IntC<128>{});

@@ -245,8 +245,8 @@ int sepattn_backward_headwise(const sepattn_params *p, const int32_t *n_per_head
  *              not together with positions (SEPATTN_ERR_PARAM)
  *   strides    HOST, elements between neighbours in the batch, head and token dimension (the head dimension is
  *              contiguous); NULL: dense [B, H, L, d].  Rows are 16-byte aligned: pointers, and strides of dimensions larger
- *              than 1 in bytes, are multiples of 16.  Inputs may be broadcast (stride 0); the rows of an output must not overlap
- *              (SEPATTN_ERR_PARAM, as for a negative stride)
+ *              than 1 in bytes, are multiples of 16.  Inputs may be broadcast (stride 0); of an output, each stride has to reach past
+ *              all that the smaller ones cover, so that no two rows overlap (SEPATTN_ERR_PARAM, as for a negative stride)
  *   v, V       both NULL where the values are laid out already (dv, dV likewise)
  * An output may be its own input (same pointer and strides: in place); otherwise outputs must not overlap inputs.
  * ------------------------------------------------------------------------------------------ */
@@ -456,7 +456,7 @@ int sepkv_fill_from_prefill_zeroed(const sepkv_params *p, int L, int nw, const v
 /* ------------------------------------------------------------------------------------------
  * Generation behind shared prompts.  Sequences that begin with the same prompt keep its entries once: G prefix caches, each a
  * four-block cache of the layout above that is filled once (sepkv_fill_from_prefill, or a prompt kept whole in the
- * window of a cache with a = s = 0, w = 1, c = its length) and not written afterwards, beside a cache of its own per sequence for
+ * window of a cache with a = s = 0, w = 1, c = its length or 2) and not written afterwards, beside a cache of its own per sequence for
  * what follows.  A sequence attends to all entries of its prefix and all of its own: Eq. 1 with M = 1 over both.
  *
  * sepkv_group_sequences lists the sequences by prefix, once per batch (the list serves all layers and tokens):

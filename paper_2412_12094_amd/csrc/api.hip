@@ -491,7 +491,7 @@ static int rope_strides(const sepattn_rope_params &p, int H, const sepattn_strid
     for (int i = 0; i < 3; ++i) {
         if (size[i] == 1) continue;
         if (stride[i] < 0 || stride[i] % unit != 0) return SEPATTN_ERR_PARAM;
-        if (stride[i] > (int64_t)1 << 40) return SEPATTN_ERR_SHAPE;
+        if (stride[i] > (int64_t)1 << 40 || stride[i] > ((int64_t)1 << 60) / size[i]) return SEPATTN_ERR_SHAPE;
     }
     if (!output) return SEPATTN_OK;
     for (int i = 0; i < 3; ++i)

@@ -56,6 +56,7 @@ def test_rope_arguments(sp, fn):
     for s in ((-2048, 128, 1024), (1, 128, 1024), (16384, 132, 1024), (16384, 128, 1028)):  # negative, not a multiple of 8
         assert r(frm=(s, None, None)) == 3
     assert r(frm=((1 << 41, 128, 1024), None, None)) == 2
+    assert r(frm=((128, 128, 1 << 40), None, None), L=1 << 30, B=1, Hq=1) == 2  # a span that 64 bits do not hold
     # outputs whose rows overlap
     for s in ((0, 2048, 128), (16 * 8 * 128, 0, 128), (16 * 8 * 128, 2048, 120), (16 * 8 * 128 - 8, 2048, 128), (128, 128, 2048), (16384, 1024, 128)):
         assert r(to=(s, None, None)) == 3, s

@@ -652,9 +652,10 @@ PyObject *rope(PyObject *const *a) {
                   if constexpr (BACKWARD) {  // as one fused projection puts them out: [B, L, q heads | k heads | v heads, d]
                       const int64_t Hv = v.defined() ? p.Hkv : 0;
                       const at::Tensor dx = empty({p.B, p.L, p.Hq + p.Hkv + Hv, p.d}, q.scalar_type(), q.device());
-                      r[0].to = dx.narrow(2, 0, p.Hq).transpose(1, 2);
-                      r[1].to = dx.narrow(2, p.Hq, p.Hkv).transpose(1, 2);
-                      if (v.defined()) r[2].to = dx.narrow(2, p.Hq + p.Hkv, Hv).transpose(1, 2);
+                      const at::AutoDispatchBelowADInplaceOrView plain;
+                      const int64_t d = p.d, l = (p.Hq + p.Hkv + Hv) * d, first[3] = {0, p.Hq * d, (p.Hq + p.Hkv) * d};
+                      for (int i = 0; i < (v.defined() ? 3 : 2); ++i)
+                          r[i].to = dx.as_strided({p.B, i == 0 ? p.Hq : p.Hkv, p.L, p.d}, {p.L * l, d, l, 1}, first[i]);
                   } else {
                       for (Rows &x : r)
                           if (x.from.defined()) x.to = fresh_like(x.from);

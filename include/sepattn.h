@@ -248,7 +248,8 @@ int sepattn_backward_headwise(const sepattn_params *p, const int32_t *n_per_head
  *              than 1 in bytes, are multiples of 16.  Inputs may be broadcast (stride 0); of an output, each stride has to reach past
  *              all that the smaller ones cover, so that no two rows overlap (SEPATTN_ERR_PARAM, as for a negative stride)
  *   v, V       both NULL where the values are laid out already (dv, dV likewise)
- * An output may be its own input (same pointer and strides: in place); otherwise outputs must not overlap inputs.
+ * An output may be its own input (same pointer and strides: in place); otherwise outputs must not overlap inputs.  The backward call
+ * has a gradient for every row: those of rows that were one broadcast row of the forward call are for the caller to add.
  * ------------------------------------------------------------------------------------------ */
 typedef struct {
     int B;           /* sequences                                                              */

@@ -4,8 +4,15 @@
 // Softmax over the two sets is softmax over each, joined by maximum and sum, so the work is cut into
 //   - the prefixes: all query heads of all sequences of a prefix that read one KV head are the rows of ONE product with its
 //     keys and values, which are read once for all of them (per chunk of rows) and not once per sequence;
-//   - the own caches, as sepattn_decode does (one slice of a cache per workgroup);
-//   - the sum of the slices' records (maximum, sum, unnormalised output), one wave per (sequence, head).
+//   - the own caches, as sepattn_decode does (one slice of a cache per workgroup), in the same launch;
+//   - the sum of the slices' records (maximum, sum, unnormalised output), in a second launch.
+// What it cannot do without is to read every cache once, and 4 d operations per (query head, entry): with R rows on a KV head an entry's 4 d
+// bytes feed 4 d R operations, so that from about 260 rows on the matrix units would bound it, below that the memory.
+// Measured, 32/8 heads, d = 128, bf16, microseconds of the first launch + the second (bytes of the caches at the rate of a large copy):
+//   2 sequences behind 300 entries                                6.4 + 3.1 (1.2; launches and round trips)
+//   32 sequences, 16 KV rows each, behind 8192 entries, turned   25 + 4.9 (18.7; 2.9 TB/s over both)
+//   48 sequences, 1 prefix of 65536, 192 rows per KV head        78 + 7.5 (72; 4.2 TB/s, 610 TFLOP/s)
+// (In one launch, the last slice of a row adding its records: 12.8 instead of 9.5 for the first; four round trips past the L2 in sequence.)
 #include "common.h"
 #include "decode_common.h"
 #include "mfma_common.h"
@@ -17,8 +24,8 @@ namespace sepattn {
 
 namespace {
 
-constexpr int kShThreads = 256, kShWaves = 4;         // of the fp32 kernel and of the sum
-constexpr int kShBlock = 32;  // keys per block; slices are whole blocks
+constexpr int kShThreads = 256, kShWaves = 4;  // of the fp32 kernel and of the sum
+constexpr int kShBlock = 32;                   // keys per block; slices are whole blocks
 
 // records of the prefixes' slices, [sequence][head][slice]: max (log2 domain), sum, 2 unused, D unnormalised outputs
 template <int D>
@@ -34,9 +41,9 @@ struct PrefixArgs {
     float *part;
 };
 
-// What a workgroup has to do: chunk `blockIdx.y` of the rows of all prefixes, cut per prefix into chunks of ROWS.
+// A chunk of ROWS rows of one prefix; chunks are numbered over all prefixes.
 struct Chunk {
-    int prefix, row0, rows, first;  // first row of the chunk, rows and first entry in group_seq of the prefix
+    int prefix, row0, rows, first;  // first row of the chunk; rows of the prefix and its first entry in group_seq
 };
 template <int ROWS>
 __device__ inline bool find_chunk(const PrefixArgs &x, int chunk, Chunk &c) {
@@ -195,13 +202,13 @@ __device__ __forceinline__ void add_wave_states(const float *states, const Rows 
 }
 
 // ---- bf16 ------------------------------------------------------------------------------------------
-// One workgroup of eight waves: rows (queries that read one KV head) against a slice of one cache, in blocks of 32 keys.  Operands as in
+// NW waves: rows (queries that read one KV head) against a slice of one cache, in blocks of 32 keys.  Operands as in
 // decode_wide.hip (v_mfma_f32_16x16x32_bf16, the cache rows as A, 16 queries as the columns of B, score tile t's row 4g+i the block's row
 // 8g+4t+i, so that a lane's probabilities are its operand of the second product); a wave has NB such column blocks, for which it
 // reads the cache's fragments from LDS once.
-//   SPLIT_ROWS: four waves have different rows (64 NB per workgroup), and two groups of four take the slice's blocks in turn.  A group
-//     shares a ring of four stages of 32 rows of K and V: three tiles are on their way, one barrier per tile.  (With one group per workgroup a
-//     SIMD has one wave of it, nothing of whose waits is hidden; two workgroups per compute unit leave twice as many records.)
+//   SPLIT_ROWS: four waves have different rows (64 NB per workgroup) and share a ring of four stages of 32 rows of K and V: three tiles are
+//     on their way, one barrier per tile.  NW = 8: two such groups, which take the slice's blocks in turn, so that a SIMD has two waves of one
+//     workgroup and the slices, with their records, are half as many as with two workgroups of four per compute unit.
 //   otherwise: the waves have the same 16 NB rows and take the blocks in turn, each with a stage of its own, whose K half is refilled
 //     as soon as its fragments are in registers and the V half one step later; no barrier in the loop.
 // The groups' or waves' states meet in LDS.
@@ -745,6 +752,8 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void shared_decode_kernel(SharedAr
 // so that a lane's operands are pieces of 16 bytes.  C: column l%16 = query, rows 4 g + i = keys.  Output: O^T += V^T P^T, the k-slots
 // of step i are keys 4 g + i, which the lane group holds.
 // KROPE (own caches): a key is turned by its distance to the query on its way into LDS, by the thread that holds both of a pair.
+// The fp32 matrix rate is a sixteenth of bf16's, and this type is there to check a bf16 run against: 8 sequences of 300 entries behind prefixes of 700
+// (2/1 heads, d = 64) take 10.8 us with the sum, of which 10 are launches and round trips.
 typedef float f4 __attribute__((ext_vector_type(4)));
 constexpr int kFpKeys = 64;
 template <int D>
@@ -887,7 +896,7 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_decode_fp32_kernel(Share
 // WPR waves per (sequence, head), prefix slices first, then the own cache's; wave w takes slices w, w + WPR, ... of both, eight records in one
 // round trip, and the waves' sums are added in wave order.  Nothing but the records has to be read for that (a slice without an entry
 // says so in its own; those of a prefix that the sequence does not have are skipped), so that the kernel is one round trip and its
-// launch: 3 us for a few rows, 5 for 1024 rows of 17 records, 10 for 1536 rows of 49.
+// launch: 3.1 us for a few rows, 4.9 for 1024 rows of 17 records, 7.5 for 1536 rows of 25.
 template <typename T, int D, int WPR>
 __global__ __launch_bounds__(kShThreads) void shared_merge_kernel(sepkv_params p, int n_prefixes, int n_prefix, int n_own,
                                                                   const int32_t *__restrict__ prefix_of, const float *__restrict__ prefix_part,
@@ -975,10 +984,17 @@ struct SharedShape {
     int n_prefix;     // slices per prefix
     int n_own;        // slices per own cache
 };
-// Host estimate in microseconds, from the capacities (the device alone knows how much of them is in use).  `bytes_us`: what reading every cache once
-// takes.  A prefix is cut so finely that a workgroup's walk through its slice, at `step` per 32 keys while the memory is busy, ends
-// well before that, and at least so finely that half of the places that the chip has for workgroups are taken; finer, and a slice more costs a
-// record per row, written and read again.
+// From the capacities (the device alone knows how much of them is in use).  Figures: microseconds of a call, 32/8 heads, d = 128, bf16, without positions
+// unless said; rows: of one KV head and prefix.
+// Rows and waves.  Up to 32 rows every wave has all of them (18 us; cut by rows 18.5: 8 sequences behind 8192 entries); above, each wave its own:
+//     64 rows, 8192 entries                              20.9 (23.5 with all of them in each wave)
+//     192 rows, 65536 entries, 3 / 2 / 1 column blocks    84 / 107 / 108: an entry read from LDS serves more rows
+//     128 rows, 8192 entries,  2 / 1 column blocks        28.9 / 27.5, turned 29.5 / 30.4: slices of few steps, level
+//   NW = 8 where a slice is long and there are many: 192 rows, 65536 entries 84 (4 waves: 87), 128 rows 69 (74); 8192 entries 29 (27.5).
+// Slices.  `bytes_us`: what reading every cache once takes.  A prefix is cut so finely that a workgroup's walk through its slice, at `step` per
+// 32 keys while the memory is busy, ends well before that, and at least so finely that half of the places that the chip has for workgroups
+// are taken; finer, and a slice more costs a record per row, written and read again (192 rows, 65536 entries, 20 / 24 / 28 slices: kernel
+// 95 / 85 / 95; 32 rows of queries on 8192 entries, 8 / 12 / 16: 35 / 29 / 32).
 SharedShape shared_shape(const sepkv_params &p, const sepkv_params &pp, bool rope) {
     SharedShape s = {};
     const long gq = p.Hq / p.Hkv, all = p.S * gq, per_prefix = (all + pp.S - 1) / pp.S, units = compute_units();
@@ -1100,7 +1116,7 @@ int launch_decode_shared(const SharedDecode &x, hipStream_t st) {
             hipLaunchKernelGGL((shared_merge_kernel<T, D, WPR>), grid, block, 0, st, x.p, x.pp.S, s.n_prefix, s.n_own, x.prefix_of, x.part,
                                own_part, static_cast<T *>(x.out), x.lse);
         };
-        // one round trip of one wave where the records are few
+        // one round trip of one wave where the records are few (128 sequences behind 2048 entries: 51.3 us a call, with four waves per row 55.8)
         s.n_prefix + s.n_own <= 8 ? rows(IntC<1>{}) : rows(IntC<kShWaves>{});
     };
     if (x.p.dtype == SEPATTN_BF16) x.p.d == 64 ? go(uint16_t{}, IntC<64>{}) : go(uint16_t{}, IntC<128>{});

@@ -20,6 +20,7 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <climits>
 #include <vector>
 
 #include "sepattn.h"
@@ -596,6 +597,7 @@ const at::Tensor &rows_arg(PyObject *o) {
     if (!t.is_cuda()) fail(PyExc_ValueError, "libsepattn works on GPU tensors only");
     if (t.dim() != 4) fail(PyExc_ValueError, "[B, H, L, d] is expected");
     if (t.size(3) != 1 && t.stride(3) != 1) fail(PyExc_ValueError, "the head dimension must be contiguous");
+    for (const int64_t n : t.sizes()) require(n <= INT_MAX, "sizes of 32 bits are expected");
     return t;
 }
 struct Rows {  // one of q, k, v and what becomes of it
@@ -707,7 +709,7 @@ PyObject *append_rope(PyObject *const *a) {
 // group_sequences(prefix_of, n_prefixes, out)
 PyObject *group_sequences(PyObject *const *a) {
     const at::Tensor &of = dev(a[0]);
-    require(of.scalar_type() == at::kInt && of.dim() == 1, "prefix_of: int32 [S]");
+    require(of.scalar_type() == at::kInt && of.dim() == 1 && of.numel() <= INT_MAX, "prefix_of: int32 [S]");
     const int S = (int)of.numel(), G = as_int(a[1]);
     const Out<2> out(a[2]);
     at::Tensor start, seq;

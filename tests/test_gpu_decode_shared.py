@@ -54,7 +54,7 @@ def blank(x, sizes, a, s, c):
 def turn(x, pos):
     """float64 [..., d] turned by pos [...]; dimension i with i + d/2."""
     h = x.shape[-1] // 2
-    f = BASE ** (-torch.arange(h, dtype=torch.float64) / h)
+    f = BASE ** (-torch.arange(h, dtype=torch.float64, device=pos.device) / h)
     angle = pos.double()[..., None] * f
     u, v = x[..., :h], x[..., h:]
     return torch.cat([u * angle.cos() - v * angle.sin(), v * angle.cos() + u * angle.sin()], -1)
@@ -84,9 +84,9 @@ class Case:
             return sp.sepattn_decode_shared(*args, self.scale, **kw)
         return sp.sepattn_decode_shared_rope(*args, sp.sepkv_rope_table(self.pc + self.c, self.d, BASE, "cuda"), self.scale, **kw)
 
-    def want(self, rope):
+    def want(self, rope, where="cpu"):
         """out, lse, mean of |V| under the weights, largest sum of |q_i k_i| scale over the keys of a row; in float64."""
-        f = lambda t: t.detach().double().cpu()
+        f = lambda t: t.detach().to(where).double()
         out, lse, size, reach = (torch.zeros(self.S, self.Hq, self.d, dtype=torch.float64), torch.full((self.S, self.Hq), float("-inf"), dtype=torch.float64),
                                  torch.zeros(self.S, self.Hq, self.d, dtype=torch.float64), torch.zeros(self.S, self.Hq, dtype=torch.float64))
         for i in range(self.S):
@@ -95,8 +95,8 @@ class Case:
             g = self.of[i]
             shared = slots_of(self.psizes[g], self.pa, self.ps, self.pc) if 0 <= g < self.G else []
             if rope and len(at) + len(shared):
-                K = turn(K, len(shared) + torch.arange(len(at))[None])
-                q = turn(q, torch.tensor(len(shared) + len(at) - 1))
+                K = turn(K, len(shared) + torch.arange(len(at), device=where)[None])
+                q = turn(q, torch.tensor(len(shared) + len(at) - 1, device=where))
             if shared:
                 K, V = torch.cat([f(self.Kp[g][:, shared]), K], 1), torch.cat([f(self.Vp[g][:, shared]), V], 1)
             if K.shape[1] == 0:
@@ -282,3 +282,81 @@ def test_in_a_graph(sp, rope):
         for q, out in zip((case.q, q2), outs):
             want = call(q)
             assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1])
+
+
+@pytest.mark.parametrize("rope", [False, True])
+@pytest.mark.parametrize("S,own_n,prompt_n,of", [
+    (13, [40, 1], [33100], [0]),                 # 104 rows of a KV head
+    (24, [40, 0, 33], [33333], [0]),             # 192
+    (24, [40], [31], [0]),                       # nearly every slice is empty
+    (40, [7, 40], [33333, 1500, 0], [0, 1, 0, 2, 0, -1])])
+def test_many_slices(sp, S, own_n, prompt_n, of, rope):
+    case = Case(S, 8, 1, 128, "bf16", SMALL, (4, 700, 64, 33333), own_n, prompt_n, of, seed=S)
+    out, lse = case.run(sp, rope)
+    case.check(out, lse, rope, tuple(t.cpu() for t in case.want(rope, "cuda")))
+
+
+@pytest.mark.parametrize("S,Hq,Hkv,G", [(1500, 2, 1, 3000), (2047, 32, 4, 2), (65535, 1, 1, 1)])
+def test_many_sequences_and_prompts(sp, S, Hq, Hkv, G):
+    """As many rows and prompts as the calls take; a few of the sequences are looked at."""
+    case = Case(min(S, 64), Hq, Hkv, 64, "bf16", (1, 1, 1, 4), (0, 0, 1, 3), [0, 1, 4], [3, 0, 2], [0], seed=5)
+    at = sorted({(i * 997) % S for i in range(64)} | {0, S - 1})[: case.S]
+    small, (K, V, Kp, Vp) = case, (case.Kc, case.Vc, case.Kp, case.Vp)
+    full = Case.__new__(Case)
+    full.__dict__.update(small.__dict__)
+    index = torch.zeros(S, dtype=torch.long, device="cuda")
+    index[at] = torch.arange(len(at), device="cuda")
+    which = torch.arange(G, device="cuda") % 3
+    full.S, full.G = S, G
+    full.q, full.Kc, full.Vc, full.sz = small.q[index], K[index], V[index], small.sz[index]
+    full.Kp, full.Vp, full.psz = Kp[which], Vp[which], small.psz[which]
+    full.prefix_of = ((torch.arange(S, device="cuda") * 7) % (G + 1)).to(torch.int32)  # G: none
+    out, lse = full.run(sp, False)
+    small.S, small.G = len(at), G
+    small.q, small.Kc, small.Vc = full.q[at], full.Kc[at], full.Vc[at]
+    small.sizes = [full.sz[i].tolist() for i in at]
+    small.Kp, small.Vp, small.psizes = full.Kp, full.Vp, full.psz.tolist()
+    small.of = full.prefix_of[at].tolist()
+    small.check(out[at], lse[at], False)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_slots_far_apart(sp, dtype):
+    """The longest caches that are taken (rows up to 2^32 bytes into a head), entries in their last and first slots."""
+    c = (2 ** 32 - 1) // (4 * 128)
+    case = Case(2, 4, 1, 128, dtype, SMALL, SMALL, [40, 37], [40], [0], seed=3)
+    a, s, w, small = SMALL
+    room = c - a - s
+    rows = [[3, 5, 10, 6, 7, room - 9], [0, 8, 20, 6, 1, room - 1]]
+
+    def spread(x, sizes):
+        big = torch.full((x.shape[0], 1, c, 128), float("nan"), dtype=x.dtype, device="cuda")
+        for i, row in enumerate(sizes):
+            at = slots_of(row, a, s, c)
+            big[i][:, at] = randn(1, len(at), 128, dtype=x.dtype, seed=11 + i)
+        return big
+
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    case.c = case.pc = c
+    case.sizes, case.psizes = rows, rows[:1]
+    case.sz, case.psz = i32(rows), i32(rows[:1])
+    case.Kc, case.Vc, case.Kp, case.Vp = spread(case.Kc, rows), spread(case.Vc, rows), spread(case.Kp, rows[:1]), spread(case.Vp, rows[:1])
+    for rope in (False, True):
+        out, lse = case.run(sp, rope)
+        case.check(out, lse, rope)
+
+
+def test_two_streams(sp):
+    """Calls on two streams at once, a workspace each."""
+    cases = [Case(6, 16, 2, 128, "bf16", SMALL, (0, 0, 1, 4000), [40, 3], [4000], [0], seed=i) for i in (1, 2)]
+    want = [c.run(sp, True) for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(5):
+        for c, st in zip(cases, streams):
+            with torch.cuda.stream(st):
+                got.append(c.run(sp, True))
+    torch.cuda.synchronize()
+    for i, (out, lse) in enumerate(got):
+        assert torch.equal(out, want[i % 2][0]) and torch.equal(lse, want[i % 2][1])

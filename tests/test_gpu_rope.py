@@ -313,3 +313,43 @@ def test_step_in_a_graph(sp):
         assert torch.equal(replayed, out)
         for x, y in zip(state, other):
             assert torch.equal(x, y)
+
+
+def test_rows_far_apart(sp):
+    """Strides whose offsets pass 2^32 bytes, on both sides."""
+    far = 2 ** 31 + 64
+    x, y = (torch.empty(far + 2 ** 30 + 4096, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    view = lambda t: t.as_strided((2, 2, 5, 64), (far, 2 ** 30, 192, 1))
+    q = randn(2, 2, 5, 64, dtype=torch.bfloat16)
+    freqs = sp.sepattn_rope_frequencies(64, 10000.0, device="cuda")
+    view(x).copy_(q)
+    for fn in (sp.sepattn_rope, sp.sepattn_rope_backward):
+        want = fn(q, q, q, freqs)
+        y.fill_(7.0)
+        k, v = torch.empty_like(q), torch.empty_like(q)
+        fn(view(x), q, q, freqs, out=(view(y), k, v))
+        assert torch.equal(view(y), want[0]) and torch.equal(k, want[1]) and torch.equal(v, q)
+        assert int((y == 7.0).sum()) == y.numel() - q.numel()
+
+
+def test_sizes_past_32_bits_are_refused(sp):
+    freqs = sp.sepattn_rope_frequencies(64, 10000.0, device="cuda")
+    q = torch.zeros(1, 1, 1, 64, dtype=torch.bfloat16, device="cuda").expand(1, 1, 2 ** 32 + 5, 64)
+    with pytest.raises(AssertionError):
+        sp.sepattn_rope(q, q, None, freqs, out=(q, q, None))
+
+
+def test_two_streams(sp):
+    freqs = sp.sepattn_rope_frequencies(128, 10000.0, device="cuda")
+    src = [[randn(1, h, 777, 128, dtype=torch.bfloat16, seed=h + i) for h in (8, 2, 2)] for i in (0, 1)]
+    want = [sp.sepattn_rope(*x, freqs) for x in src]
+    streams = [torch.cuda.Stream() for _ in src]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(4):
+        for x, st in zip(src, streams):
+            with torch.cuda.stream(st):
+                got.append(sp.sepattn_rope(*x, freqs))
+    torch.cuda.synchronize()
+    for i, out in enumerate(got):
+        assert all(torch.equal(a, b) for a, b in zip(out, want[i % 2]))

@@ -9,8 +9,8 @@
 // What it cannot do without is to read every cache once, and 4 d operations per (query head, entry): with R rows on a KV head an entry's 4 d
 // bytes feed 4 d R operations, so that from about 260 rows on the matrix units would bound it, below that the memory.
 // Measured, 32/8 heads, d = 128, bf16, microseconds of the first launch + the second (bytes of the caches at the rate of a large copy):
-//   2 sequences behind 300 entries                                6.4 + 3.1 (1.2; launches and round trips)
-//   32 sequences, 16 KV rows each, behind 8192 entries, turned   25 + 4.9 (18.7; 2.9 TB/s over both)
+//   2 sequences behind 600 entries                                6.4 + 3.1 (1.2; launches and round trips)
+//   32 sequences behind 8192 entries, 128 rows per KV head, turned  25.5 + 4.4 (18.7; 3.1 TB/s over both)
 //   48 sequences, 1 prefix of 65536, 192 rows per KV head        78 + 7.5 (72; 4.2 TB/s, 610 TFLOP/s)
 // (In one launch, the last slice of a row adding its records: 12.8 instead of 9.5 for the first; four round trips past the L2 in sequence.)
 #include "common.h"
@@ -989,12 +989,14 @@ struct SharedShape {
 // Rows and waves.  Up to 32 rows every wave has all of them (18 us; cut by rows 18.5: 8 sequences behind 8192 entries); above, each wave its own:
 //     64 rows, 8192 entries                              20.9 (23.5 with all of them in each wave)
 //     192 rows, 65536 entries, 3 / 2 / 1 column blocks    84 / 107 / 108: an entry read from LDS serves more rows
-//     128 rows, 8192 entries,  2 / 1 column blocks        28.9 / 27.5, turned 29.5 / 30.4: slices of few steps, level
+//     128 rows, 8192 entries,  2 / 1 column blocks        29.6 / 27.2, turned 31.7 / 29.9: slices of fewer than 20 steps
 //   NW = 8 where a slice is long and there are many: 192 rows, 65536 entries 84 (4 waves: 87), 128 rows 69 (74); 8192 entries 29 (27.5).
 // Slices.  `bytes_us`: what reading every cache once takes.  A prefix is cut so finely that a workgroup's walk through its slice, at `step` per
 // 32 keys while the memory is busy, ends well before that, and at least so finely that half of the places that the chip has for workgroups
 // are taken; finer, and a slice more costs a record per row, written and read again (192 rows, 65536 entries, 20 / 24 / 28 slices: kernel
-// 95 / 85 / 95; 32 rows of queries on 8192 entries, 8 / 12 / 16: 35 / 29 / 32).
+// 95 / 85 / 95; 128 rows, 8192 entries, turned, 8 / 12 / 16 of one column block: 32.0 / 30.0 / 30.9).  Turned queries, whose scores are two products, take
+// longer per step, but so do the own caches beside them, and fewer slices pay: 96 rows, 20000 entries 35.0 (steps of 0.95 and 1.1: 39.6), 400
+// rows, 4096 entries 52.1 (56.7).
 SharedShape shared_shape(const sepkv_params &p, const sepkv_params &pp, bool rope) {
     SharedShape s = {};
     const long gq = p.Hq / p.Hkv, all = p.S * gq, per_prefix = (all + pp.S - 1) / pp.S, units = compute_units();
@@ -1023,14 +1025,14 @@ SharedShape shared_shape(const sepkv_params &p, const sepkv_params &pp, bool rop
         s.n_prefix = cut(s.nb == 1 ? 0.35 : 0.45);
     } else {
         s.split_rows = true;
-        static const double step[2][3] = {{0.75, 0.85, 1.05}, {0.95, 1.1, 0.}};
+        static const double step[2][3] = {{0.75, 0.85, 1.05}, {0.7, 0.9, 0.}};
         s.nb = per_prefix <= 64 ? 1 : per_prefix <= 128 ? 2 : 3;
         // three column blocks where they waste no more rows than two (turned queries at d = 128 have no registers for them)
         if (s.nb == 3 && ((rope && p.d == 128) || (per_prefix + 191) / 192 * 3 > (per_prefix + 127) / 128 * 2)) s.nb = 2;
         for (;; --s.nb) {  // fewer rows per workgroup, and more workgroups, where a slice would be a few steps and there is room
             s.chunks = (int)chunks_of(64 * s.nb);
             s.n_prefix = cut(step[rope && p.d == 128][s.nb - 1]);
-            if (s.nb == 1 || nb / s.n_prefix >= 16 || own_groups + (long)p.Hkv * ((all + 64 * s.nb - 1) / (64 * s.nb)) * s.n_prefix >= slots) break;
+            if (s.nb == 1 || nb / s.n_prefix >= 20 || own_groups + (long)p.Hkv * ((all + 64 * s.nb - 1) / (64 * s.nb)) * s.n_prefix >= slots) break;
         }
         if (p.d == 128 && !rope && s.nb > 1 && s.n_prefix >= 24) {
             s.waves = 8;

@@ -475,6 +475,7 @@ int sepkv_fill_from_prefill_zeroed(const sepkv_params *p, int L, int nw, const v
  *   ws           DEVICE, >= sepattn_decode_shared_workspace_bytes(p, pp) bytes, 256-byte aligned; may hold anything.
  *                Calls that overlap in time need a workspace each
  * A sequence without any entry, own or of a prefix, yields out = 0, lse = -inf.
+ * Infinities and NaN in q, in a cache or in a prefix reach the results of the sequences that see them, and no others.
  *
  * sepattn_decode_shared_rope: with positions within the caches (see sepattn_decode_rope): the entries of a sequence's prefix,
  * oldest first, are at positions 0 .. np-1, its own at np .. np+nv-1, the query at np+nv-1.  The positions of a

@@ -177,6 +177,8 @@ __device__ __forceinline__ bool own_work(const SharedArgs &a, int id, SliceWork<
     w.K = static_cast<const T *>(a.Kc) + head0, w.V = static_cast<const T *>(a.Vc) + head0;
     return true;
 }
+// What to subtract in the exponent for a maximum: a row none of whose scores is above minus infinity has weights 0, not NaN.
+__device__ inline float base_of(float m) { return m == -INFINITY ? 0.f : m; }
 // The states of NW waves that had the same 16 rows, [wave][row][record] in LDS, added in wave order and written; two columns per thread.
 template <int D, int NW, typename Rows>
 __device__ __forceinline__ void add_wave_states(const float *states, const Rows &rows, int block) {
@@ -188,10 +190,11 @@ __device__ __forceinline__ void add_wave_states(const float *states, const Rows 
         float M = -INFINITY, lsum = 0.f, o0 = 0.f, o1 = 0.f;
 #pragma unroll
         for (int w = 0; w < NW; ++w) M = fmaxf(M, states[(w * 16 + row) * REC]);
+        const float base = base_of(M);
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
             const float *x = states + (w * 16 + row) * REC;
-            const float wgt = __builtin_amdgcn_exp2f(x[0] - M);  // M is finite: the slice has an entry
+            const float wgt = __builtin_amdgcn_exp2f(x[0] - base);
             lsum = fmaf(wgt, x[1], lsum);
             o0 = fmaf(wgt, x[4 + 2 * c2], o0);
             o1 = fmaf(wgt, x[5 + 2 * c2], o1);
@@ -412,13 +415,15 @@ __device__ __forceinline__ void shared_body(const CacheMap &cm, const uint16_t *
         float m = s[0][0];
 #pragma unroll
         for (int i = 1; i < 8; ++i) m = fmaxf(m, s[i >> 2][i & 3]);
-        m = fmaxf(m_run[nb], groups_max(m) * sl2);  // finite: row 0 of a block is valid
-        const float alpha = __builtin_amdgcn_exp2f(m_run[nb] - m);
-        m_run[nb] = m;
+        m = fmaxf(m_run[nb], groups_max(m) * sl2);
+        const float base = base_of(m), alpha = __builtin_amdgcn_exp2f(m_run[nb] - base);
+        m_run[nb] = base;
         l_run[nb] *= alpha;
 #pragma unroll
         for (int db = 0; db < DB; ++db) oacc[nb][db] *= alpha;
-        return exponentials(s, nb, p);
+        const float psum = exponentials(s, nb, p), all = groups_sum(psum);
+        if (m == -INFINITY && all == all) m_run[nb] = m;  // no score above minus infinity; if they were NaN the sums are now, and the record counts
+        return psum;
     };
 
     if constexpr (SPLIT_ROWS) {
@@ -564,8 +569,8 @@ __device__ __forceinline__ void shared_body(const CacheMap &cm, const uint16_t *
             }
             const float *r = red + nb * 16 * REC;
             const float2 ml = *reinterpret_cast<const float2 *>(r);
-            const float M = fmaxf(m_run[nb], ml.x);  // finite: the slice's first block is this group's
-            const float mine = __builtin_amdgcn_exp2f(m_run[nb] - M), other = __builtin_amdgcn_exp2f(ml.x - M);
+            const float M = fmaxf(m_run[nb], ml.x), base = base_of(M);
+            const float mine = __builtin_amdgcn_exp2f(m_run[nb] - base), other = __builtin_amdgcn_exp2f(ml.x - base);
             if (g == 0) *reinterpret_cast<float2 *>(to) = float2{M, fmaf(other, ml.y, mine * l_run[nb])};
 #pragma unroll
             for (int db = 0; db < DB; ++db) {
@@ -840,15 +845,17 @@ __device__ __forceinline__ void shared_fp32_body(const CacheMap &cm, const float
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) s[i] = 4 * g + i < n_valid ? s[i] * sl2 : -INFINITY;
-            const float m_new = fmaxf(m, groups_max(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]))));  // finite: key 0 of the block is valid
-            const float alpha = exp2f(m - m_new);
-            m = m_new;
-            l *= alpha;
+            const float m_new = fmaxf(m, groups_max(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]))));
+            const float base = base_of(m_new), alpha = exp2f(m - base);
+            float sum = 0.f;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                s[i] = exp2f(s[i] - m);
-                l += s[i];
+                s[i] = exp2f(s[i] - base);
+                sum += s[i];
             }
+            m = m_new;
+            if (m_new == -INFINITY) m = groups_sum(sum) == 0.f ? m_new : base;  // scores that are NaN: the sums are now, and the record counts
+            l = l * alpha + sum;
 #pragma unroll
             for (int db = 0; db < D / 16; ++db) {
                 o[db] *= alpha;
@@ -946,10 +953,10 @@ __global__ __launch_bounds__(kShThreads) void shared_merge_kernel(sepkv_params p
         }
     }
     auto write = [&](int c, float v, float lsum) {
-        v = lsum > 0.f ? v / lsum : 0.f;
+        v = lsum == 0.f ? 0.f : v / lsum;  // (NaN stays NaN)
         if constexpr (sizeof(T) == 2) out[row * D + c] = decode_f32_to_bf16(v);
         else out[row * D + c] = v;
-        if (lse && c == 0) lse[row] = lsum > 0.f ? (M + log2f(lsum)) * kLn2_f : -INFINITY;
+        if (lse && c == 0) lse[row] = lsum == 0.f ? -INFINITY : (M + log2f(lsum)) * kLn2_f;
     };
     if constexpr (WPR == 1) {
 #pragma unroll

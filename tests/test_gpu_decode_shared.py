@@ -360,3 +360,41 @@ def test_two_streams(sp):
     torch.cuda.synchronize()
     for i, (out, lse) in enumerate(got):
         assert torch.equal(out, want[i % 2][0]) and torch.equal(lse, want[i % 2][1])
+
+
+@pytest.mark.parametrize("rope", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_values_not_finite_stay_with_the_sequences_that_see_them(sp, dtype, rope, value):
+    """A query, an own value, a prefix's value: other sequences, also of the same prefix and product, are as accurate as without."""
+    case = Case(23, 8, 2, 64, dtype, SMALL, (4, 30, 20, 600), [40, 7, 30], [555, 90], [0, 1, 0, -1], seed=8)
+    want = case.want(rope)
+    clean = case.run(sp, rope)
+    case.q[4, 3, 5] = value                                                            # sequence 4 shares prefix 0
+    case.Vc[2, :, slots_of(case.sizes[2], case.a, case.s, case.c)[3], 7] = value       # sequence 2: prefix 0
+    for hit in (lambda i: i in (2, 4), lambda i: i in (2, 4) or case.of[i] == 1):
+        out, lse = case.run(sp, rope)
+        rows = [i for i in range(case.S) if hit(i)]
+        assert all(not out[i].isfinite().all() for i in rows)
+        out[rows], lse[rows] = clean[0][rows], clean[1][rows]
+        case.check(out, lse, rope, want)
+        case.Vp[1, :, slots_of(case.psizes[1], case.pa, case.ps, case.pc)[50]] = value  # everyone's behind prefix 1
+
+
+@pytest.mark.parametrize("S", [3, 20])  # a wave has all rows, or its own
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_scores_of_minus_infinity(sp, dtype, S):
+    """Entries whose scores are minus infinity count with weight 0, whole blocks and slices of them, and in front of the others."""
+    case = Case(S, 8, 2, 64, dtype, SMALL, (0, 0, 1, 700), [40, 7, 0], [700], [0], seed=S)
+    case.q[:, :, 0] = 1.0
+    case.psizes = [[0, 0, 699, 1, 0, 0]]
+    case.psz = torch.tensor(case.psizes, dtype=torch.int32, device="cuda")
+    case.Kp[:, :, :300, 0] = float("-inf")
+    got = case.run(sp, False)
+    case.psizes = [[0, 0, 399, 1, 0, 300]]
+    want = case.want(False)
+    case.check(*got, False, want)
+    case.Kp[:, :, :, 0] = float("-inf")
+    out, lse = case.run(sp, False)
+    case.of = [-1] * S
+    case.check(out, lse, False)

@@ -757,8 +757,8 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void shared_decode_kernel(SharedAr
 // so that a lane's operands are pieces of 16 bytes.  C: column l%16 = query, rows 4 g + i = keys.  Output: O^T += V^T P^T, the k-slots
 // of step i are keys 4 g + i, which the lane group holds.
 // KROPE (own caches): a key is turned by its distance to the query on its way into LDS, by the thread that holds both of a pair.
-// The fp32 matrix rate is a sixteenth of bf16's, and this type is there to check a bf16 run against: 8 sequences of 300 entries behind prefixes of 700
-// (2/1 heads, d = 64) take 10.8 us with the sum, of which 10 are launches and round trips.
+// The fp32 matrix rate is a sixteenth of bf16's, and this type is there to check a bf16 run against: 11 sequences of up to 150 entries behind three prefixes
+// of up to 250 (12/12 heads, d = 64, turned) take 9.0 us and 3.2 for the sum, most of it launches and round trips (bytes: 2.2).
 typedef float f4 __attribute__((ext_vector_type(4)));
 constexpr int kFpKeys = 64;
 template <int D>

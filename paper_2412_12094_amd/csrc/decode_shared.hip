@@ -9,9 +9,9 @@
 // What it cannot do without is to read every cache once, and 4 d operations per (query head, entry): with R rows on a KV head an entry's 4 d
 // bytes feed 4 d R operations, so that from about 260 rows on the matrix units would bound it, below that the memory.
 // Measured, 32/8 heads, d = 128, bf16, microseconds of the first launch + the second (bytes of the caches at the rate of a large copy):
-//   2 sequences behind 600 entries                                6.4 + 3.1 (1.2; launches and round trips)
-//   32 sequences behind 8192 entries, 128 rows per KV head, turned  25.5 + 4.4 (18.7; 3.1 TB/s over both)
-//   48 sequences, 1 prefix of 65536, 192 rows per KV head        78 + 7.5 (72; 4.2 TB/s, 610 TFLOP/s)
+//   2 sequences behind 600 entries                                   6.4 + 3.3 (1.2; launches and round trips)
+//   32 sequences behind 8192 entries, 128 rows per KV head, turned  26 + 4.6 (18.7; 3.0 TB/s over both)
+//   48 sequences behind 65536 entries, 192 rows per KV head          80 + 7.0 (72; 4.1 TB/s, 600 TFLOP/s)
 // (In one launch, the last slice of a row adding its records: 12.8 instead of 9.5 for the first; four round trips past the L2 in sequence.)
 #include "common.h"
 #include "decode_common.h"
@@ -214,7 +214,8 @@ __device__ __forceinline__ void add_wave_states(const float *states, const Rows 
 //     workgroup and the slices, with their records, are half as many as with two workgroups of four per compute unit.
 //   otherwise: the waves have the same 16 NB rows and take the blocks in turn, each with a stage of its own, whose K half is refilled
 //     as soon as its fragments are in registers and the V half one step later; no barrier in the loop.
-// The groups' or waves' states meet in LDS.
+// The groups' or waves' states meet in LDS.  The weights are rounded to bf16 for the second product (2^-9 of each at most, as in every bf16 kernel
+// here: an fp32 product has a sixteenth of the rate); their sum is formed from the unrounded ones.
 // KROPE (own caches): keys are turned by their distance to the query, as in decode_wide.hip.  LO (prefixes): the query is turned by its
 // position.  Either is then the sum of two bf16 numbers, 16 bits of mantissa, and the scores are two products: rounded to one
 // number, lse would be off by 1e-3.

@@ -214,7 +214,7 @@ __device__ __forceinline__ void add_wave_states(const float *states, const Rows 
 //     workgroup and the slices, with their records, are half as many as with two workgroups of four per compute unit.
 //   otherwise: the waves have the same 16 NB rows and take the blocks in turn, each with a stage of its own, whose K half is refilled
 //     as soon as its fragments are in registers and the V half one step later; no barrier in the loop.
-// The groups' or waves' states meet in LDS.  The weights are rounded to bf16 for the second product (2^-9 of each at most, as in every bf16 kernel
+// The groups' or waves' states meet in LDS.  The weights are rounded to bf16 for the second product (2^-8 of each at most, as in every bf16 kernel
 // here: an fp32 product has a sixteenth of the rate); their sum is formed from the unrounded ones.
 // KROPE (own caches): keys are turned by their distance to the query, as in decode_wide.hip.  LO (prefixes): the query is turned by its
 // position.  Either is then the sum of two bf16 numbers, 16 bits of mantissa, and the scores are two products: rounded to one

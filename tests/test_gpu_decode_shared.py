@@ -111,7 +111,7 @@ class Case:
     def check(self, out, lse, rope, want=None):
         ref, ref_lse, size, reach = want or self.want(rope)
         # a score: d products added in fp32 (each sum off by 2^-24 of what it holds, at most d of them), and scaled; with positions the angles'
-        # 2^-20 and, in bf16, turned values of 16 bits (2^-17 each for key and query)
+        # 2^-20 and, in bf16, the turned one of key and query as two numbers (2^-8 of 2^-8)
         score = reach * (self.d * 2.0 ** -24 + 2.0 ** -21 + (2.0 ** -20 + (2.0 ** -16 if self.dt == torch.bfloat16 else 0.0) if rope else 0.0))
         none = torch.isinf(ref_lse)
         got = lse.double().cpu()

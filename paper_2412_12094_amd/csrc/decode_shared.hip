@@ -412,6 +412,20 @@ __device__ __forceinline__ void shared_body(const CacheMap &cm, const uint16_t *
 #pragma unroll
         for (int i = 0; i < 8; ++i) s[i >> 2][i & 3] = 8 * g + i < n_valid ? s[i >> 2][i & 3] : -INFINITY;
     };
+    // Rows past the end repeat the last entry's: its weight there is 0, but an infinite value times 0 would be NaN, so their values count as zeros:
+    // fragments, or, in front of them, the stage's rows (every wave that reads it clears them before its own reads)
+    auto clear_tail = [&](bf16x8 (&va)[DB], int n_valid) __attribute__((always_inline)) {
+        u32x4 keep;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) keep[i] = (8 * g + 2 * i < n_valid ? 0xFFFFu : 0u) | (8 * g + 2 * i + 1 < n_valid ? 0xFFFF0000u : 0u);
+#pragma unroll
+        for (int db = 0; db < DB; ++db) va[db] = as_bf16x8(__builtin_bit_cast(u32x4, va[db]) & keep);
+    };
+    auto clear_rows = [&](uint32_t stage, int n_valid) __attribute__((always_inline)) {
+#pragma unroll 1
+        for (int chunk = n_valid * CH + lane; chunk < kShBlock * CH; chunk += 64) lds_write_b128_at(stage + chunk * 16, f32x4{0.f, 0.f, 0.f, 0.f});
+        wait_lds();
+    };
     auto raise = [&](const f32x4 (&s)[2], int nb, f32x8 &p) __attribute__((always_inline)) {
         float m = s[0][0];
 #pragma unroll
@@ -499,14 +513,26 @@ __device__ __forceinline__ void shared_body(const CacheMap &cm, const uint16_t *
                             if constexpr (LO) s[nb][t] = mfma16(ka[t][ks], qlo[nb][ks], s[nb][t]);
                         }
                 });
+                auto tail = [&]() __attribute__((always_inline)) {
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) mask_tail(s[nb], n_valid);
+                };
+                if constexpr (!EARLY_V) {
+                    if (n_valid < kShBlock) {
+                        tail();
+                        clear_rows(v_at, n_valid);
+                    }
+                }
                 bf16x8 va[DB];
 #pragma unroll
                 for (int db = 0; db < (EARLY_V ? DB : EARLY); ++db) va[db] = value_fragment(v_at, db);
                 if constexpr (AHEAD) read_keys(i + 1);
                 if constexpr (!EARLY_V) __builtin_amdgcn_sched_barrier(0);
-                if (n_valid < kShBlock) {
-#pragma unroll
-                    for (int nb = 0; nb < NB; ++nb) mask_tail(s[nb], n_valid);
+                if constexpr (EARLY_V) {
+                    if (n_valid < kShBlock) {
+                        tail();
+                        clear_tail(va, n_valid);
+                    }
                 }
                 f32x8 p[NB];
                 float psum[NB];
@@ -699,11 +725,15 @@ __device__ __forceinline__ void shared_body(const CacheMap &cm, const uint16_t *
                 wait_lds();
                 load_rows(Vh, at, vs_);
             }
+            if (n_valid < kShBlock) {
+                clear_tail(va, n_valid);
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) mask_tail(s[nb], n_valid);
+            }
             bf16x8 pb[NB];
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
                 f32x8 p;
-                if (n_valid < kShBlock) mask_tail(s[nb], n_valid);
                 float psum = exponentials(s[nb], nb, p);
                 if (__builtin_amdgcn_ballot_w64(!(psum <= kMost)) != 0ull) psum = raise(s[nb], nb, p);
                 l_run[nb] += psum;
@@ -807,10 +837,11 @@ __device__ __forceinline__ void shared_fp32_body(const CacheMap &cm, const float
             }
         }
     };
-    auto stage = [&]() __attribute__((always_inline)) {
+    auto stage = [&](int eb) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
             const int item = threadIdx.x + i * kShThreads, at = item / (D / 8) * PITCH + item % (D / 8) * 4;
+            if (eb + item / (D / 8) >= e1) vr[i][0] = vr[i][1] = f4{0.f, 0.f, 0.f, 0.f};  // (0 times an infinity of the last entry, which is there, would be NaN)
             f4 x = kr[i][0], y = kr[i][1];
             if constexpr (KROPE) {  // R(-distance)
                 x = kr[i][0] * cs[i] + kr[i][1] * sn[i];
@@ -829,7 +860,7 @@ __device__ __forceinline__ void shared_fp32_body(const CacheMap &cm, const float
     fetch(e0);
     for (int eb = e0; eb < e1; eb += kFpKeys) {
         __syncthreads();
-        stage();
+        stage(eb);
         __syncthreads();
         if (eb + kFpKeys < e1) fetch(eb + kFpKeys);
 #pragma unroll 1

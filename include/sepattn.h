@@ -475,6 +475,8 @@ int sepkv_fill_from_prefill_zeroed(const sepkv_params *p, int L, int nw, const v
  *   ws           DEVICE, >= sepattn_decode_shared_workspace_bytes(p, pp) bytes, 256-byte aligned; may hold anything.
  *                Calls that overlap in time need a workspace each
  * A sequence without any entry, own or of a prefix, yields out = 0, lse = -inf.
+ * bf16: the weights that meet V have 15 bits or more for own caches, and for prefixes up to 32 rows of a KV head (S Hq / (G Hkv)); above, those of
+ * prefixes are rounded to bf16, as in sepattn_decode.
  * Infinities and NaN in q, in a cache or in a prefix reach the results of the sequences that see them, and no others.
  *
  * sepattn_decode_shared_rope: with positions within the caches (see sepattn_decode_rope): the entries of a sequence's prefix,

@@ -214,8 +214,12 @@ __device__ __forceinline__ void add_wave_states(const float *states, const Rows 
 //     workgroup and the slices, with their records, are half as many as with two workgroups of four per compute unit.
 //   otherwise: the waves have the same 16 NB rows and take the blocks in turn, each with a stage of its own, whose K half is refilled
 //     as soon as its fragments are in registers and the V half one step later; no barrier in the loop.
-// The groups' or waves' states meet in LDS.  The weights are rounded to bf16 for the second product (2^-8 of each at most, as in every bf16 kernel
-// here: an fp32 product has a sixteenth of the rate); their sum is formed from the unrounded ones.
+// The groups' or waves' states meet in LDS.
+// Weights.  Their sum is formed in fp32 from the weights as they are.  For the second product they are the sum of two bf16 numbers (15 bits or more) where the
+// waves share their rows: the product of the second ones finds room there (2 sequences behind 600 entries 9.4 us, with one number 9.4; 32 rows, 8192
+// entries 18.7 and 18.4, 32768 entries 32.2 and 32.0).  SPLIT_ROWS: one bf16 number, 2^-8 of it at most, as in the other bf16 kernels, since there the second
+// product is paid for in full (128 rows, 8192 entries 28.1 and 27.0, turned 31.0 and 29.7; 192 rows, 65536 entries 104 and 85, turned 144 and 122).  The
+// output's distance to 64 bits is 1.66e-3 of its size with two numbers (its own rounding) and 2.35e-3 with one.
 // KROPE (own caches): keys are turned by their distance to the query, as in decode_wide.hip.  LO (prefixes): the query is turned by its
 // position.  Either is then the sum of two bf16 numbers, 16 bits of mantissa, and the scores are two products: rounded to one
 // number, lse would be off by 1e-3.
@@ -280,6 +284,25 @@ __device__ inline void run_of(const CacheMap &m, int e, int &slot, int &end) {
 __device__ inline void split_hi_lo(const f32x8 &x, bf16x8 &hi, bf16x8 &lo) {
     hi = __builtin_convertvector(x, bf16x8);
     lo = __builtin_convertvector(x - __builtin_convertvector(hi, f32x8), bf16x8);
+}
+
+// Weights as the sum of two bf16 numbers.  The first is the last one below the weight, so that the second is positive as well and an infinite
+// value times either has the same sign.
+__device__ inline void split_weights(const f32x8 &p, bf16x8 &hi, bf16x8 &lo) {
+    f32x8 rest;
+    u32x4 first;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t below[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            below[j] = __builtin_elementwise_sub_sat(__float_as_uint(p[2 * i + j]), 1u);
+            rest[2 * i + j] = p[2 * i + j] - __uint_as_float(below[j] & 0xFFFF0000u);
+        }
+        first[i] = __builtin_amdgcn_perm(below[1], below[0], 0x07060302u);
+    }
+    hi = as_bf16x8(first);
+    lo = __builtin_convertvector(rest, bf16x8);
 }
 
 // rows: SliceRow of (column block, column)
@@ -730,19 +753,23 @@ __device__ __forceinline__ void shared_body(const CacheMap &cm, const uint16_t *
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) mask_tail(s[nb], n_valid);
             }
-            bf16x8 pb[NB];
+            bf16x8 pb[NB], pl[NB];
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
                 f32x8 p;
                 float psum = exponentials(s[nb], nb, p);
                 if (__builtin_amdgcn_ballot_w64(!(psum <= kMost)) != 0ull) psum = raise(s[nb], nb, p);
                 l_run[nb] += psum;
-                pb[nb] = __builtin_convertvector(p, bf16x8);
+                split_weights(p, pb[nb], pl[nb]);
             }
 #pragma unroll
             for (int db = 0; db < DB; ++db)
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) oacc[nb][db] = mfma16(va[db], pb[nb], oacc[nb][db]);
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) oacc[nb][db] = mfma16(va[db], pl[nb], oacc[nb][db]);
         }
         // ---- the waves' states meet in LDS, one column block after the other; a thread adds two columns of a row
         constexpr int REC = kShRecord<D>;

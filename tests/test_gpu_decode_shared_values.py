@@ -33,3 +33,18 @@ def test_infinite_values(sp, S, Hq, Hkv, d, n, own_n, dtype, rope, where):  # no
         for i in rows:
             out[i, :, column] = clean[0][i, :, column]
     case.check(out, lse, rope, want)
+
+
+@pytest.mark.parametrize("rope", [False, True])
+@pytest.mark.parametrize("S,Hq,Hkv,d,n,own_n", [
+    (1, 1, 1, 64, 300, [40]), (2, 32, 8, 128, 600, [40, 1]), (8, 8, 2, 128, 700, [40, 33, 0]), (4, 32, 4, 64, 2500, [17]), (3, 8, 2, 64, 0, [40, 39, 2])])
+def test_weights_of_16_bits(sp, S, Hq, Hkv, d, n, own_n, rope):  # noqa: F811
+    """Up to 32 rows of a KV head, and in own caches: a weight is the sum of two bf16 numbers.  The first is off by 2^-7 of it at most (the last one
+    below), the second, which is rounded, by 2^-8 of that.  The rest of the bound: Case.check."""
+    case = Case(S, Hq, Hkv, d, "bf16", SMALL, (0, 0, 1, 2600), own_n, [n], [0], seed=S + d)
+    out, lse = case.run(sp, rope)
+    ref, _, size, reach = case.want(rope)
+    score = reach * (d * 2.0 ** -24 + 2.0 ** -21 + (2.0 ** -20 + 2.0 ** -16 if rope else 0.0))
+    err = (out.double().cpu() - ref).abs()
+    bound = 2.0 ** -8 * ref.abs() + (2.0 ** -15 + 2.0 * score[..., None] + 2.0 ** -18) * size
+    assert (err <= bound).all(), float((err / bound).max())

@@ -653,7 +653,11 @@ int sepkv_rope_cache(const sepkv_params *p, const int32_t *sizes, const float *r
 // own and prefix caches of one call
 static int check_shared(const sepkv_params *p, const sepkv_params *pp) {
     int rc = check_kv(p);
-    if (rc == SEPATTN_OK) rc = check_kv(pp);
+    if (rc != SEPATTN_OK) return rc;
+    if (!pp) return SEPATTN_ERR_NULL;
+    sepkv_params prefix = *pp;
+    prefix.scale = p->scale;  // pp's own is not looked at
+    rc = check_kv(&prefix);
     if (rc != SEPATTN_OK) return rc;
     if (p->Hq != pp->Hq || p->Hkv != pp->Hkv) return SEPATTN_ERR_SHAPE;
     if (p->d != pp->d || p->dtype != pp->dtype) return SEPATTN_ERR_DTYPE;

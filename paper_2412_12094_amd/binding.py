@@ -459,9 +459,12 @@ def sepattn_rope_frequencies(rotary_dim: int, base: float, factor: float = 1.0, 
     """-> float64 [rotary_dim/2], radians per position: base^(-2p/rotary_dim), for contexts longer than the trained one
     divided by `factor` (all, or with original_length > 0 the pairs that make fewer than `low` turns in it, blended up to `high`).
     The calls take it on the GPU."""
-    f = torch.empty(max(1, int(rotary_dim) // 2), dtype=torch.float64)
+    rotary_dim, original_length = int(rotary_dim), int(original_length)
+    if not all(-2 ** 31 <= x < 2 ** 31 for x in (rotary_dim, original_length)):
+        raise OverflowError("argument does not fit 32 bits")
+    f = torch.empty(max(1, rotary_dim // 2), dtype=torch.float64)
     _check("sepattn_rope_frequencies", load().sepattn_rope_frequencies(
-        int(rotary_dim), float(base), float(factor), float(low), float(high), int(original_length), _ptr(f)))
+        rotary_dim, float(base), float(factor), float(low), float(high), original_length, _ptr(f)))
     return f.to(device)
 
 

@@ -482,8 +482,9 @@ int sepkv_fill_from_prefill_zeroed(const sepkv_params *p, int L, int nw, const v
  * sepattn_decode_shared_rope: with positions within the caches (see sepattn_decode_rope): the entries of a sequence's prefix,
  * oldest first, are at positions 0 .. np-1, its own at np .. np+nv-1, the query at np+nv-1.  The positions of a
  * prefix never change, so its keys are turned once, by sepkv_rope_cache, and Kp holds them turned; own keys and q are
- * stored without encoding.  rope_table needs n_pos >= pp->c + p->c rows (SEPATTN_ERR_SHAPE).  Turned values count with 16 bits or
- * more of mantissa, so that lse holds to 1e-5 here.
+ * stored without encoding.  rope_table needs n_pos >= pp->c + p->c rows (SEPATTN_ERR_SHAPE).  The turned query and turned own keys
+ * count with 16 bits or more of mantissa, so that lse holds to 1e-5 for Kp as it is.  In bf16 sepkv_rope_cache rounds a turned key, by 2^-8 of it at
+ * most; against keys that are not rounded there lse is off by about 1e-4 behind thousands of entries, 1e-3 behind a few.
  *   sepkv_rope_cache: the key of the entry of rank e (oldest first) is turned by table row e, for all valid entries of
  *                Kc DEVICE dtype [S, Hkv, c, d] -> K_out, of the same shape, which may be Kc (in place: once).  Slots without a
  *                valid entry are not written.  n_pos >= c.

@@ -2,7 +2,7 @@
 import pytest
 
 torch = pytest.importorskip("torch")
-from test_gpu_decode_shared import SMALL, Case, slots_of, sp  # noqa: E402, F401
+from test_gpu_decode_shared import BASE, SMALL, Case, slots_of, sp, turn  # noqa: E402, F401
 
 pytestmark = pytest.mark.gpu
 
@@ -48,3 +48,27 @@ def test_weights_of_16_bits(sp, S, Hq, Hkv, d, n, own_n, rope):  # noqa: F811
     err = (out.double().cpu() - ref).abs()
     bound = 2.0 ** -8 * ref.abs() + (2.0 ** -15 + 2.0 * score[..., None] + 2.0 ** -18) * size
     assert (err <= bound).all(), float((err / bound).max())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("S,Hq,Hkv,d,n,own_n", [(4, 8, 2, 64, 700, [40, 7, 1]), (20, 8, 2, 128, 900, [33]), (3, 16, 2, 128, 2600, [40, 0]), (2, 4, 4, 64, 3, [1])])
+def test_positions_from_keys_that_are_not_turned(sp, S, Hq, Hkv, d, n, own_n, dtype):  # noqa: F811
+    """The whole chain, sepkv_rope_cache and the decode, against 64 bits from the keys as they were: a turned key of a prefix is stored in the
+    cache's type, in bf16 off by 2^-8 of it at most (fp32: 2^-24, and the turn's 2^-20), and so is a score by that of its sum of magnitudes."""
+    case = Case(S, Hq, Hkv, d, dtype, SMALL, (4, 30, 20, 2700), own_n, [n], [0], seed=n)
+    table = sp.sepkv_rope_table(case.pc, d, BASE, "cuda")
+    at = slots_of(case.psizes[0], case.pa, case.ps, case.pc)
+    plain = case.Kp.clone()
+    sp.sepkv_rope_cache(case.Kp, case.psz, table, case.pa, case.ps, case.pw)
+    out, lse = case.run(sp, True)
+    case.Kp = plain.double()
+    case.Kp[0][:, at] = turn(case.Kp[0][:, at], torch.arange(n, device="cuda")[None])
+    ref, ref_lse, size, reach = case.want(True)
+    stored = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -20
+    score = reach * (d * 2.0 ** -24 + 2.0 ** -21 + 2.0 ** -20 + (2.0 ** -16 if dtype == "bf16" else 0.0) + stored)
+    err = (lse.double().cpu() - ref_lse).abs()
+    print(f"lse off by {float(err.max()):.1e}, bound {float((score + 2.0 ** -22 * (ref_lse.abs() + 8.0)).min()):.1e}")
+    assert (err <= score + 2.0 ** -22 * (ref_lse.abs() + 8.0)).all(), float(err.max())
+    err = (out.double().cpu() - ref).abs()
+    half = torch.finfo(case.dt).eps / 2
+    assert (err <= half * ref.abs() + ((2.0 ** -8 if dtype == "bf16" else 0.0) + 2.0 * score[..., None] + 2.0 ** -18) * size).all(), float(err.max())

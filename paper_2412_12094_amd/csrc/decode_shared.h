@@ -19,19 +19,24 @@ struct SharedShape {
     int n_prefix;     // slices per prefix
     int n_own;        // slices per own cache
 };
-// From the capacities (the device alone knows how much of them is in use).  Figures: microseconds of a call, 32/8 heads, d = 128, bf16, without positions
-// unless said; rows: of one KV head and prefix.
+// From the capacities and from the mean number of rows per prefix place (the device alone knows how much of them is in use): a pool of G places of which
+// few are used is cut as if the sequences were spread over all of them, into few rows a workgroup and few slices (48 sequences behind one prompt of 65536
+// entries: 102 us with G = 1, 149 with 4, 394 with 8, 567 with 16; 32 behind 8192: 28, 39 with 4, 81 with 16).
+// Figures: microseconds of a call, 32/8 heads, d = 128, bf16, without positions unless said, each line from one machine (two differ by up to 8 %); rows: of
+// one KV head and prefix.
 // Rows and waves.  Up to 32 rows every wave has all of them (18 us; cut by rows 18.5: 8 sequences behind 8192 entries); above, each wave its own:
 //     64 rows, 8192 entries                              20.9 (23.5 with all of them in each wave)
-//     192 rows, 65536 entries, 3 / 2 / 1 column blocks    84 / 107 / 108: an entry read from LDS serves more rows
-//     128 rows, 8192 entries,  2 / 1 column blocks        29.6 / 27.2, turned 31.7 / 29.9: slices of fewer than 20 steps
-//   NW = 8 where a slice is long and there are many: 192 rows, 65536 entries 84 (4 waves: 87), 128 rows 69 (74); 8192 entries 29 (27.5).
+//     192 rows, 65536 entries, 3 / 2 / 1 column blocks    85 / 107 / 102: an entry read from LDS serves more rows (best of several numbers of slices)
+//     128 rows, 8192 entries,  2 / 1 column blocks        28.4 / 27.0, turned 33.2 / 31.2: slices of fewer than 20 steps
+//   NW = 8 where a slice is long and there are many: 192 rows, 65536 entries 85 to 90 over 20 to 28 slices (4 waves, 32 to 48 slices: 90 to 99), 128 rows
+//     69 (74); 8192 entries 29 (27.5).
 // Slices.  `bytes_us`: what reading every cache once takes.  A prefix is cut so finely that a workgroup's walk through its slice, at `step` per
 // 32 keys while the memory is busy, ends well before that, and at least so finely that half of the places that the chip has for workgroups
-// are taken; finer, and a slice more costs a record per row, written and read again (192 rows, 65536 entries, 20 / 24 / 28 slices: kernel
-// 95 / 85 / 95; 128 rows, 8192 entries, turned, 8 / 12 / 16 of one column block: 32.0 / 30.0 / 30.9).  Turned queries, whose scores are two products, take
-// longer per step, but so do the own caches beside them, and fewer slices pay: 96 rows, 20000 entries 35.0 (steps of 0.95 and 1.1: 39.6), 400
-// rows, 4096 entries 52.1 (56.7).
+// are taken; finer, and a slice more costs a record per row, written and read again (192 rows, 65536 entries, 16 / 20 / 24 / 28 / 32 slices: 98 / 87 / 85 /
+// 89 / 97, with the rule's 27 90; 128 rows, 8192 entries, turned, 8 / 12 / 16 / 20 of one column block: 32.4 / 31.4 / 32.1 / 43.3, with the rule's 13 31.2).  Turned
+// queries, whose scores are two products, take longer per step, but so do the own caches beside them, and fewer slices pay: 96 rows, 20000 entries
+// 35.0 (steps of 0.95 and 1.1: 39.6), 400 rows, 4096 entries 52.1 (56.7).  Where it misses the best of a sweep: 192 rows, 65536 entries, turned, two column
+// blocks and 32 slices 127; 28 slices 121, one block and 20 slices 117.
 inline SharedShape shared_shape(const sepkv_params &p, const sepkv_params &pp, bool rope) {
     SharedShape s = {};
     const long gq = p.Hq / p.Hkv, all = p.S * gq, per_prefix = (all + pp.S - 1) / pp.S, units = compute_units();

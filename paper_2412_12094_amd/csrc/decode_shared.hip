@@ -9,10 +9,10 @@
 // What it cannot do without is to read every cache once, and 4 d operations per (query head, entry): with R rows on a KV head an entry's 4 d
 // bytes feed 4 d R operations, so that from about 260 rows on the matrix units would bound it, below that the memory.
 // Measured, 32/8 heads, d = 128, bf16, microseconds of the first launch + the second (bytes of the caches at the rate of a large copy):
-//   2 sequences behind 600 entries                                   6.4 + 3.3 (1.2; launches and round trips)
-//   32 sequences behind 8192 entries, 128 rows per KV head, turned  26 + 4.6 (18.7; 3.0 TB/s over both)
-//   48 sequences behind 65536 entries, 192 rows per KV head          80 + 7.0 (72; 4.1 TB/s, 600 TFLOP/s)
-// (In one launch, the last slice of a row adding its records: 12.8 instead of 9.5 for the first; four round trips past the L2 in sequence.)
+//   2 sequences behind 600 entries                                   6.7 + 3.4 (1.2; launches and round trips)
+//   32 sequences behind 8192 entries, 128 rows per KV head, turned  27 + 4.8 (18.7; 3.0 TB/s over both)
+//   48 sequences behind 65536 entries, 192 rows per KV head          84 to 89 + 7.0 (72; 3.9 TB/s, 570 TFLOP/s)
+// (In one launch, the last slice of a row adding its records: 12.8 for the first, in two 9.5 a call; four round trips past the L2 in sequence.)
 #include "common.h"
 #include "decode_common.h"
 #include "decode_shared.h"
@@ -815,7 +815,9 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void shared_decode_kernel(SharedAr
 // of step i are keys 4 g + i, which the lane group holds.
 // KROPE (own caches): a key is turned by its distance to the query on its way into LDS, by the thread that holds both of a pair.
 // The fp32 matrix rate is a sixteenth of bf16's, and this type is there to check a bf16 run against: 11 sequences of up to 150 entries behind three prefixes
-// of up to 250 (12/12 heads, d = 64, turned) take 9.0 us and 3.2 for the sum, most of it launches and round trips (bytes: 2.2).
+// of up to 250 (12/12 heads, d = 64, turned) take 9.2 us and 3.2 for the sum, most of it launches and round trips (bytes: 2.2).
+// Where there is more to read it stays far from the memory's rate: 41 sequences of 32/8 heads, d = 64, behind 2209 entries 34 us (17), 8 of d = 128 behind 8192
+// 41 (19): tiles through registers, two barriers per 64 keys, V from LDS four bytes at a time.
 typedef float f4 __attribute__((ext_vector_type(4)));
 constexpr int kFpKeys = 64;
 template <int D>
@@ -961,7 +963,7 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_decode_fp32_kernel(Share
 // WPR waves per (sequence, head), prefix slices first, then the own cache's; wave w takes slices w, w + WPR, ... of both, eight records in one
 // round trip, and the waves' sums are added in wave order.  Nothing but the records has to be read for that (a slice without an entry
 // says so in its own; those of a prefix that the sequence does not have are skipped), so that the kernel is one round trip and its
-// launch: 3.1 us for a few rows, 4.9 for 1024 rows of 17 records, 7.5 for 1536 rows of 25.
+// launch: 3.3 us for a few rows, 4.7 for 1024 rows of 14 records, 7.0 for 1536 rows of 28.
 template <typename T, int D, int WPR>
 __global__ __launch_bounds__(kShThreads) void shared_merge_kernel(sepkv_params p, int n_prefixes, int n_prefix, int n_own,
                                                                   const int32_t *__restrict__ prefix_of, const float *__restrict__ prefix_part,

@@ -3,7 +3,7 @@
 // One wave per prefix g, and one more for the end: it walks through prefix_of[0 .. S), 1024 entries per round trip.  The number of entries
 // with 0 <= prefix_of < g is where its own begin; those it finds are written in ascending order at begin + (how many before),
 // counted with ballots.  Every wave reads the whole array (L2), no wave waits for another and nothing has to be cleared: G S / 64
-// steps of a few instructions.  Up to 1024 sequences the entries stay in registers between the two walks (G = 12, S = 1000: 3.8 us, of
+// steps of a few instructions.  Up to 1024 sequences the entries stay in registers between the two walks (G = 12, S = 1000: 3.1 us, of
 // which the launch is most; with 64 entries per round trip 8.0).
 #include "common.h"
 

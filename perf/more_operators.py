@@ -309,9 +309,9 @@ def _own_step(st):
     import paper_2412_12094_amd as sp
 
     sizes, cache, blocks = st["sizes"].clone(), (st["Kc"], st["Ks"], st["Vc"], st["Vs"]), (st["a"], st["s"], st["w"])
-    q = sp.sepkv_append_norm_rope_fp4(st["q"], st["k"], st["v"], st["sep"], st["pos"], *st["weights"], st["freqs"], EPS, *cache, st["flags"],
+    q = sp.sepkv_append_norm_rope_mx(st["q"], st["k"], st["v"], st["sep"], st["pos"], *st["weights"], st["freqs"], EPS, *cache, st["flags"],
                                       sizes, *blocks, interleaved=st["pairs"] == "neighbours")
-    out, lse = sp.sepattn_decode_fp4(q, *cache, sizes, *blocks, st["scale"])
+    out, lse = sp.sepattn_decode_mx(q, *cache, sizes, *blocks, st["scale"])
     return dict(q=q, out=out, lse=lse, flags=st["flags"], sizes=sizes)
 
 
@@ -319,10 +319,10 @@ def _own_admit(st):
     import paper_2412_12094_amd as sp
 
     blocks = (st["a"], st["s"], st["w"])
-    *cache, flags, sizes = sp.sepkv_fill_from_prefill_fp4(st["K"], st["V"], st["is_sep"], st["sep_idx"], st["sep_prefix"], st["Hq"], *blocks,
+    *cache, flags, sizes = sp.sepkv_fill_from_prefill_mx(st["K"], st["V"], st["is_sep"], st["sep_idx"], st["sep_prefix"], st["Hq"], *blocks,
                                                           st["c"], st["nw"])
-    sp.sepkv_evict_window_fp4(*cache, flags, sizes, st["Hq"], *blocks)
-    K, V = sp.sepkv_expand_fp4(*cache, sizes, *blocks, dtype=DTYPES[st["dtype"]])
+    sp.sepkv_evict_window_mx(*cache, flags, sizes, st["Hq"], *blocks)
+    K, V = sp.sepkv_expand_mx(*cache, sizes, *blocks, dtype=DTYPES[st["dtype"]])
     return dict(K=K, V=V, flags=flags, sizes=sizes)
 
 
@@ -331,8 +331,8 @@ def _own_decode(st):
 
     args = (st["q"], st["Kc"], st["Ks"], st["Vc"], st["Vs"], st["sizes"])
     if st["rope"]:
-        return sp.sepattn_decode_rope_fp4(*args, st["table"], st["a"], st["s"], st["w"], st["scale"])
-    return sp.sepattn_decode_fp4(*args, st["a"], st["s"], st["w"], st["scale"])
+        return sp.sepattn_decode_rope_mx(*args, st["table"], st["a"], st["s"], st["w"], st["scale"])
+    return sp.sepattn_decode_mx(*args, st["a"], st["s"], st["w"], st["scale"])
 
 
 # ---- the plain forms ------------------------------------------------------------------------------

@@ -285,6 +285,54 @@ int sepattn_rope_backward(const sepattn_rope_params *p, const double *freqs, con
                           const sepattn_strides *dv_strides, void *stream);
 
 /* ------------------------------------------------------------------------------------------
+ * Norms of queries and keys for each head, with the rotary positions in the same pass (backbones that norm q and k in front of the
+ * attention).  For a row x of d values, w the weight per dimension (one for all query heads, one for all key heads) and theta the
+ * angles of sepattn_rope:
+ *     r = (mean of x^2 + eps)^(-1/2),   z = R(theta) (w x r),   z rounded once; everything in between is fp32.
+ * sepattn_norm_rope is sepattn_rope with q and k normed first: layouts, strides, positions, frequencies and V are as there.
+ * sepattn_norm_rope_backward is its gradient, with g = R(-theta) dz and u = w g:
+ *     dx = r (u - x r^2 mean(u x)),   dw = sum over all rows of g x r   (V's gradient is moved as it is).
+ * The sum for dw has a fixed order: two calls give the same bits on one GPU.
+ *   p->rotary_dim   even, 0 <= rotary_dim <= d (SEPATTN_ERR_PARAM otherwise); 0: normed only, freqs may be NULL
+ *   p->eps          finite, >= 0 (SEPATTN_ERR_PARAM otherwise).  With eps = 0 a row of zeros gives NaN, as the formula does
+ *   q_weight, k_weight   DEVICE [d] in p->weight_dtype (bf16 or fp32, whatever p->dtype is), or NULL: ones
+ *   q, k            of the backward call: the rows that the forward call read
+ *   dq_weight, dk_weight DEVICE fp32 [d]  out, each may be NULL
+ *   ws              DEVICE, >= sepattn_norm_rope_backward_workspace_bytes(p) bytes, 256-byte aligned; may be NULL where both weight
+ *                   gradients are.  Calls that overlap in time need a workspace each
+ * Squares are formed in fp32: rows with magnitudes above 1e18 (or, with eps = 0, all below 1e-18) are outside what the calls cover.
+ * An infinity or a NaN stays in its row (and reaches dw).  An output may be its own input: Q q, dq dQ and so on; otherwise outputs must not
+ * overlap inputs (dq not q: other rows of q may still have to be read).
+ * B * L is at most 2^31 (SEPATTN_ERR_SHAPE).
+ * ------------------------------------------------------------------------------------------ */
+typedef struct {
+    int B;            /* sequences                                                              */
+    int Hq;           /* query heads                                                            */
+    int Hkv;          /* key/value heads                                                        */
+    int L;            /* tokens per sequence                                                    */
+    int d;            /* head dimension: 64 or 128                                              */
+    int rotary_dim;   /* leading dimensions of a head that are turned                           */
+    int interleaved;  /* 0: dimension p pairs with p + rotary_dim/2; 1: 2p with 2p + 1           */
+    int dtype;        /* sepattn_dtype of all tensors but the weights                           */
+    int weight_dtype; /* sepattn_dtype of the weights                                           */
+    float eps;        /* added to the mean of the squares                                       */
+} sepattn_norm_rope_params;
+int sepattn_norm_rope(const sepattn_norm_rope_params *p, const void *q_weight, const void *k_weight, const double *freqs,
+                      const int32_t *positions, const int32_t *doc_start, const void *q, const sepattn_strides *q_strides,
+                      const void *k, const sepattn_strides *k_strides, const void *v, const sepattn_strides *v_strides,
+                      void *Q, const sepattn_strides *Q_strides, void *K, const sepattn_strides *K_strides, void *V,
+                      const sepattn_strides *V_strides, void *stream);
+size_t sepattn_norm_rope_backward_workspace_bytes(const sepattn_norm_rope_params *p);
+int sepattn_norm_rope_backward(const sepattn_norm_rope_params *p, const void *q_weight, const void *k_weight,
+                               const double *freqs, const int32_t *positions, const int32_t *doc_start, const void *q,
+                               const sepattn_strides *q_strides, const void *k, const sepattn_strides *k_strides,
+                               const void *dQ, const sepattn_strides *dQ_strides, const void *dK,
+                               const sepattn_strides *dK_strides, const void *dV, const sepattn_strides *dV_strides,
+                               void *dq, const sepattn_strides *dq_strides, void *dk, const sepattn_strides *dk_strides,
+                               void *dv, const sepattn_strides *dv_strides, float *dq_weight, float *dk_weight, void *ws,
+                               size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------------------------
  * Streaming generation on the four-block KV cache (Sec. 3.3).
  * Cache layout, per (sequence, KV head): c slots of d values,
  *     [0, a)       Initial Cache
@@ -402,6 +450,13 @@ int sepkv_append_rope(const sepkv_params *p, int rotary_dim, int interleaved, co
                       const uint8_t *is_sep_new, void *q_out, void *Kc, void *Vc, uint8_t *win_is_sep, int32_t *sizes,
                       void *stream);
 
+/* sepkv_append_rope with query and key normed first (conventions of sepattn_norm_rope, rotary_dim 0 and NULL weights included; positions may
+ * be NULL where rotary_dim is 0). */
+int sepkv_append_norm_rope(const sepkv_params *p, int rotary_dim, int interleaved, float eps, int weight_dtype,
+                           const void *q_weight, const void *k_weight, const double *freqs, const int32_t *positions,
+                           const void *q, const void *k_new, const void *v_new, const uint8_t *is_sep_new, void *q_out,
+                           void *Kc, void *Vc, uint8_t *win_is_sep, int32_t *sizes, void *stream);
+
 /* Compression step (Sec. 3.3; caption of the streaming-design figure): the separators of the Past
  * Window Cache are appended to the Separator Cache, its other entries are dropped, and the Local
  * Window becomes the whole window.  If the Separator Cache would exceed s, its oldest entries are
@@ -453,6 +508,58 @@ int sepkv_fill_from_prefill_zeroed(const sepkv_params *p, int L, int nw, const v
                                    const uint8_t *is_sep, const int32_t *sep_idx, int cap,
                                    const int32_t *sep_prefix, void *Kc, void *Vc, uint8_t *win_is_sep,
                                    int32_t *sizes, void *stream);
+
+/* ------------------------------------------------------------------------------------------
+ * The four-block KV cache in 4 bits (the microscaling format MXFP4): 17/32 bytes a value instead of 2.  Blocks, rings and sizes are those above; a row of d values is
+ *   codes   d/2 bytes: dimension 2i in the low, 2i+1 in the high half of byte i.  Bits 0..2 of a code are the magnitude
+ *           (0, 0.5, 1, 1.5, 2, 3, 4, 6), bit 3 the sign (E2M1)
+ *   scales  d/32 bytes: the values of dimensions 32b .. 32b+31 are the codes' times 2^(byte b - 127) (E8M0); 255: all of them are NaN
+ * Rounding a row to it: 2^(E-2) with E the exponent of the block's largest magnitude after that is rounded to two bits of significand
+ * (7/4 2^E stays, anything above counts as 2^(E+1)), kept within 2^-125 .. 2^125; then each value over it to the nearest magnitude, ties to the
+ * even code, values above 6 (up to 7, or beyond the largest scale) to 6.  So a value is off by at most half the step around it (1/4, 1/2 or 1 times
+ * the scale), the scale being at most 2/7 of the block's largest magnitude.  A block with an infinity or a NaN becomes NaN.  Every value is
+ * exact in bf16 and fp32.
+ *   Kc, Vc   DEVICE uint8 [S, Hkv, c, d/2], 16-byte aligned;   Ks, Vs   DEVICE uint8 [S, Hkv, c, d/32], aligned to d/32
+ * p->dtype is the type of all other tensors (k_new, q, out, ...).
+ *
+ * sepkv_fill_from_prefill_mx, _mx_zeroed: as sepkv_fill_from_prefill, _zeroed, rows rounded on the way; _zeroed leaves code and scale 0 (value
+ *   0) in slots beyond the sizes.  S Hkv is at most 32767 (SEPATTN_ERR_SHAPE; also sepkv_expand_mx).
+ * sepkv_append_mx, sepkv_append_rope_mx, sepkv_append_norm_rope_mx: as sepkv_append, _rope, _norm_rope; a turned key is rounded to
+ *   p->dtype first, so that the cache holds what the separate calls would leave.
+ * sepkv_evict_window_mx: as sepkv_evict_window (bit-exact rows); p->dtype is not looked at beyond its check.
+ * sepkv_expand_mx: the values of all valid entries, in their slots: K, V  DEVICE dtype [S, Hkv, c, d]  out; other slots receive 0.
+ * sepattn_decode_mx, sepattn_decode_rope_mx: as sepattn_decode, _rope, over the cache's values.  lse holds to 1e-5 in bf16 too, also with positions
+ *   (sepattn_decode rounds its weights to bf16 once, here they have 16 bits).  Any number of query heads per KV head.  The workspace may hold anything
+ *   and is left in no particular state; calls that overlap in time need one each.
+ *   NaN in a query or in the cache reaches the results that see it, and no others.
+ * ------------------------------------------------------------------------------------------ */
+int sepkv_fill_from_prefill_mx(const sepkv_params *p, int L, int nw, const void *K, const void *V, const uint8_t *is_sep,
+                                const int32_t *sep_idx, int cap, const int32_t *sep_prefix, void *Kc, void *Ks, void *Vc,
+                                void *Vs, uint8_t *win_is_sep, int32_t *sizes, void *stream);
+int sepkv_fill_from_prefill_mx_zeroed(const sepkv_params *p, int L, int nw, const void *K, const void *V,
+                                       const uint8_t *is_sep, const int32_t *sep_idx, int cap, const int32_t *sep_prefix,
+                                       void *Kc, void *Ks, void *Vc, void *Vs, uint8_t *win_is_sep, int32_t *sizes,
+                                       void *stream);
+int sepkv_append_mx(const sepkv_params *p, const void *k_new, const void *v_new, const uint8_t *is_sep_new, void *Kc,
+                     void *Ks, void *Vc, void *Vs, uint8_t *win_is_sep, int32_t *sizes, void *stream);
+int sepkv_append_rope_mx(const sepkv_params *p, int rotary_dim, int interleaved, const double *freqs,
+                          const int32_t *positions, const void *q, const void *k_new, const void *v_new,
+                          const uint8_t *is_sep_new, void *q_out, void *Kc, void *Ks, void *Vc, void *Vs,
+                          uint8_t *win_is_sep, int32_t *sizes, void *stream);
+int sepkv_append_norm_rope_mx(const sepkv_params *p, int rotary_dim, int interleaved, float eps, int weight_dtype,
+                               const void *q_weight, const void *k_weight, const double *freqs, const int32_t *positions,
+                               const void *q, const void *k_new, const void *v_new, const uint8_t *is_sep_new, void *q_out,
+                               void *Kc, void *Ks, void *Vc, void *Vs, uint8_t *win_is_sep, int32_t *sizes, void *stream);
+int sepkv_evict_window_mx(const sepkv_params *p, void *Kc, void *Ks, void *Vc, void *Vs, const uint8_t *win_is_sep,
+                           int32_t *sizes, void *stream);
+int sepkv_expand_mx(const sepkv_params *p, const int32_t *sizes, const void *Kc, const void *Ks, const void *Vc,
+                     const void *Vs, void *K, void *V, void *stream);
+size_t sepattn_decode_mx_workspace_bytes(const sepkv_params *p);
+int sepattn_decode_mx(const sepkv_params *p, const void *q, const void *Kc, const void *Ks, const void *Vc, const void *Vs,
+                       const int32_t *sizes, void *out, float *lse, void *ws, size_t ws_bytes, void *stream);
+int sepattn_decode_rope_mx(const sepkv_params *p, const void *q, const void *Kc, const void *Ks, const void *Vc,
+                            const void *Vs, const int32_t *sizes, const float *rope_table, int n_pos, void *out, float *lse,
+                            void *ws, size_t ws_bytes, void *stream);
 
 /* ------------------------------------------------------------------------------------------
  * Generation behind shared prompts.  Sequences that begin with the same prompt keep its entries once: G prefix caches, each a
@@ -518,6 +625,8 @@ int sepattn_decode_shared_rope(const sepkv_params *p, const sepkv_params *pp, co
  * launch counts as SEPATTN_K_BWD_DKV, and SEPATTN_K_BWD_DQ is the short one in front of it that forms the row values.
  * The launches of sepattn_decode_shared count as SEPATTN_K_DECODE_SPLIT and SEPATTN_K_DECODE_MERGE, that of sepkv_append_rope as
  * SEPATTN_K_CACHE_APPEND; sepattn_rope, sepkv_rope_cache and sepkv_group_sequences have no id.
+ * The launches of the 4-bit cache calls count as their plain forms' (append, fill, evict, decode), that of sepkv_append_norm_rope as
+ * SEPATTN_K_CACHE_APPEND; sepattn_norm_rope, its backward and sepkv_expand_mx have no id.
  *   sepattn_profile_create   kernel: a sepattn_kernel_id; max_records: events are created up front
  *                            for this many launches, further launches are not recorded;
  *                            *out receives the handle (HOST)

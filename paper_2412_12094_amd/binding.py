@@ -67,6 +67,20 @@ EXPORTS = (
     "sepattn_decode_shared_workspace_bytes",
     "sepattn_decode_shared",
     "sepattn_decode_shared_rope",
+    "sepattn_norm_rope",
+    "sepattn_norm_rope_backward_workspace_bytes",
+    "sepattn_norm_rope_backward",
+    "sepkv_append_norm_rope",
+    "sepkv_fill_from_prefill_mx",
+    "sepkv_fill_from_prefill_mx_zeroed",
+    "sepkv_append_mx",
+    "sepkv_append_rope_mx",
+    "sepkv_append_norm_rope_mx",
+    "sepkv_evict_window_mx",
+    "sepkv_expand_mx",
+    "sepattn_decode_mx_workspace_bytes",
+    "sepattn_decode_mx",
+    "sepattn_decode_rope_mx",
     "sepattn_kernel_name",
     "sepattn_profile_create",
     "sepattn_profile_attach",
@@ -90,6 +104,10 @@ class SepkvParams(ctypes.Structure):
 
 class SepattnRopeParams(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int) for n in ("B", "Hq", "Hkv", "L", "d", "rotary_dim", "interleaved", "dtype")]
+
+
+class SepattnNormRopeParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("B", "Hq", "Hkv", "L", "d", "rotary_dim", "interleaved", "dtype", "weight_dtype")] + [("eps", ctypes.c_float)]
 
 
 class SepattnStrides(ctypes.Structure):
@@ -197,6 +215,35 @@ def load(path: Optional[str] = None):
     lib.sepattn_decode_shared.argtypes = [kp, kp] + [vp] * 13 + [sz, vp]
     lib.sepattn_decode_shared_rope.restype = ci
     lib.sepattn_decode_shared_rope.argtypes = [kp, kp] + [vp] * 11 + [ci, vp, vp, vp, sz, vp]
+    np_, strided = ctypes.POINTER(SepattnNormRopeParams), [vp, ctypes.POINTER(SepattnStrides)]
+    lib.sepattn_norm_rope.restype = ci
+    lib.sepattn_norm_rope.argtypes = [np_] + [vp] * 5 + strided * 6 + [vp]
+    lib.sepattn_norm_rope_backward_workspace_bytes.restype = sz
+    lib.sepattn_norm_rope_backward_workspace_bytes.argtypes = [np_]
+    lib.sepattn_norm_rope_backward.restype = ci
+    lib.sepattn_norm_rope_backward.argtypes = [np_] + [vp] * 5 + strided * 8 + [vp, vp, vp, sz, vp]
+    norm = [kp, ci, ci, ctypes.c_float, ci, vp, vp]  # params, rotary_dim, interleaved, eps, weight_dtype, weights
+    lib.sepkv_append_norm_rope.restype = ci
+    lib.sepkv_append_norm_rope.argtypes = norm + [vp] * 12
+    lib.sepkv_append_mx.restype = ci
+    lib.sepkv_append_mx.argtypes = [kp] + [vp] * 10
+    lib.sepkv_append_rope_mx.restype = ci
+    lib.sepkv_append_rope_mx.argtypes = [kp, ci, ci] + [vp] * 14
+    lib.sepkv_append_norm_rope_mx.restype = ci
+    lib.sepkv_append_norm_rope_mx.argtypes = norm + [vp] * 14
+    for name in ("sepkv_fill_from_prefill_mx", "sepkv_fill_from_prefill_mx_zeroed"):
+        getattr(lib, name).restype = ci
+        getattr(lib, name).argtypes = [kp, ci, ci, vp, vp, vp, vp, ci] + [vp] * 8
+    lib.sepkv_evict_window_mx.restype = ci
+    lib.sepkv_evict_window_mx.argtypes = [kp] + [vp] * 7
+    lib.sepkv_expand_mx.restype = ci
+    lib.sepkv_expand_mx.argtypes = [kp] + [vp] * 8
+    lib.sepattn_decode_mx_workspace_bytes.restype = sz
+    lib.sepattn_decode_mx_workspace_bytes.argtypes = [kp]
+    lib.sepattn_decode_mx.restype = ci
+    lib.sepattn_decode_mx.argtypes = [kp] + [vp] * 9 + [sz, vp]
+    lib.sepattn_decode_rope_mx.restype = ci
+    lib.sepattn_decode_rope_mx.argtypes = [kp] + [vp] * 7 + [ci, vp, vp, vp, sz, vp]
     lib.sepattn_kernel_name.restype = ctypes.c_char_p
     lib.sepattn_kernel_name.argtypes = [ci]
     lib.sepattn_profile_create.restype = ci
@@ -538,3 +585,91 @@ def sepattn_decode_shared_rope(q, Kc, Vc, sizes, a: int, s: int, w: int, Kp, Vp,
     stored without encoding; rope_table with prefix_c + c rows or more."""
     return _native().decode_shared_rope(q, Kc, Vc, sizes, a, s, w, Kp, Vp, prefix_sizes, prefix_a, prefix_s, prefix_w, prefix_of,
                                         group_start, group_seq, rope_table, scale, out, ws)
+
+
+# ---- norms of queries and keys in front of the rotary positions ------------------------------------
+def sepattn_norm_rope(q, k, v, q_weight, k_weight, freqs, eps: float, positions: Optional[torch.Tensor] = None,
+                      doc_start: Optional[torch.Tensor] = None, interleaved: bool = False, out=None):
+    """sepattn_rope with the rows of q and k divided by their root mean square (eps added to the mean square) and multiplied by
+    q_weight, k_weight [d] (bf16 or fp32, None: ones) first.  freqs None: normed only."""
+    return _native().norm_rope(q, k, v, q_weight, k_weight, freqs, eps, positions, doc_start, interleaved, out)
+
+
+def sepattn_norm_rope_backward_workspace_bytes(q, k, eps: float = 0.0, rotary_dim: int = 0) -> int:
+    """Of a call with q [B,Hq,L,d], k [B,Hkv,L,d]; the largest over all positions and weights."""
+    B, Hq, L, d = q.shape
+    p = SepattnNormRopeParams(B, Hq, k.shape[1], L, d, int(rotary_dim), 0, _dtype_code(q), SEPATTN_FP32, float(eps))
+    with torch.cuda.device(q.device):
+        return int(load().sepattn_norm_rope_backward_workspace_bytes(ctypes.byref(p)))
+
+
+def sepattn_norm_rope_backward(q, k, dQ, dK, dV, q_weight, k_weight, freqs, eps: float, positions: Optional[torch.Tensor] = None,
+                               doc_start: Optional[torch.Tensor] = None, interleaved: bool = False, out=None, out_weights=None,
+                               ws: Optional[torch.Tensor] = None):
+    """Gradient of sepattn_norm_rope, whose inputs q, k were: dQ [B,Hq,L,d], dK, dV [B,Hkv,L,d] (dV may be None)
+    -> (dq, dk, dv, dq_weight, dk_weight), the last two fp32 [d].  Unless `out` = (dq, dk, dv) is given, these are views of one buffer
+    [B, L, Hq + 2 Hkv, d].  out_weights: two tensors fp32 [d], None in the place of one that is not wanted."""
+    return _native().norm_rope_backward(q, k, dQ, dK, dV, q_weight, k_weight, freqs, eps, positions, doc_start, interleaved, out, out_weights, ws)
+
+
+def sepkv_append_norm_rope(q, k_new, v_new, is_sep_new, positions, q_weight, k_weight, freqs, eps: float, Kc, Vc, win_is_sep, sizes, a: int,
+                           s: int, w: int, interleaved: bool = False, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """sepkv_append_rope for a token whose query and key are normed first (sepattn_norm_rope; freqs and positions may be None)."""
+    return _native().append_norm_rope(q, k_new, v_new, is_sep_new, positions, q_weight, k_weight, freqs, eps, Kc, Vc, win_is_sep, sizes, a, s, w,
+                                      interleaved, out)
+
+
+# ---- the cache in 4 bits -----------------------------------------------------------------------------
+# Kc, Vc uint8 [S,Hkv,c,d/2]: codes; Ks, Vs uint8 [S,Hkv,c,d/32]: scales
+def sepkv_fill_from_prefill_mx(K, V, is_sep, sep_idx, sep_prefix, Hq: int, a: int, s: int, w: int, c: int, nw: int, out=None):
+    """sepkv_fill_from_prefill with the rows rounded to 4 bits -> (Kc, Ks, Vc, Vs, win_is_sep, sizes).  Freshly allocated outputs hold
+    zeros beyond the sizes (`out`: left untouched there)."""
+    return _native().fill_from_prefill_fp4(K, V, is_sep, sep_idx, sep_prefix, Hq, a, s, w, c, nw, out)
+
+
+def sepkv_append_mx(k_new, v_new, is_sep_new, Kc, Ks, Vc, Vs, win_is_sep, sizes, Hq: int, a: int, s: int, w: int) -> None:
+    """In place: k_new, v_new [S,Hkv,d], rounded to 4 bits, and is_sep_new uint8 [S] enter the cache."""
+    _native().append_fp4(k_new, v_new, is_sep_new, Kc, Ks, Vc, Vs, win_is_sep, sizes, Hq, a, s, w)
+
+
+def sepkv_append_rope_mx(q, k_new, v_new, is_sep_new, positions, freqs, Kc, Ks, Vc, Vs, win_is_sep, sizes, a: int, s: int, w: int,
+                          interleaved: bool = False, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """sepkv_append_rope into a cache in 4 bits."""
+    return _native().append_rope_fp4(q, k_new, v_new, is_sep_new, positions, freqs, Kc, Ks, Vc, Vs, win_is_sep, sizes, a, s, w, interleaved, out)
+
+
+def sepkv_append_norm_rope_mx(q, k_new, v_new, is_sep_new, positions, q_weight, k_weight, freqs, eps: float, Kc, Ks, Vc, Vs, win_is_sep,
+                               sizes, a: int, s: int, w: int, interleaved: bool = False, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """sepkv_append_norm_rope into a cache in 4 bits."""
+    return _native().append_norm_rope_fp4(q, k_new, v_new, is_sep_new, positions, q_weight, k_weight, freqs, eps, Kc, Ks, Vc, Vs, win_is_sep, sizes,
+                                          a, s, w, interleaved, out)
+
+
+def sepkv_evict_window_mx(Kc, Ks, Vc, Vs, win_is_sep, sizes, Hq: int, a: int, s: int, w: int) -> None:
+    """sepkv_evict_window on a cache in 4 bits."""
+    _native().evict_window_fp4(Kc, Ks, Vc, Vs, win_is_sep, sizes, Hq, a, s, w)
+
+
+def sepkv_expand_mx(Kc, Ks, Vc, Vs, sizes, a: int, s: int, w: int, dtype: torch.dtype = torch.bfloat16, out=None):
+    """-> (K, V) [S,Hkv,c,d]: the values of the cache's valid entries, exact in bf16 and fp32, 0 in all other slots."""
+    if out is None and dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError("unsupported dtype: bf16 or fp32 expected")
+    return _native().expand_fp4(Kc, Ks, Vc, Vs, sizes, a, s, w, dtype == torch.float32, out)
+
+
+def sepattn_decode_mx_workspace_bytes(q, Kc, a: int, s: int, w: int) -> int:
+    S, Hq, d = q.shape
+    p = SepkvParams(S, Hq, Kc.shape[1], d, int(a), int(s), int(w), Kc.shape[2], 1.0, _dtype_code(q))
+    with torch.cuda.device(q.device):
+        return int(load().sepattn_decode_mx_workspace_bytes(ctypes.byref(p)))
+
+
+def sepattn_decode_mx(q, Kc, Ks, Vc, Vs, sizes, a: int, s: int, w: int, scale: float, out=None, ws: Optional[torch.Tensor] = None):
+    """sepattn_decode over the values of a cache in 4 bits: q [S,Hq,d] -> (out [S,Hq,d], lse fp32 [S,Hq])."""
+    return _native().decode_fp4(q, Kc, Ks, Vc, Vs, sizes, None, a, s, w, scale, out, ws)
+
+
+def sepattn_decode_rope_mx(q, Kc, Ks, Vc, Vs, sizes, rope_table, a: int, s: int, w: int, scale: float, out=None,
+                            ws: Optional[torch.Tensor] = None):
+    """The same with positions within the cache (sepattn_decode_rope): q and the cached keys are stored without encoding."""
+    return _native().decode_rope_fp4(q, Kc, Ks, Vc, Vs, sizes, rope_table, a, s, w, scale, out, ws)

@@ -15,7 +15,8 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libsepattn.so")
 NATIVE = os.path.join(HERE, "_native.so")  # imported as paper_2412_12094_amd._native
 SOURCES = ["api.hip", "mark_compact.hip", "attn_fp32.hip", "fwd_bf16.hip", "bwd_bf16.hip", "bwd_dkv_bf16.hip", "bwd_joint64.hip", "bwd_joint128.hip", "decode.hip", "decode_mfma.hip", "decode_wide.hip", "decode_noalloc.hip",
-           "decode_shared.hip", "evict.hip", "cache_fill.hip", "rope_table.hip", "cache_append.hip", "rope.hip", "group_sequences.hip", "doc_bounds.hip"]
+           "decode_shared.hip", "evict.hip", "cache_fill.hip", "rope_table.hip", "cache_append.hip", "rope.hip", "group_sequences.hip", "doc_bounds.hip",
+           "norm_rope.hip", "cache_fp4.hip", "decode_fp4.hip"]
 # packed fp32 VALU instructions are switched off (some of their forms have miscomputed on
 # this hardware); the host pass does not know the feature and says so, which is harmless
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Xclang", "-target-feature", "-Xclang",

@@ -554,6 +554,80 @@ int sepattn_rope_backward(const sepattn_rope_params *p, const double *freqs, con
     return rope(p, freqs, positions, doc_start, src, from, dst, to, true, stream);
 }
 
+// Norms and rotary positions
+static int check_norm_rope(const sepattn_norm_rope_params *p, const void *q_weight, const void *k_weight, const double *freqs, const int32_t *positions,
+                           const int32_t *doc_start) {
+    if (!p || (p->rotary_dim != 0 && !freqs)) return SEPATTN_ERR_NULL;
+    if (p->B <= 0 || p->Hq <= 0 || p->Hkv <= 0 || p->L <= 0 || p->B > 65535) return SEPATTN_ERR_SHAPE;
+    if ((long)p->Hq + 2L * p->Hkv > 65535L || (long)p->B * (p->Hq + p->Hkv) * p->L > (1L << 40)) return SEPATTN_ERR_SHAPE;
+    if ((long)p->B * p->L > (1L << 31)) return SEPATTN_ERR_SHAPE;  // tiles of tokens are counted in 32 bits
+    if (p->d != 64 && p->d != 128) return SEPATTN_ERR_DTYPE;
+    if (p->dtype != SEPATTN_BF16 && p->dtype != SEPATTN_FP32) return SEPATTN_ERR_DTYPE;
+    if (p->weight_dtype != SEPATTN_BF16 && p->weight_dtype != SEPATTN_FP32) return SEPATTN_ERR_DTYPE;
+    if (p->rotary_dim < 0 || p->rotary_dim > p->d || p->rotary_dim % 2 != 0) return SEPATTN_ERR_PARAM;
+    if (!(p->eps >= 0.f) || p->eps > 1e30f || (positions && doc_start)) return SEPATTN_ERR_PARAM;
+    const size_t unit = p->weight_dtype == SEPATTN_BF16 ? 2 : 4;
+    if (!aligned(freqs, 8) || !aligned(q_weight, unit) || !aligned(k_weight, unit)) return SEPATTN_ERR_PARAM;
+    return SEPATTN_OK;
+}
+static sepattn_rope_params rope_shape(const sepattn_norm_rope_params &p) {
+    return {p.B, p.Hq, p.Hkv, p.L, p.d, p.rotary_dim, p.interleaved, p.dtype};
+}
+
+int sepattn_norm_rope(const sepattn_norm_rope_params *p, const void *q_weight, const void *k_weight, const double *freqs, const int32_t *positions,
+                      const int32_t *doc_start, const void *q, const sepattn_strides *q_strides, const void *k, const sepattn_strides *k_strides,
+                      const void *v, const sepattn_strides *v_strides, void *Q, const sepattn_strides *Q_strides, void *K,
+                      const sepattn_strides *K_strides, void *V, const sepattn_strides *V_strides, void *stream) {
+    int rc = check_norm_rope(p, q_weight, k_weight, freqs, positions, doc_start);
+    if (rc != SEPATTN_OK) return rc;
+    if (!q || !k || !Q || !K || !v != !V) return SEPATTN_ERR_NULL;
+    NormRopeTensors x = {{q, k, v}, {}, {Q, K, V}, {}, {}, {}, {p->Hq, p->Hkv, v ? p->Hkv : 0}, {{q_weight, p->weight_dtype}, {k_weight, p->weight_dtype}}};
+    const sepattn_strides *const from[3] = {q_strides, k_strides, v_strides}, *const to[3] = {Q_strides, K_strides, V_strides};
+    const sepattn_rope_params shape = rope_shape(*p);
+    for (int i = 0; i < 3; ++i) {
+        if (!x.src[i]) continue;
+        rc = rope_strides(shape, x.heads[i], from[i], false, x.src[i], x.from[i]);
+        if (rc == SEPATTN_OK) rc = rope_strides(shape, x.heads[i], to[i], true, x.dst[i], x.to[i]);
+        if (rc != SEPATTN_OK) return rc;
+    }
+    discard_stale_hip_error();
+    return launch_norm_rope(*p, freqs, positions, doc_start, x, static_cast<hipStream_t>(stream));
+}
+
+size_t sepattn_norm_rope_backward_workspace_bytes(const sepattn_norm_rope_params *p) {
+    // (positions, weights and frequencies have no part in it)
+    if (check_norm_rope(p, nullptr, nullptr, reinterpret_cast<const double *>(8), nullptr, nullptr) != SEPATTN_OK) return 0;
+    return norm_rope_backward_workspace(*p);
+}
+
+int sepattn_norm_rope_backward(const sepattn_norm_rope_params *p, const void *q_weight, const void *k_weight, const double *freqs,
+                               const int32_t *positions, const int32_t *doc_start, const void *q, const sepattn_strides *q_strides, const void *k,
+                               const sepattn_strides *k_strides, const void *dQ, const sepattn_strides *dQ_strides, const void *dK,
+                               const sepattn_strides *dK_strides, const void *dV, const sepattn_strides *dV_strides, void *dq,
+                               const sepattn_strides *dq_strides, void *dk, const sepattn_strides *dk_strides, void *dv,
+                               const sepattn_strides *dv_strides, float *dq_weight, float *dk_weight, void *ws, size_t ws_bytes, void *stream) {
+    int rc = check_norm_rope(p, q_weight, k_weight, freqs, positions, doc_start);
+    if (rc != SEPATTN_OK) return rc;
+    if (!q || !k || !dQ || !dK || !dq || !dk || !dV != !dv) return SEPATTN_ERR_NULL;
+    if (!aligned(dq_weight, 4) || !aligned(dk_weight, 4)) return SEPATTN_ERR_PARAM;
+    NormRopeTensors x = {{q, k, nullptr}, {dQ, dK, dV}, {dq, dk, dv}, {}, {}, {}, {p->Hq, p->Hkv, dV ? p->Hkv : 0},
+                         {{q_weight, p->weight_dtype}, {k_weight, p->weight_dtype}}};
+    const sepattn_strides *const from[3] = {q_strides, k_strides, nullptr}, *const grad[3] = {dQ_strides, dK_strides, dV_strides},
+                                 *const to[3] = {dq_strides, dk_strides, dv_strides};
+    const sepattn_rope_params shape = rope_shape(*p);
+    for (int i = 0; i < 3; ++i) {
+        if (!x.grad[i]) continue;
+        rc = x.src[i] ? rope_strides(shape, x.heads[i], from[i], false, x.src[i], x.from[i]) : SEPATTN_OK;
+        if (rc == SEPATTN_OK) rc = rope_strides(shape, x.heads[i], grad[i], false, x.grad[i], x.grad_strides[i]);
+        if (rc == SEPATTN_OK) rc = rope_strides(shape, x.heads[i], to[i], true, x.dst[i], x.to[i]);
+        if (rc != SEPATTN_OK) return rc;
+    }
+    if ((dq_weight || dk_weight) && (!ws || ws_bytes < norm_rope_backward_workspace(*p) || !aligned(ws, 256))) return SEPATTN_ERR_WORKSPACE;
+    discard_stale_hip_error();
+    return launch_norm_rope_backward(*p, freqs, positions, doc_start, x, dq_weight, dk_weight, static_cast<float *>(ws),
+                                     static_cast<hipStream_t>(stream));
+}
+
 size_t sepattn_decode_workspace_bytes(const sepkv_params *p) {
     if (check_kv(p) != SEPATTN_OK) return 0;
     return decode_workspace(*p);
@@ -615,21 +689,145 @@ int sepkv_append(const sepkv_params *p, const void *k_new, const void *v_new, co
                                static_cast<hipStream_t>(stream));
 }
 
+// A token on its way into a cache, its query and key turned: what concerns them
+static int check_token(const sepkv_params *p, const TokenTurn &turn, const void *q, const void *k_new, const void *v_new, const uint8_t *is_sep_new,
+                       const void *q_out, const uint8_t *win_is_sep, const int32_t *sizes) {
+    const int rc = check_kv(p);
+    if (rc != SEPATTN_OK) return rc;
+    const bool turned = !turn.norm || turn.rotary_dim != 0;  // a normed token may stay unturned
+    if ((turned && (!turn.freqs || !turn.positions)) || !q || !k_new || !v_new || !is_sep_new || !q_out || !win_is_sep || !sizes) return SEPATTN_ERR_NULL;
+    if (turn.rotary_dim < (turn.norm ? 0 : 2) || turn.rotary_dim > p->d || turn.rotary_dim % 2 != 0) return SEPATTN_ERR_PARAM;
+    if (!aligned(turn.freqs, 8) || !aligned(q, 16) || !aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(q_out, 16)) return SEPATTN_ERR_PARAM;
+    if (!turn.norm) return SEPATTN_OK;
+    if (turn.q_weight.dtype != SEPATTN_BF16 && turn.q_weight.dtype != SEPATTN_FP32) return SEPATTN_ERR_DTYPE;
+    const size_t unit = turn.q_weight.dtype == SEPATTN_BF16 ? 2 : 4;
+    if (!(turn.eps >= 0.f) || turn.eps > 1e30f || !aligned(turn.q_weight.w, unit) || !aligned(turn.k_weight.w, unit)) return SEPATTN_ERR_PARAM;
+    return SEPATTN_OK;
+}
+static int append_turned(const sepkv_params *p, const TokenTurn &turn, const void *q, const void *k_new, const void *v_new, const uint8_t *is_sep_new,
+                         void *q_out, void *Kc, void *Vc, uint8_t *win_is_sep, int32_t *sizes, void *stream) {
+    const int rc = check_token(p, turn, q, k_new, v_new, is_sep_new, q_out, win_is_sep, sizes);
+    if (rc != SEPATTN_OK) return rc;
+    if (!Kc || !Vc) return SEPATTN_ERR_NULL;
+    if (!aligned(Kc, 16) || !aligned(Vc, 16)) return SEPATTN_ERR_PARAM;
+    discard_stale_hip_error();
+    return launch_cache_append_rope(*p, turn, q, k_new, v_new, is_sep_new, q_out, Kc, Vc, win_is_sep, sizes, static_cast<hipStream_t>(stream));
+}
+
 int sepkv_append_rope(const sepkv_params *p, int rotary_dim, int interleaved, const double *freqs,
                       const int32_t *positions, const void *q, const void *k_new, const void *v_new,
                       const uint8_t *is_sep_new, void *q_out, void *Kc, void *Vc, uint8_t *win_is_sep, int32_t *sizes,
                       void *stream) {
-    int rc = check_kv(p);
+    return append_turned(p, {rotary_dim, interleaved, freqs, positions, false, 0.f, {}, {}}, q, k_new, v_new, is_sep_new, q_out, Kc, Vc, win_is_sep, sizes,
+                         stream);
+}
+
+int sepkv_append_norm_rope(const sepkv_params *p, int rotary_dim, int interleaved, float eps, int weight_dtype, const void *q_weight,
+                           const void *k_weight, const double *freqs, const int32_t *positions, const void *q, const void *k_new, const void *v_new,
+                           const uint8_t *is_sep_new, void *q_out, void *Kc, void *Vc, uint8_t *win_is_sep, int32_t *sizes, void *stream) {
+    return append_turned(p, {rotary_dim, interleaved, freqs, positions, true, eps, {q_weight, weight_dtype}, {k_weight, weight_dtype}}, q, k_new, v_new,
+                         is_sep_new, q_out, Kc, Vc, win_is_sep, sizes, stream);
+}
+
+// the four tensors of a cache in 4 bits
+static int check_fp4(const sepkv_params *p, const void *Kc, const void *Ks, const void *Vc, const void *Vs) {
+    const int rc = check_kv(p);
     if (rc != SEPATTN_OK) return rc;
-    if (!freqs || !positions || !q || !k_new || !v_new || !is_sep_new || !q_out || !Kc || !Vc || !win_is_sep || !sizes)
-        return SEPATTN_ERR_NULL;
-    if (rotary_dim < 2 || rotary_dim > p->d || rotary_dim % 2 != 0) return SEPATTN_ERR_PARAM;
-    if (!aligned(freqs, 8) || !aligned(q, 16) || !aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(q_out, 16) ||
-        !aligned(Kc, 16) || !aligned(Vc, 16))
-        return SEPATTN_ERR_PARAM;
+    if (!Kc || !Ks || !Vc || !Vs) return SEPATTN_ERR_NULL;
+    const size_t scales = p->d / 32;  // a row's scale bytes are one word
+    if (!aligned(Kc, 16) || !aligned(Vc, 16) || !aligned(Ks, scales) || !aligned(Vs, scales)) return SEPATTN_ERR_PARAM;
+    return SEPATTN_OK;
+}
+static Fp4Cache fp4_cache(const void *Kc, const void *Ks, const void *Vc, const void *Vs) {
+    auto bytes = [](const void *x) { return static_cast<uint8_t *>(const_cast<void *>(x)); };
+    return {bytes(Kc), bytes(Ks), bytes(Vc), bytes(Vs)};
+}
+
+int sepkv_append_mx(const sepkv_params *p, const void *k_new, const void *v_new, const uint8_t *is_sep_new, void *Kc, void *Ks, void *Vc, void *Vs,
+                     uint8_t *win_is_sep, int32_t *sizes, void *stream) {
+    const int rc = check_fp4(p, Kc, Ks, Vc, Vs);
+    if (rc != SEPATTN_OK) return rc;
+    if (!k_new || !v_new || !is_sep_new || !win_is_sep || !sizes) return SEPATTN_ERR_NULL;
+    if (!aligned(k_new, 16) || !aligned(v_new, 16)) return SEPATTN_ERR_PARAM;
     discard_stale_hip_error();
-    return launch_cache_append_rope(*p, rotary_dim, interleaved, freqs, positions, q, k_new, v_new, is_sep_new, q_out, Kc, Vc,
-                                    win_is_sep, sizes, static_cast<hipStream_t>(stream));
+    return launch_append_fp4(*p, nullptr, nullptr, k_new, v_new, is_sep_new, nullptr, fp4_cache(Kc, Ks, Vc, Vs), win_is_sep, sizes,
+                             static_cast<hipStream_t>(stream));
+}
+
+static int append_turned_fp4(const sepkv_params *p, const TokenTurn &turn, const void *q, const void *k_new, const void *v_new,
+                             const uint8_t *is_sep_new, void *q_out, void *Kc, void *Ks, void *Vc, void *Vs, uint8_t *win_is_sep, int32_t *sizes,
+                             void *stream) {
+    int rc = check_token(p, turn, q, k_new, v_new, is_sep_new, q_out, win_is_sep, sizes);
+    if (rc == SEPATTN_OK) rc = check_fp4(p, Kc, Ks, Vc, Vs);
+    if (rc != SEPATTN_OK) return rc;
+    discard_stale_hip_error();
+    return launch_append_fp4(*p, &turn, q, k_new, v_new, is_sep_new, q_out, fp4_cache(Kc, Ks, Vc, Vs), win_is_sep, sizes,
+                             static_cast<hipStream_t>(stream));
+}
+
+int sepkv_append_rope_mx(const sepkv_params *p, int rotary_dim, int interleaved, const double *freqs, const int32_t *positions, const void *q,
+                          const void *k_new, const void *v_new, const uint8_t *is_sep_new, void *q_out, void *Kc, void *Ks, void *Vc, void *Vs,
+                          uint8_t *win_is_sep, int32_t *sizes, void *stream) {
+    return append_turned_fp4(p, {rotary_dim, interleaved, freqs, positions, false, 0.f, {}, {}}, q, k_new, v_new, is_sep_new, q_out, Kc, Ks, Vc, Vs,
+                             win_is_sep, sizes, stream);
+}
+
+int sepkv_append_norm_rope_mx(const sepkv_params *p, int rotary_dim, int interleaved, float eps, int weight_dtype, const void *q_weight,
+                               const void *k_weight, const double *freqs, const int32_t *positions, const void *q, const void *k_new,
+                               const void *v_new, const uint8_t *is_sep_new, void *q_out, void *Kc, void *Ks, void *Vc, void *Vs, uint8_t *win_is_sep,
+                               int32_t *sizes, void *stream) {
+    return append_turned_fp4(p, {rotary_dim, interleaved, freqs, positions, true, eps, {q_weight, weight_dtype}, {k_weight, weight_dtype}}, q, k_new, v_new,
+                             is_sep_new, q_out, Kc, Ks, Vc, Vs, win_is_sep, sizes, stream);
+}
+
+int sepkv_evict_window_mx(const sepkv_params *p, void *Kc, void *Ks, void *Vc, void *Vs, const uint8_t *win_is_sep, int32_t *sizes, void *stream) {
+    const int rc = check_fp4(p, Kc, Ks, Vc, Vs);
+    if (rc != SEPATTN_OK) return rc;
+    if (!win_is_sep || !sizes) return SEPATTN_ERR_NULL;
+    discard_stale_hip_error();
+    return launch_evict_fp4(*p, fp4_cache(Kc, Ks, Vc, Vs), win_is_sep, sizes, static_cast<hipStream_t>(stream));
+}
+
+int sepkv_expand_mx(const sepkv_params *p, const int32_t *sizes, const void *Kc, const void *Ks, const void *Vc, const void *Vs, void *K, void *V,
+                     void *stream) {
+    const int rc = check_fp4(p, Kc, Ks, Vc, Vs);
+    if (rc != SEPATTN_OK) return rc;
+    if (!sizes || !K || !V) return SEPATTN_ERR_NULL;
+    if (!aligned(K, 16) || !aligned(V, 16)) return SEPATTN_ERR_PARAM;
+    if (2L * p->S * p->Hkv > 65535L) return SEPATTN_ERR_SHAPE;  // second grid dimension
+    discard_stale_hip_error();
+    return launch_expand_fp4(*p, sizes, fp4_cache(Kc, Ks, Vc, Vs), K, V, static_cast<hipStream_t>(stream));
+}
+
+size_t sepattn_decode_mx_workspace_bytes(const sepkv_params *p) {
+    if (check_kv(p) != SEPATTN_OK) return 0;
+    return decode_fp4_workspace(*p);
+}
+
+static int decode_fp4(const sepkv_params *p, const void *q, const void *Kc, const void *Ks, const void *Vc, const void *Vs, const int32_t *sizes,
+                      const float *rope_table, int n_pos, void *out, float *lse, void *ws, size_t ws_bytes, void *stream) {
+    const int rc = check_fp4(p, Kc, Ks, Vc, Vs);
+    if (rc != SEPATTN_OK) return rc;
+    if (!q || !sizes || !out) return SEPATTN_ERR_NULL;
+    if (!aligned(q, 16) || !aligned(out, 16)) return SEPATTN_ERR_PARAM;
+    if (!ws || ws_bytes < decode_fp4_workspace(*p) || !aligned(ws, 256)) return SEPATTN_ERR_WORKSPACE;
+    discard_stale_hip_error();
+    return launch_decode_fp4(*p, q, fp4_cache(Kc, Ks, Vc, Vs), sizes, rope_table, n_pos, out, lse, ws, static_cast<hipStream_t>(stream));
+}
+
+int sepattn_decode_mx(const sepkv_params *p, const void *q, const void *Kc, const void *Ks, const void *Vc, const void *Vs, const int32_t *sizes,
+                       void *out, float *lse, void *ws, size_t ws_bytes, void *stream) {
+    return decode_fp4(p, q, Kc, Ks, Vc, Vs, sizes, nullptr, 0, out, lse, ws, ws_bytes, stream);
+}
+
+int sepattn_decode_rope_mx(const sepkv_params *p, const void *q, const void *Kc, const void *Ks, const void *Vc, const void *Vs,
+                            const int32_t *sizes, const float *rope_table, int n_pos, void *out, float *lse, void *ws, size_t ws_bytes, void *stream) {
+    const int rc = check_kv(p);
+    if (rc != SEPATTN_OK) return rc;
+    if (!rope_table) return SEPATTN_ERR_NULL;
+    if (n_pos < p->c) return SEPATTN_ERR_SHAPE;  // a row for every position a full cache can hold
+    if (!aligned(rope_table, 16)) return SEPATTN_ERR_PARAM;
+    return decode_fp4(p, q, Kc, Ks, Vc, Vs, sizes, rope_table, n_pos, out, lse, ws, ws_bytes, stream);
 }
 
 int sepkv_group_sequences(const int32_t *prefix_of, int S, int G, int32_t *group_start, int32_t *group_seq, void *stream) {
@@ -723,9 +921,9 @@ int sepkv_evict_window(const sepkv_params *p, void *Kc, void *Vc, const uint8_t 
     return launch_evict(*p, Kc, Vc, win_is_sep, sizes, ws, static_cast<hipStream_t>(stream));
 }
 
-static int fill_from_prefill(const sepkv_params *p, int L, int nw, const void *K, const void *V, const uint8_t *is_sep,
-                             const int32_t *sep_idx, int cap, const int32_t *sep_prefix, void *Kc, void *Vc,
-                             uint8_t *win_is_sep, int32_t *sizes, bool zero_rest, void *stream) {
+// what both forms of the hand-over look at; the outputs' alignment is each form's own
+static int check_fill(const sepkv_params *p, int L, int nw, const void *K, const void *V, const uint8_t *is_sep, const int32_t *sep_idx, int cap,
+                      const int32_t *sep_prefix, const void *Kc, const void *Vc, const uint8_t *win_is_sep, const int32_t *sizes) {
     int rc = check_kv(p);
     if (rc != SEPATTN_OK) return rc;
     if (!K || !V || !is_sep || !sep_idx || !sep_prefix || !Kc || !Vc || !win_is_sep || !sizes) return SEPATTN_ERR_NULL;
@@ -733,7 +931,16 @@ static int fill_from_prefill(const sepkv_params *p, int L, int nw, const void *K
     if (cap < 1) return SEPATTN_ERR_CAPACITY;
     const int n_init = p->a < L ? p->a : L;
     if (nw < 0 || nw > p->c - p->a - p->s || nw > L - n_init) return SEPATTN_ERR_PARAM;
-    if (!aligned(K, 16) || !aligned(V, 16) || !aligned(Kc, 16) || !aligned(Vc, 16)) return SEPATTN_ERR_PARAM;
+    if (!aligned(K, 16) || !aligned(V, 16)) return SEPATTN_ERR_PARAM;
+    return SEPATTN_OK;
+}
+
+static int fill_from_prefill(const sepkv_params *p, int L, int nw, const void *K, const void *V, const uint8_t *is_sep,
+                             const int32_t *sep_idx, int cap, const int32_t *sep_prefix, void *Kc, void *Vc,
+                             uint8_t *win_is_sep, int32_t *sizes, bool zero_rest, void *stream) {
+    const int rc = check_fill(p, L, nw, K, V, is_sep, sep_idx, cap, sep_prefix, Kc, Vc, win_is_sep, sizes);
+    if (rc != SEPATTN_OK) return rc;
+    if (!aligned(Kc, 16) || !aligned(Vc, 16)) return SEPATTN_ERR_PARAM;
     discard_stale_hip_error();
     return launch_cache_fill(*p, L, nw, K, V, is_sep, sep_idx, cap, sep_prefix, Kc, Vc, win_is_sep, sizes, zero_rest,
                              static_cast<hipStream_t>(stream));
@@ -750,6 +957,30 @@ int sepkv_fill_from_prefill_zeroed(const sepkv_params *p, int L, int nw, const v
                                    const int32_t *sep_prefix, void *Kc, void *Vc, uint8_t *win_is_sep,
                                    int32_t *sizes, void *stream) {
     return fill_from_prefill(p, L, nw, K, V, is_sep, sep_idx, cap, sep_prefix, Kc, Vc, win_is_sep, sizes, true, stream);
+}
+
+static int fill_from_prefill_fp4(const sepkv_params *p, int L, int nw, const void *K, const void *V, const uint8_t *is_sep, const int32_t *sep_idx,
+                                 int cap, const int32_t *sep_prefix, void *Kc, void *Ks, void *Vc, void *Vs, uint8_t *win_is_sep, int32_t *sizes,
+                                 bool zero_rest, void *stream) {
+    int rc = check_fill(p, L, nw, K, V, is_sep, sep_idx, cap, sep_prefix, Kc, Vc, win_is_sep, sizes);
+    if (rc == SEPATTN_OK) rc = check_fp4(p, Kc, Ks, Vc, Vs);
+    if (rc != SEPATTN_OK) return rc;
+    if (2L * p->S * p->Hkv > 65535L) return SEPATTN_ERR_SHAPE;  // second grid dimension
+    discard_stale_hip_error();
+    return launch_fill_fp4(*p, L, nw, K, V, is_sep, sep_idx, cap, sep_prefix, fp4_cache(Kc, Ks, Vc, Vs), win_is_sep, sizes, zero_rest,
+                           static_cast<hipStream_t>(stream));
+}
+
+int sepkv_fill_from_prefill_mx(const sepkv_params *p, int L, int nw, const void *K, const void *V, const uint8_t *is_sep, const int32_t *sep_idx,
+                                int cap, const int32_t *sep_prefix, void *Kc, void *Ks, void *Vc, void *Vs, uint8_t *win_is_sep, int32_t *sizes,
+                                void *stream) {
+    return fill_from_prefill_fp4(p, L, nw, K, V, is_sep, sep_idx, cap, sep_prefix, Kc, Ks, Vc, Vs, win_is_sep, sizes, false, stream);
+}
+
+int sepkv_fill_from_prefill_mx_zeroed(const sepkv_params *p, int L, int nw, const void *K, const void *V, const uint8_t *is_sep,
+                                       const int32_t *sep_idx, int cap, const int32_t *sep_prefix, void *Kc, void *Ks, void *Vc, void *Vs,
+                                       uint8_t *win_is_sep, int32_t *sizes, void *stream) {
+    return fill_from_prefill_fp4(p, L, nw, K, V, is_sep, sep_idx, cap, sep_prefix, Kc, Ks, Vc, Vs, win_is_sep, sizes, true, stream);
 }
 
 }  // extern "C"

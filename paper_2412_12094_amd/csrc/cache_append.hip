@@ -13,7 +13,7 @@
 // turns the query, which needs nothing of the cache.  One sequence, 32/8 heads, d = 128, bf16: 3.0 us, 64 sequences 4.1: one chain of
 // round trips (sizes, row, store) behind a launch; the bytes would take 0.3.
 #include "decode_common.h"
-#include "rotary.h"
+#include "norm.h"
 
 namespace sepattn {
 
@@ -58,38 +58,31 @@ __global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(
     }
 }
 
-// the new sizes and the window's flag
-__device__ inline void count_appended(const sepkv_params &p, const CacheMap &cm, long sq, bool is_sep, uint8_t *__restrict__ win_is_sep,
-                                      int32_t *__restrict__ sz) {
-    if (cm.n_init < p.a) {
-        sz[0] = cm.n_init + 1;
-    } else {
-        win_is_sep[sq * cm.wcap + win_index(cm, cm.n_past + cm.n_loc)] = is_sep ? 1 : 0;
-        const int over = (cm.n_loc + 1 > p.w) ? 1 : 0;
-        sz[2] = cm.n_past + over;
-        sz[3] = cm.n_loc + 1 - over;
-    }
-}
-
-template <typename T, PairLayout LAYOUT>
+// NORM: the rows of query and key are normed first (norm.h)
+template <typename T, int D, PairLayout LAYOUT, bool NORM>
 __global__ __launch_bounds__(kAppendThreads) void cache_append_rope_kernel(
-    sepkv_params p, int n_pairs, int log_groups, const double *__restrict__ freqs, const int32_t *__restrict__ positions, const T *q,
-    const T *__restrict__ k_new, const T *__restrict__ v_new, const uint8_t *__restrict__ is_sep_new, T *q_out, T *__restrict__ Kc,
+    sepkv_params p, int n_pairs, float eps, const double *__restrict__ freqs, const int32_t *__restrict__ positions, NormWeight q_weight,
+    NormWeight k_weight, const T *q, const T *__restrict__ k_new, const T *__restrict__ v_new, const uint8_t *__restrict__ is_sep_new, T *q_out, T *__restrict__ Kc,
     T *__restrict__ Vc, uint8_t *__restrict__ win_is_sep, int32_t *__restrict__ sizes) {
     const long sq = blockIdx.x;
-    const int group = threadIdx.x & ((1 << log_groups) - 1), row = threadIdx.x >> log_groups, rows = kAppendThreads >> log_groups;
-    constexpr int E = Angles<T, LAYOUT>::E;
-    const int half = p.d / 2;
+    constexpr int E = Angles<T, LAYOUT>::E, GROUPS = D / (2 * E), half = D / 2, rows = kAppendThreads / GROUPS;
+    const int group = threadIdx.x % GROUPS, row = threadIdx.x / GROUPS;
     const bool turned = has_turned<LAYOUT, E>(group, n_pairs);
-    const int t = positions[sq];
+    const int t = turned ? positions[sq] : 0;
     Angles<T, LAYOUT> w;
+    Weights<T, LAYOUT> weight;
+    auto change = [&](Pairs<T, LAYOUT> &x) {
+        if constexpr (NORM) norm_and_turn<T, LAYOUT, D, GROUPS>(x, weight, w, eps, turned, group, n_pairs);
+        else if (turned) x.turn(w, group, n_pairs, half);
+    };
     if (blockIdx.y == 1) {  // the query
+        if constexpr (NORM) weight.load(q_weight, group, n_pairs, half);
         if (turned) w.form(freqs, n_pairs, half, group, t, 1.f);
         for (int h = row; h < p.Hq; h += rows) {
             Pairs<T, LAYOUT> x;
-            x.load(q + (sq * p.Hq + h) * p.d, group, n_pairs, half);
-            if (turned) x.turn(w, group, n_pairs, half);
-            x.store(q_out + (sq * p.Hq + h) * p.d, group, n_pairs, half);
+            x.load(q + (sq * p.Hq + h) * D, group, n_pairs, half);
+            change(x);
+            x.store(q_out + (sq * p.Hq + h) * D, group, n_pairs, half);
         }
         return;
     }
@@ -101,14 +94,15 @@ __global__ __launch_bounds__(kAppendThreads) void cache_append_rope_kernel(
     if (cm.n_init < p.a) slot = cm.n_init;
     else if (u < cm.wcap) slot = p.a + p.s + win_index(cm, u);
     else return;  // window region full (uniform over the workgroup)
+    if constexpr (NORM) weight.load(k_weight, group, n_pairs, half);
     if (turned) w.form(freqs, n_pairs, half, group, t, 1.f);
     for (int i = row; i < 2 * p.Hkv; i += rows) {
         const bool value = i >= p.Hkv;
         const int h = value ? i - p.Hkv : i;
         Pairs<T, LAYOUT> x;
-        x.load((value ? v_new : k_new) + (sq * p.Hkv + h) * p.d, group, n_pairs, half);
-        if (turned && !value) x.turn(w, group, n_pairs, half);
-        x.store((value ? Vc : Kc) + ((sq * p.Hkv + h) * p.c + slot) * p.d, group, n_pairs, half);
+        x.load((value ? v_new : k_new) + (sq * p.Hkv + h) * D, group, n_pairs, half);
+        if (!value) change(x);
+        x.store((value ? Vc : Kc) + ((sq * p.Hkv + h) * p.c + slot) * D, group, n_pairs, half);
     }
     if (threadIdx.x == 0) count_appended(p, cm, sq, is_sep_new[sq], win_is_sep, sz);
 }
@@ -126,27 +120,32 @@ int launch_cache_append(const sepkv_params &p, const void *k_new, const void *v_
     return launch_status();
 }
 
-int launch_cache_append_rope(const sepkv_params &p, int rotary_dim, int interleaved, const double *freqs, const int32_t *positions,
-                             const void *q, const void *k_new, const void *v_new, const uint8_t *is_sep_new, void *q_out, void *Kc,
-                             void *Vc, uint8_t *win_is_sep, int32_t *sizes, hipStream_t st) {
-    const int groups = p.d * (p.dtype == SEPATTN_BF16 ? 2 : 4) / 32;
-    int log_groups = 0;
-    while ((1 << log_groups) < groups) ++log_groups;
+int launch_cache_append_rope(const sepkv_params &p, const TokenTurn &turn, const void *q, const void *k_new, const void *v_new,
+                             const uint8_t *is_sep_new, void *q_out, void *Kc, void *Vc, uint8_t *win_is_sep, int32_t *sizes, hipStream_t st) {
     ProfScope prof(SEPATTN_K_CACHE_APPEND, st);
-    auto go = [&](auto T_) {
+    auto go = [&](auto T_, auto D_) {
         using T = decltype(T_);
-        const int layout = pair_layout<T>(rotary_dim, interleaved);
-#define APPEND(LAYOUT)                                                                                                               \
-    hipLaunchKernelGGL((cache_append_rope_kernel<T, LAYOUT>), dim3(p.S, 2), dim3(kAppendThreads), 0, st, p, rotary_dim / 2, log_groups, \
-                       freqs, positions, static_cast<const T *>(q), static_cast<const T *>(k_new), static_cast<const T *>(v_new),    \
-                       is_sep_new, static_cast<T *>(q_out), static_cast<T *>(Kc), static_cast<T *>(Vc), win_is_sep, sizes)
-        if (layout == kNeighbours) APPEND(kNeighbours);
-        else if (layout == kHalves) APPEND(kHalves);
-        else APPEND(kHalvesOdd);
+        constexpr int D = decltype(D_)::value;
+        const int layout = pair_layout<T>(turn.rotary_dim, turn.interleaved);
+#define APPEND(LAYOUT, NORM)                                                                                                          \
+    hipLaunchKernelGGL((cache_append_rope_kernel<T, D, LAYOUT, NORM>), dim3(p.S, 2), dim3(kAppendThreads), 0, st, p, turn.rotary_dim / 2, turn.eps, \
+                       turn.freqs, turn.positions, turn.q_weight, turn.k_weight, static_cast<const T *>(q), static_cast<const T *>(k_new),          \
+                       static_cast<const T *>(v_new), is_sep_new, static_cast<T *>(q_out), static_cast<T *>(Kc), static_cast<T *>(Vc), win_is_sep, sizes)
+        if (turn.norm) {
+            if (layout == kNeighbours) APPEND(kNeighbours, true);
+            else if (layout == kHalves) APPEND(kHalves, true);
+            else APPEND(kHalvesOdd, true);
+        } else {
+            if (layout == kNeighbours) APPEND(kNeighbours, false);
+            else if (layout == kHalves) APPEND(kHalves, false);
+            else APPEND(kHalvesOdd, false);
+        }
 #undef APPEND
     };
-    if (p.dtype == SEPATTN_BF16) go(uint16_t{});
-    else go(float{});
+    using D64 = std::integral_constant<int, 64>;
+    using D128 = std::integral_constant<int, 128>;
+    if (p.dtype == SEPATTN_BF16) p.d == 64 ? go(uint16_t{}, D64{}) : go(uint16_t{}, D128{});
+    else p.d == 64 ? go(float{}, D64{}) : go(float{}, D128{});
     return launch_status();
 }
 

@@ -162,6 +162,30 @@ int launch_rope(const sepattn_rope_params &p, const double *freqs, const int32_t
                 const void *const (&src)[3], const sepattn_strides (&from)[3], void *const (&dst)[3], const sepattn_strides (&to)[3],
                 bool backward, hipStream_t st);
 
+// ---- norms in front of them ------------------------------------------------------------------------
+struct NormWeight {
+    const void *w;  // DEVICE [d], or nullptr: ones
+    int dtype;      // SEPATTN_BF16 or SEPATTN_FP32
+};
+struct NormRopeTensors {  // q, k, v; heads[2] = 0: no values
+    const void *src[3], *grad[3];  // grad: the backward's dQ, dK, dV; src: the rows in front of the norm
+    void *dst[3];
+    sepattn_strides from[3], grad_strides[3], to[3];
+    int heads[3];
+    NormWeight weight[2];
+};
+struct NormRopeGrid {  // how a backward call is cut
+    int B, log_tokens, tiles_per_row;  // tiles of 1 << log_tokens tokens
+    int chunk, chunks[3];              // heads per workgroup; chunks of q, k, v
+    int walkers;                       // workgroups that share a chunk's tiles
+};
+NormRopeGrid norm_rope_grid(const sepattn_norm_rope_params &p, bool values, int units);
+size_t norm_rope_backward_workspace(const sepattn_norm_rope_params &p);
+int launch_norm_rope(const sepattn_norm_rope_params &p, const double *freqs, const int32_t *positions, const int32_t *doc_start,
+                     const NormRopeTensors &x, hipStream_t st);
+int launch_norm_rope_backward(const sepattn_norm_rope_params &p, const double *freqs, const int32_t *positions, const int32_t *doc_start,
+                              const NormRopeTensors &x, float *dq_weight, float *dk_weight, float *part, hipStream_t st);
+
 // ---- streaming cache ---------------------------------------------------------------------------
 int check_kv_params(const sepkv_params *p);  // host validation shared by every cache call
 size_t decode_workspace(const sepkv_params &p);
@@ -173,14 +197,36 @@ int launch_decode(const sepkv_params &p, const void *q, const void *Kc, const vo
 int launch_rope_table(int n_pos, int d, double base, const double *freqs, float *table, hipStream_t st);
 int launch_cache_append(const sepkv_params &p, const void *k_new, const void *v_new, const uint8_t *is_sep_new,
                         void *Kc, void *Vc, uint8_t *win_is_sep, int32_t *sizes, hipStream_t st);
-int launch_cache_append_rope(const sepkv_params &p, int rotary_dim, int interleaved, const double *freqs, const int32_t *positions,
-                             const void *q, const void *k_new, const void *v_new, const uint8_t *is_sep_new, void *q_out, void *Kc,
-                             void *Vc, uint8_t *win_is_sep, int32_t *sizes, hipStream_t st);
+// what happens to a token's query and key on their way into the cache
+struct TokenTurn {
+    int rotary_dim, interleaved;
+    const double *freqs;
+    const int32_t *positions;
+    bool norm;  // normed first, with eps and the weights
+    float eps;
+    NormWeight q_weight, k_weight;
+};
+int launch_cache_append_rope(const sepkv_params &p, const TokenTurn &turn, const void *q, const void *k_new, const void *v_new,
+                             const uint8_t *is_sep_new, void *q_out, void *Kc, void *Vc, uint8_t *win_is_sep, int32_t *sizes, hipStream_t st);
 int launch_rope_cache(const sepkv_params &p, const int32_t *sizes, const float *rope, int n_pos, const void *Kc, void *K_out, hipStream_t st);
 int launch_group_sequences(const int32_t *prefix_of, int S, int G, int32_t *group_start, int32_t *group_seq, hipStream_t st);
 size_t evict_workspace(const sepkv_params &p);
 int launch_evict(const sepkv_params &p, void *Kc, void *Vc, const uint8_t *win_is_sep, int32_t *sizes,
                  void *ws, hipStream_t st);
+// ---- the cache in 4 bits ----
+struct Fp4Cache {  // codes [S, Hkv, c, d/2] and scale bytes [S, Hkv, c, d/32] of keys and values
+    uint8_t *Kc, *Ks, *Vc, *Vs;
+};
+int launch_fill_fp4(const sepkv_params &p, int L, int nw, const void *K, const void *V, const uint8_t *is_sep, const int32_t *sep_idx, int cap,
+                    const int32_t *sep_prefix, const Fp4Cache &cache, uint8_t *win_is_sep, int32_t *sizes, bool zero_rest, hipStream_t st);
+// turn: nullptr for a token that enters as it is (no query then)
+int launch_append_fp4(const sepkv_params &p, const TokenTurn *turn, const void *q, const void *k_new, const void *v_new, const uint8_t *is_sep_new,
+                      void *q_out, const Fp4Cache &cache, uint8_t *win_is_sep, int32_t *sizes, hipStream_t st);
+int launch_expand_fp4(const sepkv_params &p, const int32_t *sizes, const Fp4Cache &cache, void *K, void *V, hipStream_t st);
+int launch_evict_fp4(const sepkv_params &p, const Fp4Cache &cache, const uint8_t *win_is_sep, int32_t *sizes, hipStream_t st);
+size_t decode_fp4_workspace(const sepkv_params &p);
+int launch_decode_fp4(const sepkv_params &p, const void *q, const Fp4Cache &cache, const int32_t *sizes, const float *rope, int n_pos, void *out,
+                      float *lse, void *ws, hipStream_t st);
 // ---- shared prefixes ----
 struct SharedDecode {  // arguments of one call
     sepkv_params p, pp;

@@ -53,6 +53,19 @@ __device__ inline int rank_of_slot(const CacheMap &m, int slot) {
     return e < m.n_past + m.n_loc ? m.n_init + m.n_sep + e : -1;
 }
 
+// the new sizes and the window's flag
+__device__ inline void count_appended(const sepkv_params &p, const CacheMap &cm, long sq, bool is_sep, uint8_t *__restrict__ win_is_sep,
+                                      int32_t *__restrict__ sz) {
+    if (cm.n_init < p.a) {
+        sz[0] = cm.n_init + 1;
+    } else {
+        win_is_sep[sq * cm.wcap + win_index(cm, cm.n_past + cm.n_loc)] = is_sep ? 1 : 0;
+        const int over = (cm.n_loc + 1 > p.w) ? 1 : 0;
+        sz[2] = cm.n_past + over;
+        sz[3] = cm.n_loc + 1 - over;
+    }
+}
+
 __device__ inline uint16_t decode_f32_to_bf16(float f) {
     uint32_t u = __float_as_uint(f);
     u += 0x7FFFu + ((u >> 16) & 1u);

@@ -17,6 +17,8 @@
 //   sizes: one workgroup per sequence counts the kept entries again and writes the new `sizes`
 //          row.  It runs after the move kernel (stream order), so no workgroup of the move kernel
 //          can see the new values.  The window flags stay where they are (they move with the head).
+#include <type_traits>
+
 #include "decode_common.h"
 
 namespace sepattn {
@@ -60,12 +62,17 @@ __device__ inline int count_kept(const CacheMap &cm, const uint8_t *__restrict__
     return k;
 }
 
-// rows are moved as 16-byte pieces; row16 = pieces per row
+// rows are moved as 16-byte pieces; row16 = pieces per row.  SCALE: the scale bytes of a row of 4-bit codes, which go with its first piece
+// (uint4: there are none)
+template <typename SCALE>
 __global__ __launch_bounds__(kEvictThreads) void evict_move_kernel(sepkv_params p, int row16,
                                                                    uint4 *__restrict__ Kc,
                                                                    uint4 *__restrict__ Vc,
+                                                                   SCALE *__restrict__ Ks,
+                                                                   SCALE *__restrict__ Vs,
                                                                    const uint8_t *__restrict__ win_is_sep,
                                                                    const int32_t *__restrict__ sizes) {
+    constexpr bool kScales = !std::is_same_v<SCALE, uint4>;
     constexpr int kUnroll = 8;
     __shared__ int wave_cnt[kEvictWaves];
     __shared__ int32_t kept[kChunk];
@@ -81,6 +88,7 @@ __global__ __launch_bounds__(kEvictThreads) void evict_move_kernel(sepkv_params 
     const int k = count_kept(cm, fl, P, wave_cnt);
     const EvictPlan pl = evict_plan(p, cm, k);
     uint4 *base = (which ? Vc : Kc) + ((long)sq * p.Hkv + kv) * (long)p.c * row16;
+    SCALE *scales = kScales ? (which ? Vs : Ks) + ((long)sq * p.Hkv + kv) * (long)p.c : nullptr;
     const int rows_per_pass = kEvictThreads / row16;  // row16 divides 256 for d in {64,128}, both dtypes
     const int r_in = threadIdx.x / row16, piece = threadIdx.x % row16;
     int rank0 = 0;  // kept entries before the chunk
@@ -118,10 +126,12 @@ __global__ __launch_bounds__(kEvictThreads) void evict_move_kernel(sepkv_params 
         const int skip = max(pl.first - rank0, 0);
         for (int r0 = skip; r0 < in_chunk; r0 += rows_per_pass * kUnroll) {
             uint4 v[kUnroll];
+            SCALE sc[kUnroll];
 #pragma unroll
             for (int u = 0; u < kUnroll; ++u) {
                 const int r = r0 + u * rows_per_pass + r_in;
                 if (r < in_chunk) v[u] = base[(long)(p.a + p.s + kept[r]) * row16 + piece];
+                if (kScales && r < in_chunk && piece == 0) sc[u] = scales[p.a + p.s + kept[r]];
             }
 #pragma unroll
             for (int u = 0; u < kUnroll; ++u) {
@@ -130,6 +140,7 @@ __global__ __launch_bounds__(kEvictThreads) void evict_move_kernel(sepkv_params 
                     int t = pl.dst0 + (rank0 + r - pl.first);
                     if (t >= p.s) t -= p.s;
                     base[(long)(p.a + t) * row16 + piece] = v[u];
+                    if (kScales && piece == 0) scales[p.a + t] = sc[u];
                 }
             }
         }
@@ -161,19 +172,40 @@ __global__ __launch_bounds__(kEvictThreads) void evict_sizes_kernel(sepkv_params
 // the step needs no scratch memory; the query stays in the interface and answers 0
 size_t evict_workspace(const sepkv_params &) { return 0; }
 
+namespace {
+
+// the sizes follow in a launch of their own
+int evict_sizes(const sepkv_params &p, const uint8_t *win_is_sep, int32_t *sizes, hipStream_t st) {
+    if (hipGetLastError() != hipSuccess) return SEPATTN_ERR_HIP;
+    ProfScope prof(SEPATTN_K_EVICT_SIZES, st);
+    hipLaunchKernelGGL(evict_sizes_kernel, dim3(p.S), dim3(kEvictThreads), 0, st, p, win_is_sep, sizes);
+    return launch_status();
+}
+
+}  // namespace
+
 int launch_evict(const sepkv_params &p, void *Kc, void *Vc, const uint8_t *win_is_sep, int32_t *sizes,
                  void *, hipStream_t st) {
     int elem = (p.dtype == SEPATTN_BF16) ? 2 : 4;
     int row16 = p.d * elem / 16;
     {
         ProfScope prof(SEPATTN_K_EVICT_MOVE, st);
-        hipLaunchKernelGGL(evict_move_kernel, dim3(p.S * p.Hkv * 2), dim3(kEvictThreads), 0, st, p, row16,
-                           (uint4 *)Kc, (uint4 *)Vc, win_is_sep, sizes);
+        hipLaunchKernelGGL(evict_move_kernel<uint4>, dim3(p.S * p.Hkv * 2), dim3(kEvictThreads), 0, st, p, row16,
+                           (uint4 *)Kc, (uint4 *)Vc, nullptr, nullptr, win_is_sep, sizes);
     }
-    if (hipGetLastError() != hipSuccess) return SEPATTN_ERR_HIP;
-    ProfScope prof(SEPATTN_K_EVICT_SIZES, st);
-    hipLaunchKernelGGL(evict_sizes_kernel, dim3(p.S), dim3(kEvictThreads), 0, st, p, win_is_sep, sizes);
-    return launch_status();
+    return evict_sizes(p, win_is_sep, sizes, st);
+}
+
+int launch_evict_fp4(const sepkv_params &p, const Fp4Cache &cache, const uint8_t *win_is_sep, int32_t *sizes, hipStream_t st) {
+    auto go = [&](auto SCALE_) {
+        using SCALE = decltype(SCALE_);
+        ProfScope prof(SEPATTN_K_EVICT_MOVE, st);
+        hipLaunchKernelGGL(evict_move_kernel<SCALE>, dim3(p.S * p.Hkv * 2), dim3(kEvictThreads), 0, st, p, p.d / 32, (uint4 *)cache.Kc, (uint4 *)cache.Vc,
+                           (SCALE *)cache.Ks, (SCALE *)cache.Vs, win_is_sep, sizes);
+    };
+    if (p.d == 128) go(uint32_t{});  // four blocks of 32 a row
+    else go(uint16_t{});
+    return evict_sizes(p, win_is_sep, sizes, st);
 }
 
 }  // namespace sepattn

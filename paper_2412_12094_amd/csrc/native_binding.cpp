@@ -40,11 +40,18 @@ namespace {
 #define LIB_POSITION_FUNCTIONS(P)                                                                                      \
     P(sepattn_rope) P(sepattn_rope_backward) P(sepkv_append_rope) P(sepkv_group_sequences) P(sepkv_rope_cache)          \
     P(sepattn_decode_shared_workspace_bytes) P(sepattn_decode_shared) P(sepattn_decode_shared_rope)
+// norms in front of them, the cache in 4 bits
+#define LIB_NORM_FP4_FUNCTIONS(N)                                                                                      \
+    N(sepattn_norm_rope) N(sepattn_norm_rope_backward_workspace_bytes) N(sepattn_norm_rope_backward) N(sepkv_append_norm_rope) \
+    N(sepkv_fill_from_prefill_mx) N(sepkv_fill_from_prefill_mx_zeroed) N(sepkv_append_mx) N(sepkv_append_rope_mx)      \
+    N(sepkv_append_norm_rope_mx) N(sepkv_evict_window_mx) N(sepkv_expand_mx) N(sepattn_decode_mx_workspace_bytes)      \
+    N(sepattn_decode_mx) N(sepattn_decode_rope_mx)
 struct Lib {
 #define X(name) decltype(&::name) name;
     LIB_FUNCTIONS(X)
     LIB_FRESH_FUNCTIONS(X)
     LIB_POSITION_FUNCTIONS(X)
+    LIB_NORM_FP4_FUNCTIONS(X)
 #undef X
 } lib;
 PyObject *g_raise = nullptr;  // Python callable: raises SepattnError(function, status)
@@ -617,6 +624,27 @@ const double *freqs_arg(const at::Tensor &f) {
     return static_cast<const double *>(f.data_ptr());
 }
 
+// three outputs, the caller's, of the shapes of `like` (r[i].from)
+template <int N>
+void rows_out(const Out<N> &out, Rows (&r)[3]) {
+    for (int i = 0; out.given() && i < 3; ++i) {
+        if (!r[i].from.defined()) {
+            require(out[i] == Py_None, "out: no values were given");
+            continue;
+        }
+        r[i].to = rows_arg(out[i]);
+        require(r[i].to.sizes() == r[i].from.sizes() && r[i].to.scalar_type() == r[i].from.scalar_type(), "out: shapes and dtype of the inputs");
+    }
+}
+// as one fused projection puts them out: [B, L, q heads | k heads | v heads, d]
+void fused_rows(Rows (&r)[3], const at::Tensor &q, int B, int L, int Hq, int Hkv, int64_t d) {
+    const int64_t Hv = r[2].from.defined() ? Hkv : 0;
+    const at::Tensor dx = empty({B, L, Hq + Hkv + Hv, d}, q.scalar_type(), q.device());
+    const at::AutoDispatchBelowADInplaceOrView plain;
+    const int64_t l = (Hq + Hkv + Hv) * d, first[3] = {0, Hq * d, (Hq + Hkv) * d};
+    for (int i = 0; i < (Hv ? 3 : 2); ++i) r[i].to = dx.as_strided({B, i == 0 ? Hq : Hkv, L, d}, {L * l, d, l, 1}, first[i]);
+}
+
 // rope(q, k, v, freqs, positions, doc_start, interleaved, out)
 template <bool BACKWARD>
 PyObject *rope(PyObject *const *a) {
@@ -639,25 +667,13 @@ PyObject *rope(PyObject *const *a) {
     p.interleaved = as_bool(a[6]);
     p.dtype = dtype_code(q);
     const Out<3> out(a[7]);
-    for (int i = 0; out.given() && i < 3; ++i) {
-        if (!r[i].from.defined()) {
-            require(out[i] == Py_None, "out: no values were given");
-            continue;
-        }
-        r[i].to = rows_arg(out[i]);
-        require(r[i].to.sizes() == r[i].from.sizes() && r[i].to.scalar_type() == r[i].from.scalar_type(), "out: shapes and dtype of the inputs");
-    }
+    rows_out(out, r);
     one_device(q, k, v, f, pos, doc, r[0].to, r[1].to, r[2].to);
     check(BACKWARD ? "sepattn_rope_backward" : "sepattn_rope", unlocked([&] {
               const c10::DeviceGuard guard(q.device());
               if (!out.given()) {
-                  if constexpr (BACKWARD) {  // as one fused projection puts them out: [B, L, q heads | k heads | v heads, d]
-                      const int64_t Hv = v.defined() ? p.Hkv : 0;
-                      const at::Tensor dx = empty({p.B, p.L, p.Hq + p.Hkv + Hv, p.d}, q.scalar_type(), q.device());
-                      const at::AutoDispatchBelowADInplaceOrView plain;
-                      const int64_t d = p.d, l = (p.Hq + p.Hkv + Hv) * d, first[3] = {0, p.Hq * d, (p.Hq + p.Hkv) * d};
-                      for (int i = 0; i < (v.defined() ? 3 : 2); ++i)
-                          r[i].to = dx.as_strided({p.B, i == 0 ? p.Hq : p.Hkv, p.L, p.d}, {p.L * l, d, l, 1}, first[i]);
+                  if constexpr (BACKWARD) {
+                      fused_rows(r, q, p.B, p.L, p.Hq, p.Hkv, p.d);
                   } else {
                       for (Rows &x : r)
                           if (x.from.defined()) x.to = fresh_like(x.from);
@@ -673,36 +689,342 @@ PyObject *rope(PyObject *const *a) {
     return tuple_of(wrap(r[0].to), wrap(r[1].to), v.defined() ? wrap(r[2].to) : keep(Py_None));
 }
 
-// append_rope(q, k_new, v_new, is_sep_new, positions, freqs, Kc, Vc, win_is_sep, sizes, a, s, w, interleaved, out)
-PyObject *append_rope(PyObject *const *a) {
-    const at::Tensor &q = dev(a[0]), &k = dev(a[1]), &v = dev(a[2]), &sep = dev(a[3]), &pos = dev(a[4]), &f = dev(a[5]), &Kc = dev(a[6]),
-                     &Vc = dev(a[7]), &flags = dev(a[8]);
-    const at::Tensor &sizes = sizes_arg(a[9]);
-    if (q.dim() != 3) fail(PyExc_ValueError, "q [S,Hq,d] is expected");
-    const sepkv_params p = kv_params(Kc, (int)q.size(0), (int)q.size(1), as_int(a[10]), as_int(a[11]), as_int(a[12]), 1.0f);
-    const int64_t want[3] = {p.S, p.Hkv, p.d};
-    require(k.sizes() == c10::IntArrayRef(want, 3) && v.sizes() == k.sizes() && k.scalar_type() == Kc.scalar_type() &&
-                v.scalar_type() == Kc.scalar_type(), "k_new, v_new: [S, Hkv, d] in the cache's dtype");
-    require(q.size(2) == p.d && q.scalar_type() == Kc.scalar_type(), "q: [S, Hq, d] in the cache's dtype");
-    require(Kc.size(0) == p.S && Vc.sizes() == Kc.sizes() && Vc.scalar_type() == Kc.scalar_type(), "Kc, Vc: [S, Hkv, c, d] of one dtype");
-    require(sep.scalar_type() == at::kByte && flags.scalar_type() == at::kByte && sep.numel() == p.S && flags.dim() == 2 &&
-                flags.size(0) == p.S && flags.size(1) == (int64_t)p.c - p.a - p.s, "is_sep_new: uint8 [S], win_is_sep: uint8 [S, c-a-s]");
-    require(pos.scalar_type() == at::kInt && pos.dim() == 1 && pos.size(0) == p.S && sizes.size(0) == p.S, "positions: int32 [S], sizes: int32 [S, 6]");
-    const double *freqs = freqs_arg(f);
-    const int rotary_dim = (int)(2 * f.numel()), interleaved = as_bool(a[13]);
-    at::Tensor o;
-    if (a[14] != Py_None) {
-        o = dev(a[14]);
-        require(o.sizes() == q.sizes() && o.scalar_type() == q.scalar_type(), "out: like q");
+// How a token's query and key are changed on their way into a cache: arguments positions, [q_weight, k_weight,] freqs[, eps]
+struct Turn {
+    at::Tensor pos, qw, kw, f;
+    const double *freqs = nullptr;
+    int rotary_dim = 0, weight_dtype = SEPATTN_FP32;
+    float eps = 0.f;
+    const int32_t *positions() const { return (const int32_t *)ptr_or_null(pos); }
+};
+// weights [d] of one dtype, each may be None
+void weights_arg(Turn &t, PyObject *q, PyObject *k, int64_t d) {
+    t.qw = dev_or_none(q), t.kw = dev_or_none(k);
+    for (const at::Tensor *w : {&t.qw, &t.kw}) {
+        if (!w->defined()) continue;
+        require(w->dim() == 1 && w->size(0) == d, "q_weight, k_weight: [d]");
+        t.weight_dtype = dtype_code(*w);
     }
-    one_device(q, k, v, sep, pos, f, Kc, Vc, flags, sizes, o);
-    check("sepkv_append_rope", unlocked([&] {
-              const c10::DeviceGuard guard(q.device());
-              if (!o.defined()) o = fresh_like(q);
-              return lib.sepkv_append_rope(&p, rotary_dim, interleaved, freqs, i32(pos), ptr(q), ptr(k), ptr(v), (const uint8_t *)ptr(sep), ptr(o),
-                                           ptr(Kc), ptr(Vc), (uint8_t *)ptr(flags), (int32_t *)ptr(sizes), stream_of(q));
+    require(!t.qw.defined() || !t.kw.defined() || t.qw.scalar_type() == t.kw.scalar_type(), "q_weight, k_weight: one dtype");
+}
+
+// What the forms of a token's append share: its tensors, those of the cache's bookkeeping, and the turned query.
+struct Token {
+    at::Tensor q, k, v, sep, flags, sizes, out;
+    PyObject *out_arg;
+    Token(PyObject *q_, PyObject *k_, PyObject *v_, PyObject *sep_, PyObject *flags_, PyObject *sizes_, PyObject *out_)
+        : q(q_ ? dev(q_) : at::Tensor()), k(dev(k_)), v(dev(v_)), sep(dev(sep_)), flags(dev(flags_)), sizes(sizes_arg(sizes_)), out_arg(out_) {
+        if (q_ && q.dim() != 3) fail(PyExc_ValueError, "q [S,Hq,d] is expected");
+    }
+    // `type`: of all rows
+    void match(const sepkv_params &p, at::ScalarType type) {
+        const int64_t want[3] = {p.S, p.Hkv, p.d};
+        require(k.sizes() == c10::IntArrayRef(want, 3) && v.sizes() == k.sizes() && k.scalar_type() == type && v.scalar_type() == type,
+                "k_new, v_new: [S, Hkv, d] in the cache's dtype");
+        require(!q.defined() || (q.size(2) == p.d && q.scalar_type() == type), "q: [S, Hq, d] in the cache's dtype");
+        require(sep.scalar_type() == at::kByte && flags.scalar_type() == at::kByte && sep.numel() == p.S && flags.dim() == 2 &&
+                    flags.size(0) == p.S && flags.size(1) == (int64_t)p.c - p.a - p.s, "is_sep_new: uint8 [S], win_is_sep: uint8 [S, c-a-s]");
+        require(sizes.size(0) == p.S, "sizes: int32 [S, 6]");
+        if (!out_arg || out_arg == Py_None) return;
+        out = dev(out_arg);
+        require(out.sizes() == q.sizes() && out.scalar_type() == q.scalar_type(), "out: like q");
+    }
+    void match_turn(const Turn &t, const sepkv_params &p) const {
+        require(!t.pos.defined() || (t.pos.scalar_type() == at::kInt && t.pos.dim() == 1 && t.pos.size(0) == p.S), "positions: int32 [S]");
+    }
+    void allocate() {
+        if (!out.defined()) out = fresh_like(q);
+    }
+    PyObject *result() { return out_arg == Py_None ? wrap(std::move(out)) : keep(out_arg); }
+    const uint8_t *is_sep() const { return (const uint8_t *)ptr(sep); }
+    uint8_t *win() const { return (uint8_t *)ptr(flags); }
+    int32_t *sz() const { return (int32_t *)ptr(sizes); }
+};
+// the frequencies, and with NORM eps and the weights in front of them
+template <bool NORM>
+Turn turn_args(PyObject *positions, PyObject *q_weight, PyObject *k_weight, PyObject *freqs, PyObject *eps, int64_t d) {
+    Turn t;
+    t.pos = NORM ? dev_or_none(positions) : at::Tensor(dev(positions));
+    t.f = NORM ? dev_or_none(freqs) : at::Tensor(dev(freqs));
+    if (t.f.defined()) {
+        t.freqs = freqs_arg(t.f);
+        t.rotary_dim = (int)(2 * t.f.numel());
+    }
+    if (NORM) {
+        weights_arg(t, q_weight, k_weight, d);
+        t.eps = as_float(eps);
+    }
+    return t;
+}
+
+// append_rope(q, k_new, v_new, is_sep_new, positions, freqs, Kc, Vc, win_is_sep, sizes, a, s, w, interleaved, out)
+// append_norm_rope(q, k_new, v_new, is_sep_new, positions, q_weight, k_weight, freqs, eps, Kc, Vc, win_is_sep, sizes, a, s, w, interleaved, out)
+template <bool NORM>
+PyObject *append_turned(PyObject *const *a) {
+    PyObject *const *b = a + (NORM ? 9 : 6);  // the cache and what follows
+    Token x(a[0], a[1], a[2], a[3], b[2], b[3], b[8]);
+    const at::Tensor &Kc = dev(b[0]), &Vc = dev(b[1]);
+    const sepkv_params p = kv_params(Kc, (int)x.q.size(0), (int)x.q.size(1), as_int(b[4]), as_int(b[5]), as_int(b[6]), 1.0f);
+    x.match(p, Kc.scalar_type());
+    require(Kc.size(0) == p.S && Vc.sizes() == Kc.sizes() && Vc.scalar_type() == Kc.scalar_type(), "Kc, Vc: [S, Hkv, c, d] of one dtype");
+    const Turn t = turn_args<NORM>(a[4], NORM ? a[5] : nullptr, NORM ? a[6] : nullptr, a[NORM ? 7 : 5], NORM ? a[8] : nullptr, p.d);
+    x.match_turn(t, p);
+    const int interleaved = as_bool(b[7]);
+    one_device(x.q, x.k, x.v, x.sep, t.pos, t.f, t.qw, t.kw, Kc, Vc, x.flags, x.sizes, x.out);
+    check(NORM ? "sepkv_append_norm_rope" : "sepkv_append_rope", unlocked([&] {
+              const c10::DeviceGuard guard(x.q.device());
+              x.allocate();
+              if constexpr (NORM)
+                  return lib.sepkv_append_norm_rope(&p, t.rotary_dim, interleaved, t.eps, t.weight_dtype, ptr_or_null(t.qw), ptr_or_null(t.kw), t.freqs,
+                                                    t.positions(), ptr(x.q), ptr(x.k), ptr(x.v), x.is_sep(), ptr(x.out), ptr(Kc), ptr(Vc), x.win(),
+                                                    x.sz(), stream_of(x.q));
+              else
+                  return lib.sepkv_append_rope(&p, t.rotary_dim, interleaved, t.freqs, t.positions(), ptr(x.q), ptr(x.k), ptr(x.v), x.is_sep(),
+                                               ptr(x.out), ptr(Kc), ptr(Vc), x.win(), x.sz(), stream_of(x.q));
           }));
-    return a[14] == Py_None ? wrap(std::move(o)) : keep(a[14]);
+    return x.result();
+}
+
+// ---- norms in front of the rotary positions --------------------------------------------------------
+// What forward and backward share: q, k (and v, or the three gradients) with weights, frequencies and positions
+struct NormRope {
+    Turn t;
+    at::Tensor doc;
+    sepattn_norm_rope_params p;
+    NormRope(const at::Tensor &q, const at::Tensor &k, const at::Tensor &v, PyObject *q_weight, PyObject *k_weight, PyObject *freqs, PyObject *eps,
+             PyObject *positions, PyObject *doc_start, PyObject *interleaved) {
+        t = turn_args<true>(positions, q_weight, k_weight, freqs, eps, q.size(3));
+        doc = dev_or_none(doc_start);
+        const int64_t want[4] = {q.size(0), k.size(1), q.size(2), q.size(3)};
+        require(k.sizes() == c10::IntArrayRef(want, 4) && (!v.defined() || v.sizes() == k.sizes()) && k.scalar_type() == q.scalar_type() &&
+                    (!v.defined() || v.scalar_type() == q.scalar_type()), "q [B, Hq, L, d], k and v [B, Hkv, L, d] of one dtype");
+        for (const at::Tensor *x : {&t.pos, &doc})
+            require(!x->defined() || (x->scalar_type() == at::kInt && x->dim() == 2 && x->size(0) == q.size(0) && x->size(1) == q.size(2)),
+                    "positions, doc_start: int32 [B, L]");
+        p.B = (int)q.size(0), p.Hq = (int)q.size(1), p.Hkv = (int)k.size(1), p.L = (int)q.size(2), p.d = (int)q.size(3);
+        p.rotary_dim = t.rotary_dim, p.interleaved = as_bool(interleaved), p.dtype = dtype_code(q), p.weight_dtype = t.weight_dtype, p.eps = t.eps;
+    }
+    const int32_t *doc_start() const { return (const int32_t *)ptr_or_null(doc); }
+};
+// norm_rope(q, k, v, q_weight, k_weight, freqs, eps, positions, doc_start, interleaved, out)
+PyObject *norm_rope(PyObject *const *a) {
+    Rows r[3];
+    for (int i = 0; i < 3; ++i)
+        if (i < 2 || a[i] != Py_None) r[i].from = rows_arg(a[i]);
+    const at::Tensor &q = r[0].from, &k = r[1].from, &v = r[2].from;
+    const NormRope n(q, k, v, a[3], a[4], a[5], a[6], a[7], a[8], a[9]);
+    const Out<3> out(a[10]);
+    rows_out(out, r);
+    one_device(q, k, v, n.t.f, n.t.qw, n.t.kw, n.t.pos, n.doc, r[0].to, r[1].to, r[2].to);
+    check("sepattn_norm_rope", unlocked([&] {
+              const c10::DeviceGuard guard(q.device());
+              for (Rows &x : r) {
+                  if (!out.given() && x.from.defined()) x.to = fresh_like(x.from);
+                  x.finish();
+              }
+              return lib.sepattn_norm_rope(&n.p, ptr_or_null(n.t.qw), ptr_or_null(n.t.kw), n.t.freqs, n.t.positions(), n.doc_start(), ptr(q), r[0].from_s(),
+                                           ptr(k), r[1].from_s(), ptr_or_null(v), r[2].from_s(), ptr(r[0].to), r[0].to_s(), ptr(r[1].to), r[1].to_s(),
+                                           ptr_or_null(r[2].to), r[2].to_s(), stream_of(q));
+          }));
+    if (out.given()) return tuple_of(keep(out[0]), keep(out[1]), keep(out[2]));
+    return tuple_of(wrap(r[0].to), wrap(r[1].to), v.defined() ? wrap(r[2].to) : keep(Py_None));
+}
+
+// norm_rope_backward(q, k, dQ, dK, dV, q_weight, k_weight, freqs, eps, positions, doc_start, interleaved, out, out_weights, ws)
+PyObject *norm_rope_backward(PyObject *const *a) {
+    const at::Tensor &q = rows_arg(a[0]), &k = rows_arg(a[1]);
+    Rows r[3];
+    for (int i = 0; i < 3; ++i)
+        if (i < 2 || a[2 + i] != Py_None) r[i].from = rows_arg(a[2 + i]);
+    const at::Tensor &dQ = r[0].from, &dK = r[1].from, &dV = r[2].from;
+    const NormRope n(dQ, dK, dV, a[5], a[6], a[7], a[8], a[9], a[10], a[11]);
+    require(q.sizes() == dQ.sizes() && k.sizes() == dK.sizes() && q.scalar_type() == dQ.scalar_type() && k.scalar_type() == dK.scalar_type(),
+            "q like dQ, k like dK");
+    const Out<3> out(a[12]);
+    rows_out(out, r);
+    const Out<2> out_w(a[13]);
+    at::Tensor w[2];
+    for (int i = 0; out_w.given() && i < 2; ++i) {
+        w[i] = dev_or_none(out_w[i]);  // None: not wanted
+        require(!w[i].defined() || (w[i].scalar_type() == at::kFloat && w[i].dim() == 1 && w[i].size(0) == n.p.d), "out_weights: fp32 [d]");
+    }
+    Workspace ws(a[14]);
+    at::Tensor given_ws;
+    if (ws.given) {
+        given_ws = dev(a[14]);
+        ws.bytes = (size_t)given_ws.nbytes();
+    }
+    one_device(q, k, dQ, dK, dV, n.t.f, n.t.qw, n.t.kw, n.t.pos, n.doc, r[0].to, r[1].to, r[2].to, w[0], w[1], given_ws);
+    const sepattn_strides qs = Rows::strides_of(q), ks = Rows::strides_of(k);
+    check("sepattn_norm_rope_backward", unlocked([&] {
+              const c10::DeviceGuard guard(q.device());
+              if (!out.given()) fused_rows(r, q, n.p.B, n.p.L, n.p.Hq, n.p.Hkv, n.p.d);
+              if (!out_w.given())
+                  for (at::Tensor &x : w) x = empty({n.p.d}, at::kFloat, q.device());
+              if (!ws.given && (w[0].defined() || w[1].defined())) ws.allocate(lib.sepattn_norm_rope_backward_workspace_bytes(&n.p), q.device());
+              for (Rows &x : r) x.finish();
+              return lib.sepattn_norm_rope_backward(&n.p, ptr_or_null(n.t.qw), ptr_or_null(n.t.kw), n.t.freqs, n.t.positions(), n.doc_start(), ptr(q), &qs,
+                                                    ptr(k), &ks, ptr(dQ), r[0].from_s(), ptr(dK), r[1].from_s(), ptr_or_null(dV), r[2].from_s(),
+                                                    ptr(r[0].to), r[0].to_s(), ptr(r[1].to), r[1].to_s(), ptr_or_null(r[2].to), r[2].to_s(),
+                                                    static_cast<float *>(ptr_or_null(w[0])), static_cast<float *>(ptr_or_null(w[1])), ws.p, ws.bytes,
+                                                    stream_of(q));
+          }));
+    PyObject *dx[3], *dw[2];
+    for (int i = 0; i < 3; ++i) dx[i] = out.given() ? keep(out[i]) : r[i].to.defined() ? wrap(r[i].to) : keep(Py_None);
+    for (int i = 0; i < 2; ++i) dw[i] = out_w.given() ? keep(out_w[i]) : wrap(w[i]);
+    return tuple_of(dx[0], dx[1], dx[2], dw[0], dw[1]);
+}
+
+// ---- the cache in 4 bits -----------------------------------------------------------------------------
+// Kc, Ks, Vc, Vs: uint8 [S, Hkv, c, d/2] and [S, Hkv, c, d/32]
+struct Fp4Args {
+    at::Tensor Kc, Ks, Vc, Vs;
+    explicit Fp4Args(PyObject *const *a) : Kc(dev(a[0])), Ks(dev(a[1])), Vc(dev(a[2])), Vs(dev(a[3])) {
+        for (const at::Tensor *t : {&Kc, &Ks, &Vc, &Vs}) {
+            require(t->scalar_type() == at::kByte && t->dim() == 4, "Kc, Ks, Vc, Vs: uint8 [S, Hkv, c, d/2] and [S, Hkv, c, d/32]");
+            for (const int64_t n : t->sizes()) require(n <= INT_MAX / 2, "sizes of 32 bits are expected");
+        }
+        const int64_t want[4] = {Kc.size(0), Kc.size(1), Kc.size(2), Kc.size(3) / 16};
+        require(Vc.sizes() == Kc.sizes() && Ks.sizes() == c10::IntArrayRef(want, 4) && Vs.sizes() == Ks.sizes(),
+                "Kc, Ks, Vc, Vs: uint8 [S, Hkv, c, d/2] and [S, Hkv, c, d/32]");
+    }
+    sepkv_params params(int Hq, PyObject *const *blocks, float scale, int dtype) const {
+        sepkv_params p;
+        p.S = (int)Kc.size(0), p.Hq = Hq, p.Hkv = (int)Kc.size(1), p.d = (int)Kc.size(3) * 2, p.c = (int)Kc.size(2);
+        p.a = as_int(blocks[0]), p.s = as_int(blocks[1]), p.w = as_int(blocks[2]);
+        p.scale = scale, p.dtype = dtype;
+        return p;
+    }
+};
+
+// append_fp4(k_new, v_new, is_sep_new, Kc, Ks, Vc, Vs, win_is_sep, sizes, Hq, a, s, w)
+PyObject *append_fp4(PyObject *const *a) {
+    Token x(nullptr, a[0], a[1], a[2], a[7], a[8], nullptr);
+    const Fp4Args c(a + 3);
+    const sepkv_params p = c.params(as_int(a[9]), a + 10, 1.0f, dtype_code(x.k));
+    x.match(p, x.k.scalar_type());
+    one_device(x.k, x.v, x.sep, c.Kc, c.Ks, c.Vc, c.Vs, x.flags, x.sizes);
+    check("sepkv_append_mx", unlocked([&] {
+              const c10::DeviceGuard guard(x.k.device());
+              return lib.sepkv_append_mx(&p, ptr(x.k), ptr(x.v), x.is_sep(), ptr(c.Kc), ptr(c.Ks), ptr(c.Vc), ptr(c.Vs), x.win(), x.sz(), stream_of(x.k));
+          }));
+    return keep(Py_None);
+}
+
+// append_rope_fp4, append_norm_rope_fp4: as append_rope, append_norm_rope, with Kc, Ks, Vc, Vs in the place of Kc, Vc
+template <bool NORM>
+PyObject *append_turned_fp4(PyObject *const *a) {
+    PyObject *const *b = a + (NORM ? 9 : 6);
+    Token x(a[0], a[1], a[2], a[3], b[4], b[5], b[10]);
+    const Fp4Args c(b);
+    const sepkv_params p = c.params((int)x.q.size(1), b + 6, 1.0f, dtype_code(x.q));
+    require(x.q.size(0) == p.S, "q: [S, Hq, d]");
+    x.match(p, x.q.scalar_type());
+    const Turn t = turn_args<NORM>(a[4], NORM ? a[5] : nullptr, NORM ? a[6] : nullptr, a[NORM ? 7 : 5], NORM ? a[8] : nullptr, p.d);
+    x.match_turn(t, p);
+    const int interleaved = as_bool(b[9]);
+    one_device(x.q, x.k, x.v, x.sep, t.pos, t.f, t.qw, t.kw, c.Kc, c.Ks, c.Vc, c.Vs, x.flags, x.sizes, x.out);
+    check(NORM ? "sepkv_append_norm_rope_mx" : "sepkv_append_rope_mx", unlocked([&] {
+              const c10::DeviceGuard guard(x.q.device());
+              x.allocate();
+              if constexpr (NORM)
+                  return lib.sepkv_append_norm_rope_mx(&p, t.rotary_dim, interleaved, t.eps, t.weight_dtype, ptr_or_null(t.qw), ptr_or_null(t.kw), t.freqs,
+                                                        t.positions(), ptr(x.q), ptr(x.k), ptr(x.v), x.is_sep(), ptr(x.out), ptr(c.Kc), ptr(c.Ks),
+                                                        ptr(c.Vc), ptr(c.Vs), x.win(), x.sz(), stream_of(x.q));
+              else
+                  return lib.sepkv_append_rope_mx(&p, t.rotary_dim, interleaved, t.freqs, t.positions(), ptr(x.q), ptr(x.k), ptr(x.v), x.is_sep(),
+                                                   ptr(x.out), ptr(c.Kc), ptr(c.Ks), ptr(c.Vc), ptr(c.Vs), x.win(), x.sz(), stream_of(x.q));
+          }));
+    return x.result();
+}
+
+void window_args(const at::Tensor &flags, const at::Tensor &sizes, const sepkv_params &p) {
+    require(flags.scalar_type() == at::kByte && flags.dim() == 2 && flags.size(0) == p.S && flags.size(1) == (int64_t)p.c - p.a - p.s,
+            "win_is_sep: uint8 [S, c-a-s]");
+    require(sizes.size(0) == p.S, "sizes: int32 [S, 6]");
+}
+
+// evict_window_fp4(Kc, Ks, Vc, Vs, win_is_sep, sizes, Hq, a, s, w)
+PyObject *evict_window_fp4(PyObject *const *a) {
+    const Fp4Args c(a);
+    const at::Tensor &flags = dev(a[4]), &sizes = sizes_arg(a[5]);
+    const sepkv_params p = c.params(as_int(a[6]), a + 7, 1.0f, SEPATTN_BF16);
+    window_args(flags, sizes, p);
+    one_device(c.Kc, c.Ks, c.Vc, c.Vs, flags, sizes);
+    check("sepkv_evict_window_mx", unlocked([&] {
+              const c10::DeviceGuard guard(c.Kc.device());
+              return lib.sepkv_evict_window_mx(&p, ptr(c.Kc), ptr(c.Ks), ptr(c.Vc), ptr(c.Vs), (const uint8_t *)ptr(flags), (int32_t *)ptr(sizes),
+                                                stream_of(c.Kc));
+          }));
+    return keep(Py_None);
+}
+
+// fill_from_prefill_fp4(K, V, is_sep, sep_idx, sep_prefix, Hq, a, s, w, c, nw, out)
+PyObject *fill_from_prefill_fp4(PyObject *const *a) {
+    const at::Tensor &K = dev(a[0]), &V = dev(a[1]), &sep = dev(a[2]), &idx = dev(a[3]), &pre = dev(a[4]);
+    if (K.dim() != 4) fail(PyExc_ValueError, "K [S,Hkv,L,d] is expected");
+    for (const int64_t n : K.sizes()) require(n < INT_MAX, "sizes of 32 bits are expected");
+    const int64_t S = K.size(0), L = K.size(2);
+    const int nw = as_int(a[10]);
+    sepkv_params p = {(int)S, as_int(a[5]), (int)K.size(1), (int)K.size(3), as_int(a[6]), as_int(a[7]), as_int(a[8]), as_int(a[9]), 1.0f, dtype_code(K)};
+    require(V.sizes() == K.sizes() && V.scalar_type() == K.scalar_type(), "V like K");
+    require(sep.scalar_type() == at::kByte && sep.dim() == 2 && sep.size(0) == S && sep.size(1) == L, "is_sep: uint8 [S, L]");
+    require(idx.scalar_type() == at::kInt && idx.dim() == 2 && idx.size(0) == S && pre.scalar_type() == at::kInt && pre.dim() == 2 && pre.size(0) == S &&
+                pre.size(1) == L + 1, "sep_idx: int32 [S, cap], sep_prefix: int32 [S, L+1]");
+    require(p.d == 64 || p.d == 128, "d: 64 or 128");
+    require(p.a >= 0 && p.s >= 0 && p.c > 0 && (int64_t)p.a + p.s < p.c, "blocks: a + s + w < c");
+    const Out<6> out(a[11]);
+    at::Tensor x[4], flags, sizes;
+    if (out.given()) {
+        PyObject *const four[4] = {out[0], out[1], out[2], out[3]};
+        const Fp4Args c(four);
+        x[0] = c.Kc, x[1] = c.Ks, x[2] = c.Vc, x[3] = c.Vs;
+        const int64_t want[4] = {S, p.Hkv, p.c, p.d / 2};
+        require(c.Kc.sizes() == c10::IntArrayRef(want, 4), "out: Kc, Ks, Vc, Vs: uint8 [S, Hkv, c, d/2] and [S, Hkv, c, d/32]");
+        flags = dev(out[4]), sizes = sizes_arg(out[5]);
+        window_args(flags, sizes, p);
+    }
+    one_device(K, V, sep, idx, pre, x[0], x[1], x[2], x[3], flags, sizes);
+    check("sepkv_fill_from_prefill_mx", unlocked([&] {
+              const c10::DeviceGuard guard(K.device());
+              if (!out.given()) {
+                  for (int i = 0; i < 4; ++i) x[i] = empty({p.S, p.Hkv, p.c, p.d / (i % 2 ? 32 : 2)}, at::kByte, K.device());
+                  flags = empty({p.S, p.c - p.a - p.s}, at::kByte, K.device());
+                  sizes = empty({p.S, SEPKV_SIZES_COLS}, at::kInt, K.device());
+              }
+              return (out.given() ? lib.sepkv_fill_from_prefill_mx : lib.sepkv_fill_from_prefill_mx_zeroed)(
+                  &p, (int)L, nw, ptr(K), ptr(V), (const uint8_t *)ptr(sep), i32(idx), (int)idx.size(1), i32(pre), ptr(x[0]), ptr(x[1]), ptr(x[2]), ptr(x[3]),
+                  (uint8_t *)ptr(flags), (int32_t *)ptr(sizes), stream_of(K));
+          }));
+    if (out.given()) return tuple_of(keep(out[0]), keep(out[1]), keep(out[2]), keep(out[3]), keep(out[4]), keep(out[5]));
+    return tuple_of(wrap(x[0]), wrap(x[1]), wrap(x[2]), wrap(x[3]), wrap(flags), wrap(sizes));
+}
+
+// expand_fp4(Kc, Ks, Vc, Vs, sizes, a, s, w, fp32, out)
+PyObject *expand_fp4(PyObject *const *a) {
+    const Fp4Args c(a);
+    const at::Tensor &sizes = sizes_arg(a[4]);
+    const Out<2> out(a[9]);
+    at::Tensor K, V;
+    if (out.given()) K = dev(out[0]), V = dev(out[1]);
+    const auto type = K.defined() ? K.scalar_type() : as_bool(a[8]) ? at::kFloat : at::kBFloat16;
+    const sepkv_params p = c.params((int)c.Kc.size(1), a + 5, 1.0f, K.defined() ? dtype_code(K) : type == at::kFloat ? SEPATTN_FP32 : SEPATTN_BF16);
+    require(sizes.size(0) == p.S, "sizes: int32 [S, 6]");
+    if (out.given()) {
+        const int64_t want[4] = {p.S, p.Hkv, p.c, p.d};
+        require(K.sizes() == c10::IntArrayRef(want, 4) && V.sizes() == K.sizes() && V.scalar_type() == type, "out: K, V [S, Hkv, c, d] of one dtype");
+    }
+    one_device(c.Kc, c.Ks, c.Vc, c.Vs, sizes, K, V);
+    check("sepkv_expand_mx", unlocked([&] {
+              const c10::DeviceGuard guard(c.Kc.device());
+              if (!out.given()) {
+                  K = empty({p.S, p.Hkv, p.c, p.d}, type, c.Kc.device());
+                  V = empty({p.S, p.Hkv, p.c, p.d}, type, c.Kc.device());
+              }
+              return lib.sepkv_expand_mx(&p, i32(sizes), ptr(c.Kc), ptr(c.Ks), ptr(c.Vc), ptr(c.Vs), ptr(K), ptr(V), stream_of(c.Kc));
+          }));
+    if (out.given()) return tuple_of(keep(out[0]), keep(out[1]));
+    return tuple_of(wrap(std::move(K)), wrap(std::move(V)));
 }
 
 // ---- shared prompts ----------------------------------------------------------------------------------
@@ -822,6 +1144,50 @@ PyObject *decode_shared_workspace_bytes(PyObject *const *a) {
     return PyLong_FromSize_t(lib.sepattn_decode_shared_workspace_bytes(&x.p, &x.pp));
 }
 
+// decode_fp4(q, Kc, Ks, Vc, Vs, sizes, rope_table, a, s, w, scale, out, ws)
+template <bool ROPE>
+PyObject *decode_fp4(PyObject *const *a) {
+    const at::Tensor &q = dev(a[0]), &sizes = sizes_arg(a[5]);
+    const Fp4Args c(a + 1);
+    const at::Tensor table = ROPE ? at::Tensor(dev(a[6])) : at::Tensor();
+    if (q.dim() != 3) fail(PyExc_ValueError, "q [S,Hq,d] is expected");
+    const sepkv_params p = c.params((int)q.size(1), a + 7, as_float(a[10]), dtype_code(q));
+    require(q.size(0) == p.S && q.size(2) == p.d && sizes.size(0) == p.S, "q [S, Hq, d], sizes int32 [S, 6], Kc [S, Hkv, c, d/2]");
+    if (ROPE) table_arg(table, p.d);
+    const Out<2> out(a[11]);
+    at::Tensor o, lse;
+    if (out.given()) {
+        o = dev(out[0]);
+        lse = dev_or_none(out[1]);  // None: no LSE wanted
+        require(o.sizes() == q.sizes() && o.scalar_type() == q.scalar_type() &&
+                    (!lse.defined() || (lse.scalar_type() == at::kFloat && lse.numel() == (int64_t)p.S * p.Hq)), "out: like q, lse: fp32 [S, Hq]");
+    }
+    Workspace ws(a[12]);
+    at::Tensor given_ws;
+    if (ws.given) {
+        given_ws = dev(a[12]);
+        ws.bytes = (size_t)given_ws.nbytes();
+    }
+    one_device(q, c.Kc, c.Ks, c.Vc, c.Vs, sizes, table, o, lse, given_ws);
+    check(ROPE ? "sepattn_decode_rope_mx" : "sepattn_decode_mx", unlocked([&] {
+              const c10::DeviceGuard guard(q.device());
+              if (!out.given()) {
+                  o = fresh_like(q);
+                  lse = empty({p.S, p.Hq}, at::kFloat, q.device());
+              }
+              if (!ws.given) ws.allocate(lib.sepattn_decode_mx_workspace_bytes(&p), q.device());
+              float *l = static_cast<float *>(ptr_or_null(lse));
+              if constexpr (ROPE)
+                  return lib.sepattn_decode_rope_mx(&p, ptr(q), ptr(c.Kc), ptr(c.Ks), ptr(c.Vc), ptr(c.Vs), i32(sizes), (const float *)ptr(table),
+                                                     (int)table.size(0), ptr(o), l, ws.p, ws.bytes, stream_of(q));
+              else
+                  return lib.sepattn_decode_mx(&p, ptr(q), ptr(c.Kc), ptr(c.Ks), ptr(c.Vc), ptr(c.Vs), i32(sizes), ptr(o), l, ws.p, ws.bytes,
+                                                stream_of(q));
+          }));
+    if (out.given()) return tuple_of(keep(out[0]), keep(out[1]));
+    return tuple_of(wrap(std::move(o)), wrap(std::move(lse)));
+}
+
 // ---- module ------------------------------------------------------------------------------------------
 typedef PyObject *(*Body)(PyObject *const *);
 template <Body F, int N>
@@ -862,6 +1228,7 @@ PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n) {
     LIB_FUNCTIONS(X)
     LIB_FRESH_FUNCTIONS(X)
     LIB_POSITION_FUNCTIONS(X)
+    LIB_NORM_FP4_FUNCTIONS(X)
 #undef X
     Py_INCREF(args[1]);
     Py_XSETREF(g_raise, args[1]);
@@ -890,7 +1257,18 @@ PyMethodDef methods[] = {
     METHOD("fill_from_prefill", fill_from_prefill, 12),
     METHOD("rope", rope<false>, 8),
     METHOD("rope_backward", rope<true>, 8),
-    METHOD("append_rope", append_rope, 15),
+    METHOD("append_rope", append_turned<false>, 15),
+    METHOD("append_norm_rope", append_turned<true>, 18),
+    METHOD("norm_rope", norm_rope, 11),
+    METHOD("norm_rope_backward", norm_rope_backward, 15),
+    METHOD("append_fp4", append_fp4, 13),
+    METHOD("append_rope_fp4", append_turned_fp4<false>, 17),
+    METHOD("append_norm_rope_fp4", append_turned_fp4<true>, 20),
+    METHOD("evict_window_fp4", evict_window_fp4, 10),
+    METHOD("fill_from_prefill_fp4", fill_from_prefill_fp4, 12),
+    METHOD("expand_fp4", expand_fp4, 10),
+    METHOD("decode_fp4", decode_fp4<false>, 13),
+    METHOD("decode_rope_fp4", decode_fp4<true>, 13),
     METHOD("group_sequences", group_sequences, 3),
     METHOD("rope_cache", rope_cache, 7),
     METHOD("decode_shared", decode_shared<false>, 20),

@@ -48,6 +48,16 @@ __device__ inline int pair_of(int group, int e, int half) {
 template <PairLayout LAYOUT, int E>
 __device__ inline bool has_turned(int group, int n_pairs) { return pair_of<LAYOUT, E>(group, 0, 0) < n_pairs; }
 
+// where the members of pair e of a group stand in the row
+template <PairLayout LAYOUT, int E>
+__device__ inline void members_of(int group, int e, int n_pairs, int half, int &first, int &second) {
+    const int p = pair_of<LAYOUT, E>(group, e, half);
+    if (LAYOUT == kNeighbours) first = 2 * p, second = 2 * p + 1;
+    else if (LAYOUT == kHalves && group * E >= n_pairs) first = 2 * group * E + e, second = first + E;  // a piece, and the piece behind it
+    else if (p < n_pairs) first = p, second = p + n_pairs;
+    else first = 2 * p, second = 2 * p + 1;
+}
+
 // cos / sin of the E pairs of a group at one position
 template <typename T, PairLayout LAYOUT>
 struct Angles {
@@ -110,6 +120,29 @@ struct Pairs {
             const int second = second_piece(group, n_pairs, half, first);
             *reinterpret_cast<Run *>(row + first) = a;
             *reinterpret_cast<Run *>(row + second) = b;
+        }
+    }
+    // first and second members in fp32, and back (rounded to nearest even)
+    __device__ void widen(float (&u)[E], float (&v)[E]) const {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            if constexpr (LAYOUT == kNeighbours) {
+                const Run &r = e < E / 2 ? a : b;
+                u[e] = widened(r[2 * e % E]), v[e] = widened(r[2 * e % E + 1]);
+            } else {
+                u[e] = widened(a[e]), v[e] = widened(b[e]);
+            }
+        }
+    }
+    __device__ void narrow(const float (&u)[E], const float (&v)[E]) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            if constexpr (LAYOUT == kNeighbours) {
+                Run &r = e < E / 2 ? a : b;
+                r[2 * e % E] = narrowed<T>(u[e]), r[2 * e % E + 1] = narrowed<T>(v[e]);
+            } else {
+                a[e] = narrowed<T>(u[e]), b[e] = narrowed<T>(v[e]);
+            }
         }
     }
     __device__ void turn(const Angles<T, LAYOUT> &w, int group, int n_pairs, int half) {

@@ -176,8 +176,7 @@ struct NormRopeTensors {  // q, k, v; heads[2] = 0: no values
 };
 struct NormRopeGrid {  // how a backward call is cut
     int B, log_tokens, tiles_per_row;  // tiles of 1 << log_tokens tokens
-    int chunk, chunks[3];              // heads per workgroup; chunks of q, k, v
-    int walkers;                       // workgroups that share a chunk's tiles
+    int first[4];                      // workgroups of q, k and v: first[i] .. first[i+1] - 1
 };
 NormRopeGrid norm_rope_grid(const sepattn_norm_rope_params &p, bool values, int units);
 size_t norm_rope_backward_workspace(const sepattn_norm_rope_params &p);

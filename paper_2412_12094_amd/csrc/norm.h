@@ -29,18 +29,38 @@ struct Weights {
     static constexpr int E = 16 / (int)sizeof(T);
     float u[E], v[E];
     __device__ void load(const NormWeight &w, int group, int n_pairs, int half) {
+        if (!w.w) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            int i, j;
-            members_of<LAYOUT, E>(group, e, n_pairs, half, i, j);
-            u[e] = v[e] = 1.f;
-            if (!w.w) continue;
-            if (w.dtype == SEPATTN_BF16) {
-                const uint16_t *p = static_cast<const uint16_t *>(w.w);
-                u[e] = widened(p[i]), v[e] = widened(p[j]);
-            } else {
-                const float *p = static_cast<const float *>(w.w);
-                u[e] = p[i], v[e] = p[j];
+            for (int e = 0; e < E; ++e) u[e] = v[e] = 1.f;
+        } else if (w.dtype == SEPATTN_BF16) {
+            load_from(static_cast<const uint16_t *>(w.w), group, n_pairs, half);
+        } else {
+            load_from(static_cast<const float *>(w.w), group, n_pairs, half);
+        }
+    }
+
+private:
+    template <typename W>
+    __device__ void load_from(const W *w, int group, int n_pairs, int half) {
+        if constexpr (LAYOUT == kHalvesOdd) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                int i, j;
+                members_of<LAYOUT, E>(group, e, n_pairs, half, i, j);
+                u[e] = widened(w[i]), v[e] = widened(w[j]);
+            }
+        } else {  // two pieces of E values, as Pairs has them
+            int first;
+            const int second = Pairs<T, LAYOUT>::second_piece(group, n_pairs, half, first);
+            const W *a = w + first, *b = w + second;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                if constexpr (LAYOUT == kNeighbours) {
+                    const W *r = e < E / 2 ? a : b;
+                    u[e] = widened(r[2 * e % E]), v[e] = widened(r[2 * e % E + 1]);
+                } else {
+                    u[e] = widened(a[e]), v[e] = widened(b[e]);
+                }
             }
         }
     }

@@ -16,6 +16,8 @@ namespace sepattn {
 namespace {
 
 constexpr int kNormThreads = 256;
+constexpr int kNormRows = 2;   // rows of q or k that a lane of the backward has in flight
+constexpr int kMovedRows = 4;  // ... of v
 
 template <typename T, int D, PairLayout LAYOUT, bool STREAM>
 __global__ __launch_bounds__(kNormThreads) void norm_rope_kernel(NormRopeTensors x, int L, int n_pairs, int log_tokens, int chunk, float eps,
@@ -60,96 +62,136 @@ __global__ __launch_bounds__(kNormThreads) void norm_rope_kernel(NormRopeTensors
     }
 }
 
-// Grid (walkers over the tiles of tokens, chunks of heads).  A chunk is of q, of k or of v.  Row blockIdx.x of the partial sums of chunk y.
+// sum over the lanes of a wave that hold the same group of pairs: lanes l, l + GROUPS, l + 2 GROUPS, ...
+template <int GROUPS>
+__device__ inline float rows_sum(float x) {
+    auto turned_by = [](float y, auto CTRL) { return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(y), decltype(CTRL)::value, 0xF, 0xF, true)); };
+    if constexpr (GROUPS <= 8) x += turned_by(x, std::integral_constant<int, 0x128>{});  // row_ror 8
+    if constexpr (GROUPS <= 4) x += turned_by(x, std::integral_constant<int, 0x124>{});  // row_ror 4
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// A workgroup has q, k or v (grid.first) and a run of that tensor's items, which are (tile of tokens, group of heads), the groups fastest, so that angles
+// serve all heads of a tile.
 template <typename T, int D, PairLayout LAYOUT, bool STREAM>
-__global__ __launch_bounds__(kNormThreads) void norm_rope_backward_kernel(NormRopeTensors x, NormRopeGrid grid, int L, int n_pairs, float eps,
-                                                                           const double *__restrict__ freqs,
-                                                                           const int32_t *__restrict__ positions,
-                                                                           const int32_t *__restrict__ doc_start, float *__restrict__ part) {
+__global__ __launch_bounds__(kNormThreads, LAYOUT == kHalvesOdd ? 2 : 3) void norm_rope_backward_kernel(
+    NormRopeTensors x, NormRopeGrid grid, int L, int n_pairs, float eps, const double *__restrict__ freqs, const int32_t *__restrict__ positions,
+    const int32_t *__restrict__ doc_start, float *__restrict__ part) {
     constexpr int E = 16 / (int)sizeof(T), GROUPS = D / (2 * E), half = D / 2, ROWS = kNormThreads / GROUPS;
     const int group = threadIdx.x % GROUPS, row_slot = threadIdx.x / GROUPS;
     const int token = row_slot & ((1 << grid.log_tokens) - 1), slot = row_slot >> grid.log_tokens, slots = ROWS >> grid.log_tokens;
-    const int y = blockIdx.y, which = y < grid.chunks[0] ? 0 : y < grid.chunks[0] + grid.chunks[1] ? 1 : 2;
-    const int c = y - (which > 0 ? grid.chunks[0] : 0) - (which > 1 ? grid.chunks[1] : 0);
-    const int h0 = c * grid.chunk, h1 = min(h0 + grid.chunk, x.heads[which]);
+    const int which = (int)blockIdx.x < grid.first[1] ? 0 : (int)blockIdx.x < grid.first[2] ? 1 : 2;
+    const int mine = blockIdx.x - grid.first[which], sharers = grid.first[which + 1] - grid.first[which];
+    const int heads = x.heads[which], step = (which < 2 ? kNormRows : kMovedRows) * slots, groups = (heads + step - 1) / step;
+    const long items = (long)grid.tiles_per_row * grid.B * groups, last = items * (mine + 1) / sharers;
+    long item = items * mine / sharers;
+    int tile = (int)(item / groups), h0 = (int)(item - (long)tile * groups) * step;
     const sepattn_strides from = x.from[which], to = x.to[which], gs = x.grad_strides[which];
+    // the token of a tile: row of the batch, index in it
+    auto place = [&](int &b, int &l) {
+        b = tile / grid.tiles_per_row;
+        l = ((tile - b * grid.tiles_per_row) << grid.log_tokens) + token;
+    };
+    int b, l;
+    if (which == 2) {  // values: moved only
+        for (place(b, l); item < last; ++item, h0 += step) {
+            if (h0 >= heads) h0 = 0, ++tile, place(b, l);
+            const T *g = static_cast<const T *>(x.grad[which]) + b * gs.b + l * gs.l;
+            T *dst = static_cast<T *>(x.dst[which]) + b * to.b + l * to.l;
+            Pairs<T, LAYOUT> row[kMovedRows];
+#pragma unroll
+            for (int n = 0; n < kMovedRows; ++n)
+                if (l < L && h0 + slot + n * slots < heads) row[n].template load<STREAM>(g + (h0 + slot + n * slots) * gs.h, group, n_pairs, half);
+#pragma unroll
+            for (int n = 0; n < kMovedRows; ++n)
+                if (l < L && h0 + slot + n * slots < heads) row[n].store(dst + (h0 + slot + n * slots) * to.h, group, n_pairs, half);
+        }
+        return;
+    }
     const bool turned = has_turned<LAYOUT, E>(group, n_pairs);
     Weights<T, LAYOUT> weight;
+    weight.load(x.weight[which], group, n_pairs, half);
     float su[E], sv[E];
-    if (which < 2) {
-        weight.load(x.weight[which], group, n_pairs, half);
 #pragma unroll
-        for (int e = 0; e < E; ++e) su[e] = sv[e] = 0.f;
-    }
-    for (int tile = blockIdx.x; tile < grid.tiles_per_row * grid.B; tile += gridDim.x) {
-        const int b = tile / grid.tiles_per_row, l = ((tile - b * grid.tiles_per_row) << grid.log_tokens) + token;
-        if (l >= L) continue;
-        const T *g = static_cast<const T *>(x.grad[which]) + b * gs.b + l * gs.l;
-        T *dst = static_cast<T *>(x.dst[which]) + b * to.b + l * to.l;
-        if (which == 2) {  // values: moved only
-            constexpr int N = 4;
-            for (int h = h0 + slot; h < h1; h += N * slots) {
-                Pairs<T, LAYOUT> row[N];
+    for (int e = 0; e < E; ++e) su[e] = sv[e] = 0.f;
+    // All lanes go through the whole loop, those beyond the tokens and heads with rows of zeros that are not stored: where lanes drop out, the sums are
+    // kept twice.  The rows of the next item are requested before those of this one are worked on.
+    struct Item {
+        int h0, b, l;
+        Pairs<T, LAYOUT> x[kNormRows], g[kNormRows];
+    };
+    auto request = [&](Item &i) __attribute__((always_inline)) {
+        const T *src = static_cast<const T *>(x.src[which]) + i.b * from.b + i.l * from.l, *g = static_cast<const T *>(x.grad[which]) + i.b * gs.b + i.l * gs.l;
 #pragma unroll
-                for (int n = 0; n < N; ++n)
-                    if (h + n * slots < h1) row[n].template load<STREAM>(g + (h + n * slots) * gs.h, group, n_pairs, half);
-#pragma unroll
-                for (int n = 0; n < N; ++n)
-                    if (h + n * slots < h1) row[n].store(dst + (h + n * slots) * to.h, group, n_pairs, half);
+        for (int n = 0; n < kNormRows; ++n) {
+            const int h = i.h0 + slot + n * slots;
+            i.x[n].clear(), i.g[n].clear();
+            if (i.l < L && h < heads) {
+                i.x[n].template load<STREAM>(src + h * from.h, group, n_pairs, half);
+                i.g[n].template load<STREAM>(g + h * gs.h, group, n_pairs, half);
             }
-            continue;
         }
-        const T *src = static_cast<const T *>(x.src[which]) + b * from.b + l * from.l;
-        const long at = (long)b * L + l;
-        Angles<T, LAYOUT> w;
-        if (turned) w.form(freqs, n_pairs, half, group, positions ? positions[at] : l - (doc_start ? doc_start[at] : 0), -1.f);
-        constexpr int N = 2;
-        for (int h = h0 + slot; h < h1; h += N * slots) {
-            Pairs<T, LAYOUT> rx[N], rg[N];
-#pragma unroll
-            for (int n = 0; n < N; ++n)
-                if (h + n * slots < h1) {
-                    rx[n].template load<STREAM>(src + (h + n * slots) * from.h, group, n_pairs, half);
-                    rg[n].template load<STREAM>(g + (h + n * slots) * gs.h, group, n_pairs, half);
-                }
-#pragma unroll
-            for (int n = 0; n < N; ++n)
-                if (h + n * slots < h1) {
-                    float xu[E], xv[E], gu[E], gv[E];
-                    rx[n].widen(xu, xv);
-                    rg[n].widen(gu, gv);
-                    if (turned) turn_pairs(gu, gv, w, group, n_pairs, half);
-                    const float r = row_rms<D, GROUPS>(xu, xv, eps);
-                    float dot = 0.f;
-#pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        su[e] = fmaf(gu[e], xu[e] * r, su[e]);
-                        sv[e] = fmaf(gv[e], xv[e] * r, sv[e]);
-                        gu[e] *= weight.u[e], gv[e] *= weight.v[e];
-                        dot = fmaf(gu[e], xu[e], fmaf(gv[e], xv[e], dot));
-                    }
-                    const float back = row_sum<GROUPS>(dot) * (r * r) * (1.f / D);
-#pragma unroll
-                    for (int e = 0; e < E; ++e) gu[e] = r * fmaf(-back, xu[e], gu[e]), gv[e] = r * fmaf(-back, xv[e], gv[e]);
-                    rg[n].narrow(gu, gv);
-                    rg[n].store(dst + (h + n * slots) * to.h, group, n_pairs, half);
-                }
+    };
+    Item now, next;
+    now.h0 = h0;
+    place(now.b, now.l);
+    Angles<T, LAYOUT> w;
+    if (item < last) request(now);
+    for (bool fresh = true; item < last; ++item) {
+        next.h0 = now.h0 + step, next.b = now.b, next.l = now.l;
+        const bool turn_over = next.h0 >= heads;
+        if (turn_over) next.h0 = 0, ++tile, place(next.b, next.l);
+        if (item + 1 < last) request(next);
+        if (fresh) {
+            const long at = (long)now.b * L + now.l;
+            asm volatile("" : "+s"(freqs));  // (read for every tile: kept, they and their products are 32 registers)
+            if (turned) w.template form<true>(freqs, n_pairs, half, group, now.l >= L ? 0 : positions ? positions[at] : now.l - (doc_start ? doc_start[at] : 0), -1.f);
         }
+        fresh = turn_over;
+        T *dst = static_cast<T *>(x.dst[which]) + now.b * to.b + now.l * to.l;
+        const int h = now.h0 + slot;
+#pragma unroll
+        for (int n = 0; n < kNormRows; ++n) {
+            const bool row = now.l < L && h + n * slots < heads;
+            float xu[E], xv[E], gu[E], gv[E];
+            now.x[n].widen(xu, xv);
+            now.g[n].widen(gu, gv);
+            if (turned) turn_pairs(gu, gv, w, group, n_pairs, half);
+            float r = row_rms<D, GROUPS>(xu, xv, eps), dot = 0.f;
+            r = row ? r : 0.f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                su[e] = fmaf(gu[e], xu[e] * r, su[e]);
+                sv[e] = fmaf(gv[e], xv[e] * r, sv[e]);
+                asm volatile("" : "+v"(su[e]), "+v"(sv[e]));  // now: put off, the sums keep the values of all rows alive
+                gu[e] *= weight.u[e], gv[e] *= weight.v[e];
+                dot = fmaf(gu[e], xu[e], fmaf(gv[e], xv[e], dot));
+            }
+            const float back = row_sum<GROUPS>(dot) * (r * r) * (1.f / D);
+#pragma unroll
+            for (int e = 0; e < E; ++e) gu[e] = r * fmaf(-back, xu[e], gu[e]), gv[e] = r * fmaf(-back, xv[e], gv[e]);
+            now.g[n].narrow(gu, gv);
+            if (row) now.g[n].store(dst + (h + n * slots) * to.h, group, n_pairs, half);
+            __builtin_amdgcn_sched_barrier(0);  // row by row: the fp32 values of several leave no room for more waves
+        }
+        now = next;
     }
-    if (which == 2 || !part) return;
-    __shared__ float sums[ROWS][D];
+    if (!part) return;
+    __shared__ float sums[kNormThreads / kWave][D];
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
         int i, j;
         members_of<LAYOUT, E>(group, e, n_pairs, half, i, j);
-        sums[row_slot][i] = su[e], sums[row_slot][j] = sv[e];
+        const float u = rows_sum<GROUPS>(su[e]), v = rows_sum<GROUPS>(sv[e]);
+        if (lane < GROUPS) sums[wave][i] = u, sums[wave][j] = v;
     }
     __syncthreads();
-    for (int rows = ROWS / 2; rows >= 1; rows /= 2) {
-        for (int i = threadIdx.x; i < rows * D; i += kNormThreads) sums[i / D][i % D] += sums[i / D + rows][i % D];
-        __syncthreads();
-    }
-    if (threadIdx.x < D) part[((long)y * gridDim.x + blockIdx.x) * D + threadIdx.x] = sums[0][threadIdx.x];
+    if (threadIdx.x < D)
+        part[(long)blockIdx.x * D + threadIdx.x] = (sums[0][threadIdx.x] + sums[1][threadIdx.x]) + (sums[2][threadIdx.x] + sums[3][threadIdx.x]);
 }
 
 // dw of q (blockIdx.y 0) and of k (1): rows of partial sums, eight columns per workgroup
@@ -159,7 +201,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_weights_kernel(int D, int r
     if (!out) return;
     const int col = blockIdx.x * 8 + threadIdx.x % 8, first = threadIdx.x / 8, rows = blockIdx.y ? rows_k : rows_q;
     const float *p = part + (blockIdx.y ? (long)rows_q * D : 0) + col;
-    constexpr int STEP = kNormThreads / 8, N = 8;
+    constexpr int STEP = kNormThreads / 8, N = 32;
     double sum = 0.0;
     for (int r = first; r < rows; r += N * STEP) {
         float v[N];
@@ -212,24 +254,23 @@ NormRopeGrid norm_rope_grid(const sepattn_norm_rope_params &p, bool values, int 
     g.B = p.B;
     g.log_tokens = log_tokens_of(p.L, rows);
     g.tiles_per_row = (int)(((long)p.L + (1 << g.log_tokens) - 1) >> g.log_tokens);
-    const int heads[3] = {p.Hq, p.Hkv, values ? p.Hkv : 0}, slots = rows >> g.log_tokens;
-    const long tiles = (long)g.tiles_per_row * p.B, want = 6L * units;
-    // a chunk of heads such that there are `want` workgroups, if there is work for them; then walkers for as many
-    const long all = heads[0] + heads[1] + heads[2], per = (all * tiles + want - 1) / want;
-    g.chunk = (int)(per < 8 ? per : 8);
-    g.chunk = (g.chunk + slots - 1) / slots * slots;
-    int chunks = 0;
-    for (int i = 0; i < 3; ++i) chunks += g.chunks[i] = (heads[i] + g.chunk - 1) / g.chunk;
-    const long walkers = (want + chunks - 1) / chunks;
-    g.walkers = (int)(walkers < tiles ? walkers : tiles);
+    const long want = 3L * units;
+    // workgroups by the bytes that a tensor moves: q and k are read twice and written once, v is read and written
+    const long heads[3] = {p.Hq, p.Hkv, values ? p.Hkv : 0}, moved[3] = {3 * heads[0], 3 * heads[1], 2 * heads[2]}, all = moved[0] + moved[1] + moved[2];
+    g.first[0] = 0;
+    for (int i = 0; i < 3; ++i) {
+        const long step = (long)(i < 2 ? kNormRows : kMovedRows) * (rows >> g.log_tokens), items = (long)g.tiles_per_row * g.B * ((heads[i] + step - 1) / step);
+        long n = (want * moved[i] + all / 2) / all;
+        n = n < 1 ? 1 : n;
+        g.first[i + 1] = g.first[i] + (int)(n < items ? n : items);
+    }
     return g;
 }
 
 size_t norm_rope_backward_workspace(const sepattn_norm_rope_params &p) {
     // with and without values a call is cut differently
-    const NormRopeGrid a = norm_rope_grid(p, true, compute_units()), b = norm_rope_grid(p, false, compute_units());
-    auto rows = [](const NormRopeGrid &g) { return (size_t)(g.chunks[0] + g.chunks[1]) * g.walkers; };
-    return align_up((rows(a) > rows(b) ? rows(a) : rows(b)) * p.d * sizeof(float), 256);
+    const int units = compute_units(), a = norm_rope_grid(p, true, units).first[2], b = norm_rope_grid(p, false, units).first[2];
+    return align_up((size_t)(a > b ? a : b) * p.d * sizeof(float), 256);
 }
 
 int launch_norm_rope(const sepattn_norm_rope_params &p, const double *freqs, const int32_t *positions, const int32_t *doc_start,
@@ -259,15 +300,13 @@ int launch_norm_rope(const sepattn_norm_rope_params &p, const double *freqs, con
 int launch_norm_rope_backward(const sepattn_norm_rope_params &p, const double *freqs, const int32_t *positions, const int32_t *doc_start,
                               const NormRopeTensors &x, float *dq_weight, float *dk_weight, float *part, hipStream_t st) {
     const NormRopeGrid g = norm_rope_grid(p, x.heads[2] > 0, compute_units());
-    const int chunks = g.chunks[0] + g.chunks[1] + g.chunks[2];
-    if (chunks > 65535) return SEPATTN_ERR_SHAPE;
     const bool sums = dq_weight || dk_weight;
     by_layout(p, [&](auto T_, auto D_, auto LAYOUT_) {
         using T = decltype(T_);
         constexpr int D = decltype(D_)::value;
         constexpr PairLayout LAYOUT = decltype(LAYOUT_)::value;
         auto go = [&](auto STREAM_) {
-            hipLaunchKernelGGL((norm_rope_backward_kernel<T, D, LAYOUT, decltype(STREAM_)::value>), dim3(g.walkers, chunks), dim3(kNormThreads), 0, st, x,
+            hipLaunchKernelGGL((norm_rope_backward_kernel<T, D, LAYOUT, decltype(STREAM_)::value>), dim3(g.first[3]), dim3(kNormThreads), 0, st, x,
                                g, p.L, p.rotary_dim / 2, p.eps, freqs, positions, doc_start, sums ? part : nullptr);
         };
         if (LAYOUT != kHalvesOdd && streams(p, (long)p.B * p.L * (3L * (x.heads[0] + x.heads[1]) + 2L * x.heads[2]))) go(std::bool_constant<LAYOUT != kHalvesOdd>{});
@@ -275,7 +314,7 @@ int launch_norm_rope_backward(const sepattn_norm_rope_params &p, const double *f
     });
     if (!sums) return launch_status();
     if (hipGetLastError() != hipSuccess) return SEPATTN_ERR_HIP;
-    hipLaunchKernelGGL(norm_weights_kernel, dim3(p.d / 8, 2), dim3(kNormThreads), 0, st, p.d, g.chunks[0] * g.walkers, g.chunks[1] * g.walkers, part,
+    hipLaunchKernelGGL(norm_weights_kernel, dim3(p.d / 8, 2), dim3(kNormThreads), 0, st, p.d, g.first[1], g.first[2] - g.first[1], part,
                        dq_weight, dk_weight);
     return launch_status();
 }

@@ -63,12 +63,14 @@ template <typename T, PairLayout LAYOUT>
 struct Angles {
     static constexpr int E = 16 / (int)sizeof(T);
     float cs[E], sn[E];
-    // sign -1: the opposite angles.  Pairs from n_pairs on are not looked at later.
+    // sign -1: the opposite angles.  Pairs from n_pairs on are not looked at later.  ONE_BY_ONE: in turn, for kernels that have no registers for all at once
+    template <bool ONE_BY_ONE = false>
     __device__ void form(const double *__restrict__ freqs, int n_pairs, int half, int group, int t, float sign) {
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             angle_of(t, freqs[min(pair_of<LAYOUT, E>(group, e, half), n_pairs - 1)], cs[e], sn[e]);
             sn[e] *= sign;
+            if constexpr (ONE_BY_ONE) __builtin_amdgcn_sched_barrier(0);
         }
     }
 };
@@ -89,6 +91,7 @@ struct Pairs {
         first = turned ? group * E : 2 * group * E;
         return first + (turned ? n_pairs : E);
     }
+    __device__ void clear() { a = b = Run(T(0)); }
     // STREAM: the non-temporal hint, for rows whose pieces one instruction reads by whole cache lines
     template <bool STREAM = false>
     __device__ void load(const T *row, int group, int n_pairs, int half) {

@@ -26,6 +26,18 @@ namespace {
 
 constexpr int kRows = 32;      // entries per block
 constexpr int kColumns = 16;   // query heads of a workgroup
+// waves per SIMD that the registers have to leave room for
+template <typename T, int D, bool ROPE>
+constexpr int kResident = sizeof(T) == 2 ? (ROPE && D == 128 ? 3 : 4) : (D == 128 ? (ROPE ? 2 : 3) : (ROPE ? 3 : 4));
+constexpr int kWaves = 4;
+template <int D, bool ROPE>
+constexpr int kDepth = D == 64 && !ROPE ? 2 : 1;  // blocks of a wave on their way
+constexpr int kLeastBlocks = kWaves;  // of a slice
+constexpr int kManyBlocks = 32;       // of a slice that leaves room for four workgroups per compute unit
+constexpr int kMostSlices = 64;       // of a sequence
+constexpr int kMostAdded = 16;        // slices that the kernel itself adds, at most
+constexpr int kWordPitch = 128;  // bytes: a cache line for each word in which slices are counted
+__host__ __device__ inline size_t words_bytes(long pairs) { return align_up((size_t)pairs * kWordPitch, 256); }
 
 __device__ inline f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
@@ -88,16 +100,48 @@ __device__ inline void finish(int entries, float M, float sum, float o, T *out, 
     if (lse) *lse = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2_f;
 }
 
-template <typename T, int D, bool ROPE, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void decode_fp4_kernel(sepkv_params p, int G, int n_pos, const T *__restrict__ q, Fp4Cache cache,
-                                                                 const int32_t *__restrict__ sizes, const float *__restrict__ rope,
-                                                                 float *__restrict__ part, T *__restrict__ out, float *__restrict__ lse) {
-    constexpr int KSTEPS = D / 32, KS2 = KSTEPS / 2, DB = D / 16;
+// The valid entries as runs of consecutive slots: entry e of a run sits in slot e + off, up to `end`.  All scalar.
+struct Runs {
+    int n1, n2, nv, sep_end, win_end, sep_off, win_off, s, wcap;
+    __device__ Runs(const CacheMap &m)
+        : n1(m.n_init), n2(m.n_init + m.n_sep), nv(m.n_init + m.n_sep + m.n_past + m.n_loc), s(m.s), wcap(m.wcap) {
+        sep_off = m.a + m.sep_head - n1, win_off = m.a + m.s + m.win_head - n2;
+        sep_end = min(n1 + m.s - m.sep_head, n2), win_end = min(n2 + m.wcap - m.win_head, nv);  // where the rings wrap
+    }
+    // the run of entry e (the same in all lanes)
+    __device__ int find(int e, int &off) const {
+        off = 0;
+        int end = n1;
+        if (e >= n1) off = sep_off, end = sep_end;
+        if (e >= sep_end && e >= n1) off = sep_off - s, end = n2;
+        if (e >= n2) off = win_off, end = win_end;
+        if (e >= win_end && e >= n2) off = win_off - wcap, end = nv;
+        return end;
+    }
+    // slot of entry e (of the lane's own)
+    __device__ int slot(int e) const {
+        int off = e >= sep_end ? sep_off - s : sep_off;
+        off = e < n1 ? 0 : off;
+        const int w = e >= win_end ? win_off - wcap : win_off;
+        return e + (e >= n2 ? w : off);
+    }
+};
+
+template <int D>
+constexpr int kMergeParts = 256 / (D / 2);  // threads of the merge launch that share two columns
+
+// ADD: the slices of a sequence are added by the workgroup that finishes last.  Otherwise, where there are several, they are left to a merge launch.
+template <typename T, int D, bool ROPE, bool ADD>
+__global__ __launch_bounds__(64 * kWaves, (kResident<T, D, ROPE>)) void decode_fp4_kernel(
+    sepkv_params p, int G, int n_pos, const T *__restrict__ q, Fp4Cache cache, const int32_t *__restrict__ sizes, const float *__restrict__ rope,
+    uint64_t one, char *__restrict__ ws, T *__restrict__ out, float *__restrict__ lse) {
+    constexpr int KSTEPS = D / 32, KS2 = KSTEPS / 2, DB = D / 16, NW = kWaves;
     constexpr int QP = Precision<T>::kQuery, WP = Precision<T>::kWeights, KP = ROPE ? Precision<T>::kTurned : 1;
     constexpr int PF = D + 2;  // record: max (log2 domain), sum, D unnormalised outputs
     constexpr int RF = D + 4;  // the same in LDS, in whole 16-byte pieces
     constexpr int STAGE = kColumns * RF * 4 > kRows * D * 2 ? kColumns * RF * 4 : kRows * D * 2;
     __shared__ __attribute__((aligned(1024))) unsigned char smem[NW][STAGE];  // V rows of every wave's block; at the end the waves' records
+    __shared__ __attribute__((aligned(16))) float base_s[ROPE ? NW : 1][2][ROPE ? D : 4];  // table rows of every wave's block
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, g = lane >> 4;
@@ -106,11 +150,12 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_fp4_kernel(sepkv_params p, 
     const int heads = min(G - first, kColumns), h0 = kv * G + first;
     const long head = (long)sq * p.Hkv + kv;
     const uint8_t *Kc = cache.Kc + head * p.c * (D / 2), *Vc = cache.Vc + head * p.c * (D / 2);
-    const Fp4Scales<D> *Ks = reinterpret_cast<const Fp4Scales<D> *>(cache.Ks) + head * p.c,
-                       *Vs = reinterpret_cast<const Fp4Scales<D> *>(cache.Vs) + head * p.c;
-    const CacheMap cm = cache_map(p, sizes + SEPKV_SIZES_COLS * sq);
-    const int nv = cm.n_init + cm.n_sep + cm.n_past + cm.n_loc;
-    const int nb = (nv + kRows - 1) / kRows, per = (nb + nsplit - 1) / nsplit * kRows;
+    const uint8_t *Ks = cache.Ks + head * p.c * (D / 32), *Vs = cache.Vs + head * p.c * (D / 32);
+    const Runs runs(cache_map(p, sizes + SEPKV_SIZES_COLS * sq));
+    const int nv = runs.nv, nb = (nv + kRows - 1) / kRows;
+    // slices of whole blocks (c d < 2^30, so nb < 2^19)
+    const int share = small_quotient(nb + nsplit - 1, reciprocal(nsplit));
+    const int per = (nsplit == 1 ? nb : __builtin_amdgcn_readfirstlane(share)) * kRows;
     const int e0 = min(split * per, nv), e1 = min(nv, e0 + per);
 
     // first dimension of this lane's fragment ks: whole rows by the four lane groups; with ROPE both members of every pair are one lane's
@@ -133,73 +178,145 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_fp4_kernel(sepkv_params p, 
     const int krow = 8 * (col >> 2) + (col & 3);  // this lane's rows of a block: krow, krow + 4
     struct Rows {
         RowCodes<D> k[2], v[2];
-        uint32_t ks[2], vs[2];
+        Fp4Scales<D> ks[2], vs[2];  // (as they are loaded: widened here, the half words of d = 64 would be waited for at once)
+        float base[2][ROPE ? D / 64 : 1];  // value(s) lane, lane + 64 of the table rows of the distances of entries 0 and 4 of the block
     };
-    auto request = [&](int eb, Rows &r) __attribute__((always_inline)) {
+    // slots of the lane's rows of a block; entries past the end: the last one (masked)
+    int run_end = -1, run_off = 0;
+    auto find_slots = [&](int eb, uint32_t (&slot)[2]) __attribute__((always_inline)) {
+        if (eb >= run_end) run_end = min(runs.find(eb, run_off), e1);
+        if (eb + kRows <= run_end) {  // one run of slots
+            slot[0] = eb + run_off + krow;
+            slot[1] = slot[0] + 4;
+        } else {
+            slot[0] = runs.slot(min(eb + krow, e1 - 1));
+            slot[1] = runs.slot(min(eb + krow + 4, e1 - 1));
+        }
+    };
+    auto request_keys = [&](Rows &rows, int eb, const uint32_t (&slot)[2]) __attribute__((always_inline)) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const uint32_t slot = decode_slot_of(cm, min(eb + krow + 4 * t, e1 - 1));  // entries past the end: the last one (masked)
-            const uint8_t *k = Kc + slot * (D / 2), *v = Vc + slot * (D / 2) + g * (D / 8);
+            const uint32_t off = slot[t] * (D / 2) + g * (ROPE ? D / 16 : D / 8);  // (c d / 2 < 2^29)
             if constexpr (ROPE) {  // D / 8 values of each half
                 using Half = uint32_t __attribute__((ext_vector_type(KS2)));
-                const Half a = __builtin_nontemporal_load(reinterpret_cast<const Half *>(k + g * (D / 16))),
-                           b = __builtin_nontemporal_load(reinterpret_cast<const Half *>(k + D / 4 + g * (D / 16)));
+                const Half a = __builtin_nontemporal_load(reinterpret_cast<const Half *>(Kc + (size_t)off)),
+                           b = __builtin_nontemporal_load(reinterpret_cast<const Half *>(Kc + (size_t)(off + D / 4)));
 #pragma unroll
-                for (int ks = 0; ks < KS2; ++ks) r.k[t][ks] = a[ks], r.k[t][ks + KS2] = b[ks];
+                for (int ks = 0; ks < KS2; ++ks) rows.k[t][ks] = a[ks], rows.k[t][ks + KS2] = b[ks];
+#pragma unroll
+                for (int i = 0; i < D / 64; ++i)  // (4 c d < 2^32; beyond the end: masked)
+                    rows.base[t][i] = *reinterpret_cast<const float *>(reinterpret_cast<const char *>(rope) +
+                                                                       (size_t)((uint32_t)(max(nv - 1 - eb - 4 * t, 0) * D + 64 * i + lane) * 4u));
             } else {
-                r.k[t] = __builtin_nontemporal_load(reinterpret_cast<const RowCodes<D> *>(k + g * (D / 8)));
+                rows.k[t] = __builtin_nontemporal_load(reinterpret_cast<const RowCodes<D> *>(Kc + (size_t)off));
             }
-            r.v[t] = __builtin_nontemporal_load(reinterpret_cast<const RowCodes<D> *>(v));
-            r.ks[t] = __builtin_nontemporal_load(Ks + slot), r.vs[t] = __builtin_nontemporal_load(Vs + slot);
+            rows.ks[t] = __builtin_nontemporal_load(reinterpret_cast<const Fp4Scales<D> *>(Ks + (size_t)(slot[t] * (D / 32))));
+        }
+    };
+    auto request_values = [&](Rows &rows, const uint32_t (&slot)[2]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            rows.v[t] = __builtin_nontemporal_load(reinterpret_cast<const RowCodes<D> *>(Vc + (size_t)(slot[t] * (D / 2) + g * (D / 8))));
+            rows.vs[t] = __builtin_nontemporal_load(reinterpret_cast<const Fp4Scales<D> *>(Vs + (size_t)(slot[t] * (D / 32))));
         }
     };
 
-    // cos / sin of the lane's two rows' places within a block
-    float rc[2][KS2][8], rs[2][KS2][8];
-    if constexpr (ROPE) {
+    int eb = e0 + wave * kRows;
+    // cos / sin of the place of the lane's row krow within a block (that of row krow + 4 is the same behind entry 4): the table's rows 0 .. 31 pass through
+    // LDS, where the V stages lie later, with the 16-byte chunks of a row permuted (row by row from memory, an instruction is 64 pieces of 16 bytes)
+    float rc[KS2][8], rs[KS2][8];
+    constexpr int STEP = NW * kRows, DEPTH = kDepth<D, ROPE>;
+    Rows ring[DEPTH];
+    auto request_first = [&] {
+        if (eb >= e1) return;
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const float *row = rope + (long)min(krow + 4 * t, n_pos - 1) * D + (D / 8) * g;
-#pragma unroll
-            for (int ks = 0; ks < KS2; ++ks)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) rc[t][ks][e] = row[8 * ks + e], rs[t][ks][e] = row[D / 2 + 8 * ks + e];
+        for (int i = 0; i < DEPTH; ++i) {
+            const int at = eb + i * STEP;
+            uint32_t slot[2];
+            find_slots(at, slot);
+            request_keys(ring[i], at, slot);
+            request_values(ring[i], slot);
         }
+    };
+    if constexpr (ROPE) {
+        constexpr int CH = D / 4, N = kRows * CH / (64 * NW);
+        static_assert(kRows * D * 4 <= NW * STAGE, "the table's rows fit the stages");
+        f32x4 t[N];
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int i = tid + n * 64 * NW, r = i / CH;
+            t[n] = *reinterpret_cast<const f32x4 *>(rope + (long)min(r, n_pos - 1) * D + (i % CH) * 4);
+        }
+        request_first();
+        const uint32_t t_lds = lds_addr(&smem[0][0]);
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int i = tid + n * 64 * NW, r = i / CH;
+            lds_write_b128_at(t_lds + r * D * 4 + (((uint32_t)(i % CH) ^ chunk_swizzle<128>(r)) << 4), t[n]);
+        }
+        auto barrier = [] {  // of LDS alone: a __syncthreads would also wait for the rows
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+        };
+        barrier();
+#pragma unroll
+        for (int ks = 0; ks < KS2; ++ks)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t row = t_lds + krow * D * 4, chunk = ((D / 8) * g + 8 * ks + 4 * h) / 4, swz = chunk_swizzle<128>(krow);
+                const f32x4 c = lds_read_f32x4_at(row + ((chunk ^ swz) << 4)), sn = lds_read_f32x4_at(row + (((D / 8 + chunk) ^ swz) << 4));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) rc[ks][4 * h + e] = c[e], rs[ks][4 * h + e] = sn[e];
+            }
+        barrier();
+    } else {
+        request_first();
     }
 
-    const uint32_t v_lds = lds_addr(&smem[wave][0]);
+    const uint32_t v_lds = lds_addr(&smem[wave][0]), b_lds = lds_addr(&base_s[ROPE ? wave : 0][0][0]);
     const int vrow = 8 * g + (col >> 2);  // transposed reads: rows vrow, vrow + 4, columns 16 db + 4 (col % 4)
     const uint32_t kswz = chunk_swizzle<D>(krow), vswz = chunk_swizzle<D>(vrow);  // the same for rows + 4
-    const uint32_t vwrite = v_lds + krow * D * 2, vread = v_lds + vrow * D * 2 + ((col & 1) << 3);
+    // Stages start at multiples of 256 bytes, so that the permuted chunk is an XOR into the address: one instruction per access in the loop (kept there by
+    // the empty statements), not a register per access
+    static_assert(STAGE % 256 == 0, "");
+    uint32_t vwrite = v_lds + krow * D * 2 + (((uint32_t)(KSTEPS * g) ^ kswz) << 4);
+    uint32_t vread = v_lds + vrow * D * 2 + ((col & 1) << 3) + ((((uint32_t)(col & 3) >> 1) ^ vswz) << 4);
     const float sl2 = p.scale * kLog2e_f;
     f32x4 acc[DB];
 #pragma unroll
     for (int db = 0; db < DB; ++db) acc[db] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m_run = -INFINITY, l_run = 0.f;
 
-    int eb = e0 + wave * kRows;
-    Rows now, next;
-    if (eb < e1) request(eb, now);
-    for (; eb < e1; eb += NW * kRows, now = next) {
-        if (eb + NW * kRows < e1) request(eb + NW * kRows, next);
+    auto work = [&](Rows &rows) __attribute__((always_inline)) {
+        // (requested in any case, beyond the end as the last entry again: behind a branch the compiler could not count the loads, and would wait for all)
+        uint32_t next[2];
+        find_slots(eb + DEPTH * STEP, next);
         // ---- scores
         f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
         if constexpr (ROPE) {
-            const float *base = rope + (long)(nv - 1 - eb) * D + (D / 8) * g;
 #pragma unroll
-            for (int ks = 0; ks < KS2; ++ks) {
-                float bc[8], bs[8];
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) bc[e] = base[8 * ks + e], bs[e] = base[D / 2 + 8 * ks + e];
+                for (int i = 0; i < D / 64; ++i) base_s[wave][t][64 * i + lane] = rows.base[t][i];
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int ks = 0; ks < KS2; ++ks) {
+                    f32x4 bc[2], bs[2];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        bc[h] = lds_read_f32x4_at(b_lds + (t * D + (D / 8) * g + 8 * ks + 4 * h) * 4);
+                        bs[h] = lds_read_f32x4_at(b_lds + (t * D + D / 2 + (D / 8) * g + 8 * ks + 4 * h) * 4);
+                    }
                     float x[8], y[8];
-                    fp4_to_f32(now.k[t][ks], fp4_scale(now.ks[t], D == 128 ? g >> 1 : 0), x);
-                    fp4_to_f32(now.k[t][ks + KS2], fp4_scale(now.ks[t], D == 128 ? 2 + (g >> 1) : 1), y);
+                    fp4_to_f32(rows.k[t][ks], fp4_scale(rows.ks[t], D == 128 ? g >> 1 : 0), x);
+                    fp4_to_f32(rows.k[t][ks + KS2], fp4_scale(rows.ks[t], D == 128 ? 2 + (g >> 1) : 1), y);
                     f32x8 u, v;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {  // R(-distance): the distance is that of the block's first entry minus the row's place
-                        const float c = fmaf(bs[e], rs[t][ks][e], bc[e] * rc[t][ks][e]), sn = fmaf(-bc[e], rs[t][ks][e], bs[e] * rc[t][ks][e]);
+                    for (int e = 0; e < 8; ++e) {  // R(-distance): the distance is that of the block's entry 0 (4) minus the row's place behind it
+                        const float c0 = bc[e >> 2][e & 3], s0 = bs[e >> 2][e & 3];
+                        const float c = fmaf(s0, rs[ks][e], c0 * rc[ks][e]), sn = fmaf(-c0, rs[ks][e], s0 * rc[ks][e]);
                         u[e] = fmaf(y[e], sn, x[e] * c);
                         v[e] = fmaf(-x[e], sn, y[e] * c);
                     }
@@ -214,26 +331,31 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_fp4_kernel(sepkv_params p, 
                                 s[t] = mfma16(ku[i], query[ks][j], s[t]);
                                 s[t] = mfma16(kv_[i], query[ks + KS2][j], s[t]);
                             }
+                    __builtin_amdgcn_sched_barrier(0);  // one piece at a time: their values together do not leave room for three waves
                 }
-            }
         } else {
 #pragma unroll
             for (int ks = 0; ks < KSTEPS; ++ks)
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
-                    const bf16x8 a = __builtin_bit_cast(bf16x8, fp4_to_bf16(now.k[t][ks], fp4_scale(now.ks[t], D == 128 ? g : g >> 1)));
+                    const bf16x8 a = __builtin_bit_cast(bf16x8, fp4_to_bf16(rows.k[t][ks], fp4_scale(rows.ks[t], D == 128 ? g : g >> 1)));
 #pragma unroll
                     for (int j = 0; j < QP; ++j) s[t] = mfma16(a, query[ks][j], s[t]);
                 }
         }
+        __builtin_amdgcn_sched_barrier(0);
+        request_keys(rows, eb + DEPTH * STEP, next);
         // ---- V rows into LDS
+        asm volatile("" : "+v"(vwrite), "+v"(vread));
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int ks = 0; ks < KSTEPS; ++ks) {
-                const fp4_bf16x8 v = fp4_to_bf16(now.v[t][ks], fp4_scale(now.vs[t], D == 128 ? g : g >> 1));
-                lds_write_b128_at(vwrite + 4 * t * D * 2 + (((uint32_t)(KSTEPS * g + ks) ^ kswz) << 4), __builtin_bit_cast(f32x4, v));
+                const fp4_bf16x8 v = fp4_to_bf16(rows.v[t][ks], fp4_scale(rows.vs[t], D == 128 ? g : g >> 1));
+                lds_write_b128_at((vwrite ^ (uint32_t)(ks << 4)) + 4 * t * D * 2, __builtin_bit_cast(f32x4, v));
             }
+        __builtin_amdgcn_sched_barrier(0);
+        request_values(rows, next);
         // ---- weights
         float x[8] = {s[0][0], s[0][1], s[0][2], s[0][3], s[1][0], s[1][1], s[1][2], s[1][3]};  // rows 8g .. 8g+7 of the block
         const int n_valid = e1 - eb;
@@ -263,9 +385,17 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_fp4_kernel(sepkv_params p, 
         // ---- output
 #pragma unroll
         for (int db = 0; db < DB; ++db) {
-            const bf16x8 v = lds_read_tr_at(vread + (((uint32_t)(2 * db + ((col & 3) >> 1)) ^ vswz) << 4), 4 * D * 2);
+            const bf16x8 v = lds_read_tr_at(vread ^ (uint32_t)(db << 5), 4 * D * 2);
 #pragma unroll
             for (int i = 0; i < WP; ++i) acc[db] = mfma16(v, w[i], acc[db]);
+        }
+        eb += STEP;
+    };
+    while (eb < e1) {
+        work(ring[0]);
+        if constexpr (DEPTH == 2) {
+            if (eb >= e1) break;
+            work(ring[1]);
         }
     }
 
@@ -279,82 +409,189 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_fp4_kernel(sepkv_params p, 
         for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4 *>(r + 16 * db + 4 * g) = acc[db];
     }
     __syncthreads();
-    for (int item = tid; item < heads * D; item += 64 * NW) {
-        const int h = item / D, c = item % D;
-        float M = -INFINITY, lsum = 0.f, o = 0.f;
-#pragma unroll
-        for (int w = 0; w < NW; ++w) M = fmaxf(M, reinterpret_cast<const float *>(&smem[w][0])[h * RF + D]);
+    // the word in which this pair's slices are counted, and the records behind all words
+    const long pair = head * chunks + first / kColumns;
+    uint64_t *const arrived = reinterpret_cast<uint64_t *>(ws + pair * kWordPitch);
+    float *const recs = reinterpret_cast<float *>(ws + words_bytes((long)p.S * p.Hkv * chunks)) + ((long)sq * p.Hq + h0) * nsplit * PF;
+    uint64_t seen = 0;
+    if constexpr (ADD) {
+        if (tid == 0) seen = arrival_seen(arrived);
+    }
+    for (int item = tid; item < heads * (D / 2); item += 64 * NW) {  // two columns per thread
+        const int h = item / (D / 2), c2 = item % (D / 2);
+        float2 ml[NW], o[NW];
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
             const float *r = reinterpret_cast<const float *>(&smem[w][0]) + h * RF;
-            const float wgt = r[D] == -INFINITY ? 0.f : exp2f(r[D] - M);
-            lsum = fmaf(wgt, r[D + 1], lsum);
-            o = fmaf(wgt, r[c], o);
+            ml[w] = *reinterpret_cast<const float2 *>(r + D), o[w] = *reinterpret_cast<const float2 *>(r + 2 * c2);
+        }
+        float M = -INFINITY, lsum = 0.f, o0 = 0.f, o1 = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) M = fmaxf(M, ml[w].x);
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const float wgt = ml[w].x == -INFINITY ? 0.f : exp2f(ml[w].x - M);
+            lsum = fmaf(wgt, ml[w].y, lsum), o0 = fmaf(wgt, o[w].x, o0), o1 = fmaf(wgt, o[w].y, o1);
         }
         const long sh = (long)sq * p.Hq + h0 + h;
-        if (nsplit == 1) {
-            finish<T>(nv, M, lsum, o, out + sh * D + c, lse && c == 0 ? lse + sh : nullptr);
+        if (!ADD && nsplit == 1) {
+            finish<T>(nv, M, lsum, o0, out + sh * D + 2 * c2, nullptr);
+            finish<T>(nv, M, lsum, o1, out + sh * D + 2 * c2 + 1, lse && c2 == 0 ? lse + sh : nullptr);
         } else {
-            float *rec = part + (sh * nsplit + split) * PF;
-            rec[2 + c] = o;
-            if (c == 0) rec[0] = M, rec[1] = lsum;
+            float *rec = recs + (h * nsplit + split) * PF;
+            if constexpr (ADD) {
+                publish(rec + 2 + 2 * c2, float2{o0, o1});
+                if (c2 == 0) publish(rec, float2{M, lsum});
+            } else {
+                *reinterpret_cast<float2 *>(rec + 2 + 2 * c2) = float2{o0, o1};
+                if (c2 == 0) *reinterpret_cast<float2 *>(rec) = float2{M, lsum};
+            }
         }
+    }
+    if constexpr (!ADD) return;
+
+    // ---- the workgroup that finishes last adds the slices' records, in slice order, whichever it is
+    __shared__ int last_s;
+    if (tid == 0) arrival_ready(arrived, seen, one, nsplit);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's part of the record is where every XCD sees it
+    __syncthreads();
+    if (tid == 0) last_s = arrives_last(arrived, one, nsplit);
+    __syncthreads();
+    if (!last_s) return;
+    if (tid == 0) arrival_reset(arrived);
+    for (int item = tid; item < heads * (D / 2); item += 64 * NW) {
+        const int h = item / (D / 2), c2 = item % (D / 2);
+        const float *rec = recs + h * nsplit * PF;
+        float2 ml[kMostAdded], o[kMostAdded];
+#pragma unroll
+        for (int k = 0; k < kMostAdded; ++k)
+            if (k < nsplit) ml[k] = fetch_published(rec + k * PF), o[k] = fetch_published(rec + k * PF + 2 + 2 * c2);
+        // every sum in the order in which merge_fp4_kernel forms it: captured calls, which that kernel finishes, give the same bits
+        float M = -INFINITY, wgt[kMostAdded], sum[kMostAdded], o0 = 0.f, o1 = 0.f;
+#pragma unroll
+        for (int k = 0; k < kMostAdded; ++k)
+            if (k < nsplit) M = fmaxf(M, ml[k].x);
+#pragma unroll
+        for (int k = 0; k < kMostAdded; ++k) {
+            wgt[k] = k >= nsplit || ml[k].x == -INFINITY ? 0.f : exp2f(ml[k].x - M);
+            sum[k] = k < nsplit ? wgt[k] * ml[k].y : 0.f;
+        }
+#pragma unroll
+        for (int x = kMostAdded / 2; x > 0; x /= 2)
+#pragma unroll
+            for (int k = 0; k < x; ++k) sum[k] += sum[k + x];
+        const float lsum = sum[0];
+#pragma unroll
+        for (int i = 0; i < kMergeParts<D>; ++i) {
+            float a0 = 0.f, a1 = 0.f;
+#pragma unroll
+            for (int k = i; k < kMostAdded; k += kMergeParts<D>)
+                if (k < nsplit) a0 = fmaf(wgt[k], o[k].x, a0), a1 = fmaf(wgt[k], o[k].y, a1);
+            o0 += a0, o1 += a1;
+        }
+        const long sh = (long)sq * p.Hq + h0 + h;
+        finish<T>(nv, M, lsum, o0, out + sh * D + 2 * c2, nullptr);
+        finish<T>(nv, M, lsum, o1, out + sh * D + 2 * c2 + 1, lse && c2 == 0 ? lse + sh : nullptr);
     }
 }
 
-// the slices' records of a (sequence, query head)
+// The slices' records of a (sequence, query head), where there are several.  Thread k of the first wave has slice k's maximum and sum (there are at most
+// 64), all of them its weight through LDS; the records are requested before that is known.
 template <typename T, int D>
-__global__ void merge_fp4_kernel(sepkv_params p, int nsplit, const int32_t *__restrict__ sizes, const float *__restrict__ part, T *__restrict__ out,
-                                 float *__restrict__ lse) {
-    constexpr int PF = D + 2;
+__global__ __launch_bounds__(256) void merge_fp4_kernel(sepkv_params p, int nsplit, const int32_t *__restrict__ sizes, const float *__restrict__ part,
+                                                         T *__restrict__ out, float *__restrict__ lse) {
+    constexpr int PF = D + 2, PARTS = kMergeParts<D>, N = kMostSlices / PARTS;  // a thread: two columns, every PARTS-th slice
+    __shared__ float weight[kMostSlices], sums[PARTS][D];
+    __shared__ float2 state;
     const long sh = blockIdx.x;
     const CacheMap cm = cache_map(p, sizes + SEPKV_SIZES_COLS * (sh / p.Hq));
-    const int c = threadIdx.x;
+    const int c2 = threadIdx.x % (D / 2), which = threadIdx.x / (D / 2);
     const float *r = part + sh * nsplit * PF;
-    float M = -INFINITY, lsum = 0.f, o = 0.f;
-    for (int k = 0; k < nsplit; ++k) M = fmaxf(M, r[k * PF]);
-    for (int k = 0; k < nsplit; ++k) {
-        const float *rec = r + k * PF;
-        const float wgt = rec[0] == -INFINITY ? 0.f : exp2f(rec[0] - M);
-        lsum = fmaf(wgt, rec[1], lsum);
-        o = fmaf(wgt, rec[2 + c], o);
+    float2 o[N];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const int k = which + n * PARTS;
+        o[n] = k < nsplit ? *reinterpret_cast<const float2 *>(r + k * PF + 2 + 2 * c2) : float2{0.f, 0.f};
     }
-    finish<T>(cm.n_init + cm.n_sep + cm.n_past + cm.n_loc, M, lsum, o, out + sh * D + c, lse && c == 0 ? lse + sh : nullptr);
+    if (threadIdx.x < 64) {
+        const int k = threadIdx.x;
+        const float2 ml = k < nsplit ? *reinterpret_cast<const float2 *>(r + k * PF) : float2{-INFINITY, 0.f};
+        float M = ml.x;
+#pragma unroll
+        for (int x = 32; x > 0; x /= 2) M = fmaxf(M, __shfl_xor(M, x));
+        const float w = ml.x == -INFINITY ? 0.f : exp2f(ml.x - M);
+        float sum = w * ml.y;
+#pragma unroll
+        for (int x = 32; x > 0; x /= 2) sum += __shfl_xor(sum, x);
+        weight[k] = w;
+        if (k == 0) state = float2{M, sum};
+    }
+    __syncthreads();
+    float o0 = 0.f, o1 = 0.f;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const float w = weight[which + n * PARTS];
+        o0 = fmaf(w, o[n].x, o0), o1 = fmaf(w, o[n].y, o1);
+    }
+    sums[which][2 * c2] = o0, sums[which][2 * c2 + 1] = o1;
+    __syncthreads();
+    const int c = threadIdx.x;
+    if (c >= D) return;
+    float total = 0.f;
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) total += sums[i][c];
+    finish<T>(cm.n_init + cm.n_sep + cm.n_past + cm.n_loc, state.x, state.y, total, out + sh * D + c, lse && c == 0 ? lse + sh : nullptr);
 }
 
 int chunks_of(const sepkv_params &p) { return (p.Hq / p.Hkv + kColumns - 1) / kColumns; }
 
-int slices_of(const sepkv_params &p, int units) {
-    const long pairs = (long)p.S * p.Hkv * chunks_of(p), fit = 2L * units / pairs;
-    const int nb = (p.c + kRows - 1) / kRows;
-    long n = (nb + 7) / 8;
-    if (n > fit) n = fit;
-    return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
+struct Shape {
+    int nsplit;
+    bool add;  // the kernel adds the slices itself
+};
+// Enough slices for two workgroups per compute unit, for four where these still have 32 blocks, eight a wave.  Measured in us with 2 / 4 per unit (bf16,
+// d = 128, 32 query heads on 8 KV heads):  4 sequences of 65536 entries (16 or 32 slices, 128 or 64 blocks) 32.1 / 29.8, with positions
+// 59.5 / 50.9;  32 of 3332 (2 or 4, 53 or 27 blocks) 20.5 / 21.9;  8 of 8192 (8 or 16, 32 or 16) 15.8 / 18.0;  64 of 300 (1 or 2, 10 or 5) 8.0 / 11.6.
+Shape shape_of(const sepkv_params &p, int units) {
+    const long pairs = (long)p.S * p.Hkv * chunks_of(p);
+    const int nb = (p.c + kRows - 1) / kRows, row = p.Hq / p.Hkv * p.d;
+    long n = 4L * units / pairs;
+    if (n * kManyBlocks > nb) n = 2L * units / pairs;
+    const long most = (nb + kLeastBlocks - 1) / kLeastBlocks;
+    if (n > most) n = most;
+    Shape x = {(int)(n < 1 ? 1 : n > kMostSlices ? kMostSlices : n), false};
+    x.add = x.nsplit > 1 && x.nsplit <= kMostAdded && row <= 1024 && x.nsplit * row <= 8192;
+    return x;
 }
 
 }  // namespace
 
 size_t decode_fp4_workspace(const sepkv_params &p) {
-    return align_up((size_t)p.S * p.Hq * slices_of(p, compute_units()) * (p.d + 2) * sizeof(float), 256);
+    return words_bytes((long)p.S * p.Hkv * chunks_of(p)) +
+           align_up((size_t)p.S * p.Hq * shape_of(p, compute_units()).nsplit * (p.d + 2) * sizeof(float), 256);
 }
 
 int launch_decode_fp4(const sepkv_params &p, const void *q, const Fp4Cache &cache, const int32_t *sizes, const float *rope, int n_pos, void *out,
                       float *lse, void *ws, hipStream_t st) {
-    const int G = p.Hq / p.Hkv, nsplit = slices_of(p, compute_units());
-    float *part = static_cast<float *>(ws);
-    constexpr int NW = 8;
+    const int G = p.Hq / p.Hkv, chunks = chunks_of(p);
+    const Shape shape = shape_of(p, compute_units());
+    const bool add = shape.add && !being_captured(st);  // else a merge launch adds the slices
+    const uint64_t one = add ? launch_number() : 0;
     auto go = [&](auto T_, auto D_, auto ROPE_) {
         using T = decltype(T_);
         constexpr int D = decltype(D_)::value;
-        {
+        auto launch = [&](auto ADD_) {
             ProfScope prof(SEPATTN_K_DECODE_SPLIT, st);
-            hipLaunchKernelGGL((decode_fp4_kernel<T, D, decltype(ROPE_)::value, NW>), dim3(nsplit, p.Hkv * chunks_of(p), p.S), dim3(64 * NW), 0, st, p, G,
-                               n_pos, static_cast<const T *>(q), cache, sizes, rope, part, static_cast<T *>(out), lse);
-        }
-        if (nsplit == 1) return launch_status();
+            hipLaunchKernelGGL((decode_fp4_kernel<T, D, decltype(ROPE_)::value, decltype(ADD_)::value>), dim3(shape.nsplit, p.Hkv * chunks, p.S),
+                               dim3(64 * kWaves), 0, st, p, G, n_pos, static_cast<const T *>(q), cache, sizes, rope, one, static_cast<char *>(ws),
+                               static_cast<T *>(out), lse);
+        };
+        add ? launch(std::true_type{}) : launch(std::false_type{});
+        if (shape.nsplit == 1 || add) return launch_status();
         if (hipGetLastError() != hipSuccess) return (int)SEPATTN_ERR_HIP;
         ProfScope prof(SEPATTN_K_DECODE_MERGE, st);
-        hipLaunchKernelGGL((merge_fp4_kernel<T, D>), dim3(p.S * p.Hq), dim3(D), 0, st, p, nsplit, sizes, part, static_cast<T *>(out), lse);
+        hipLaunchKernelGGL((merge_fp4_kernel<T, D>), dim3(p.S * p.Hq), dim3(256), 0, st, p, shape.nsplit, sizes,
+                           reinterpret_cast<const float *>(static_cast<char *>(ws) + words_bytes((long)p.S * p.Hkv * chunks)), static_cast<T *>(out), lse);
         return launch_status();
     };
     auto with = [&](auto T_, auto D_) { return rope ? go(T_, D_, std::true_type{}) : go(T_, D_, std::false_type{}); };

@@ -14,8 +14,11 @@ namespace sepattn {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kFillSlots = 128;  // cache slots per workgroup of the hand-over
-constexpr int kFillUnroll = 8;   // rows a thread has in flight
+// Cache slots per workgroup and rows that a thread has in flight.  8 sequences, 8 KV heads of 128, bf16, 3332 slots: the hand-over takes 21.2 us with 64 slots
+// and 4 rows, 23.6 with 32 and 2 or 256 and 8;  in fp32, 3 sequences, 12 heads of 64, 601 slots 5.4, 6.8 with 128 and 8.  The expansion 20.2 us with 32 and 2,
+// 22.5 with 64 and 4, 23.8 with 128 and 8.
+constexpr int kFillSlots = 64, kFillRows = 4;
+constexpr int kExpandSlots = 32, kExpandRows = 2;
 
 // eight values of T
 template <typename T>
@@ -82,10 +85,10 @@ __global__ __launch_bounds__(kThreads) void fill_fp4_kernel(sepkv_params p, int 
     Fp4Scales<D> *scales = reinterpret_cast<Fp4Scales<D> *>(which ? cache.Vs : cache.Ks) + head * p.c;
     constexpr int PIECES = D / 8, ROWS = kThreads / PIECES;
     const int r_in = threadIdx.x / PIECES, piece = threadIdx.x % PIECES, t_end = min((int)(blockIdx.x + 1) * kFillSlots, p.c);
-    for (int t0 = blockIdx.x * kFillSlots; t0 < t_end; t0 += ROWS * kFillUnroll) {
-        int from[kFillUnroll];  // source position of the slot, -1: the slot is not in use
+    for (int t0 = blockIdx.x * kFillSlots; t0 < t_end; t0 += ROWS * kFillRows) {
+        int from[kFillRows];  // source position of the slot, -1: the slot is not in use
 #pragma unroll
-        for (int u = 0; u < kFillUnroll; ++u) {
+        for (int u = 0; u < kFillRows; ++u) {
             const int t = t0 + u * ROWS + r_in;
             from[u] = -1;
             if (t >= t_end) continue;
@@ -98,14 +101,14 @@ __global__ __launch_bounds__(kThreads) void fill_fp4_kernel(sepkv_params p, int 
                 from[u] = wstart + t - p.a - p.s;
             }
         }
-        Eight<T> v[kFillUnroll];
+        Eight<T> v[kFillRows];
 #pragma unroll
-        for (int u = 0; u < kFillUnroll; ++u) {
+        for (int u = 0; u < kFillRows; ++u) {
             v[u].clear();
             if (from[u] >= 0) v[u].stream(src + (long)from[u] * D + piece * 8);
         }
 #pragma unroll
-        for (int u = 0; u < kFillUnroll; ++u) {
+        for (int u = 0; u < kFillRows; ++u) {
             const int t = t0 + u * ROWS + r_in;
             Fp4Piece f = v[u].template round<D>(piece);  // (all lanes of a row take part)
             if (from[u] < 0) f = {0u, 0u};
@@ -206,9 +209,9 @@ __global__ __launch_bounds__(kThreads) void expand_fp4_kernel(sepkv_params p, co
     const uint32_t *codes = reinterpret_cast<const uint32_t *>(which ? cache.Vc : cache.Kc) + head * p.c * (D / 8);
     const Fp4Scales<D> *scales = reinterpret_cast<const Fp4Scales<D> *>(which ? cache.Vs : cache.Ks) + head * p.c;
     T *dst = (which ? V : K) + head * p.c * D;
-    constexpr int PIECES = D / 8, ROWS = kThreads / PIECES, N = kFillUnroll;
-    const int r_in = threadIdx.x / PIECES, piece = threadIdx.x % PIECES, t_end = min((int)(blockIdx.x + 1) * kFillSlots, p.c);
-    for (int t0 = blockIdx.x * kFillSlots; t0 < t_end; t0 += ROWS * N) {
+    constexpr int PIECES = D / 8, ROWS = kThreads / PIECES, N = kExpandRows;
+    const int r_in = threadIdx.x / PIECES, piece = threadIdx.x % PIECES, t_end = min((int)(blockIdx.x + 1) * kExpandSlots, p.c);
+    for (int t0 = blockIdx.x * kExpandSlots; t0 < t_end; t0 += ROWS * N) {
         uint32_t c[N], s[N];
 #pragma unroll
         for (int u = 0; u < N; ++u) {
@@ -280,7 +283,7 @@ int launch_append_fp4(const sepkv_params &p, const TokenTurn *turn, const void *
 }
 
 int launch_expand_fp4(const sepkv_params &p, const int32_t *sizes, const Fp4Cache &cache, void *K, void *V, hipStream_t st) {
-    const dim3 grid((p.c + kFillSlots - 1) / kFillSlots, 2 * p.S * p.Hkv);
+    const dim3 grid((p.c + kExpandSlots - 1) / kExpandSlots, 2 * p.S * p.Hkv);
     by_type(p, [&](auto T_, auto D_) {
         using T = decltype(T_);
         hipLaunchKernelGGL((expand_fp4_kernel<T, decltype(D_)::value>), grid, dim3(kThreads), 0, st, p, sizes, cache, static_cast<T *>(K),

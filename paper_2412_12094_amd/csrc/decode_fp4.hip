@@ -14,6 +14,8 @@
 //
 // Operand layouts of 16x16x32 and the order of a block's rows as in decode_wide.hip: row 4g+i of score tile t is row 8g+4t+i of the block, so
 // that a lane group's scores are the k-slots that it holds of the weights as B operand.
+#include <algorithm>
+
 #include "common.h"
 #include "decode_common.h"
 #include "fp4.h"
@@ -33,9 +35,10 @@ constexpr int kWaves = 4;
 template <int D, bool ROPE>
 constexpr int kDepth = D == 64 && !ROPE ? 2 : 1;  // blocks of a wave on their way
 constexpr int kLeastBlocks = kWaves;  // of a slice
-constexpr int kManyBlocks = 32;       // of a slice that leaves room for four workgroups per compute unit
+constexpr int kManyBlocks = 20;       // of a slice where there is more than one workgroup per compute unit
 constexpr int kMostSlices = 64;       // of a sequence
-constexpr int kMostAdded = 16;        // slices that the kernel itself adds, at most
+constexpr int kMostAdded = 16;        // of a sequence whose slices the kernel itself adds
+constexpr int kMostDivided = 512;     // sequences of a call in which they are cut
 constexpr int kWordPitch = 128;  // bytes: a cache line for each word in which slices are counted
 __host__ __device__ inline size_t words_bytes(long pairs) { return align_up((size_t)pairs * kWordPitch, 256); }
 
@@ -127,13 +130,86 @@ struct Runs {
     }
 };
 
+// How sequences are cut into slices.  Their lengths stand on the device, and those of a batch differ, so every workgroup finds its slice by itself, a
+// sequence per lane.  With T blocks in all sequences a slice has at most  share = max(kLeastBlocks, min(T / one, max(many, T / all)))  blocks, where `one`
+// and `all` are the workgroups that one (KV head, 16 query heads) has if there is one per compute unit and if there are as many as it holds: more than one
+// only where slices stay long enough to pay for being added.  A sequence of nb blocks has ceil(nb / share) slices, at least 1, at most `most`; they are
+// numbered through all sequences and at most  all + S.  (most 1: the slices are the sequences.)
+// Against as many slices for every sequence of the batch, chosen by the capacity (bf16, d = 128, 32 query heads on 8 KV heads): 32 sequences of 1 to 3277
+// entries 20.5 -> 18.8 us, with positions 36.5 -> 30.1; 8 of up to 8192 15.8 -> 14.5; 4 of up to 53019 29.7 -> 30.8, where memory was the bound and the
+// search is on the way.  With positions and equal lengths of 1706 entries, one, two and three workgroups per unit take 29.8, 27.7 and 26.8 us.
+struct Plan {
+    int most, many;
+    float per_one, per_all;  // 1 / one, 1 / all
+};
+struct Slice {
+    int sq, index, count, before;  // sequence, which of its slices, how many it has (0: there is no such slice), slices of the sequences in front of it
+    CacheMap map;
+};
+// sums over the lanes up to this one
+__device__ inline int lanes_sum(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);  // row_shr 1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);  // row_bcast 15, 31: of a row to the next, of two to the last two
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
+    return x;
+}
+__device__ inline int blocks_of(const CacheMap &m) { return (m.n_init + m.n_sep + m.n_past + m.n_loc + kRows - 1) / kRows; }
+// slice number `want`; `want` < 0: the first one of sequence -1 - want
+__device__ inline Slice slice_of(const sepkv_params &p, const Plan &plan, const int32_t *__restrict__ sizes, int want) {
+    if (plan.most == 1) {
+        if (want >= p.S) return {0, 0, 0, 0, {}};
+        const int sq = want < 0 ? -1 - want : want;
+        return {sq, 0, 1, sq, cache_map(p, sizes + SEPKV_SIZES_COLS * sq)};
+    }
+    auto count_of = [&](int nb, float per_share) { return min(1 + small_quotient(max(nb - 1, 0), per_share), plan.most); };  // (c d < 2^30, so nb < 2^19)
+    auto share_of = [&](int total) {  // (512 sequences: below 2^28; rounded in fp32, alike in every workgroup)
+        return max(kLeastBlocks, min((int)((float)total * plan.per_one), max(plan.many, (int)((float)total * plan.per_all))) + 1);
+    };
+    if (p.S == 1) {
+        const CacheMap m = cache_map(p, sizes);
+        const int nb = blocks_of(m), n = __builtin_amdgcn_readfirstlane(count_of(nb, reciprocal(share_of(nb))));
+        return {0, max(want, 0), want < n ? n : 0, 0, m};
+    }
+    const int lane = threadIdx.x & 63;
+    CacheMap m;
+    int total = 0, before = 0;
+    for (int s0 = (p.S - 1) & ~63; s0 >= 0; s0 -= 64) {  // (the first ones last: theirs are at hand then)
+        m = cache_map(p, sizes + SEPKV_SIZES_COLS * min(s0 + lane, p.S - 1));
+        total += s0 + lane < p.S ? blocks_of(m) : 0;
+    }
+    const float per_share = reciprocal(share_of(__builtin_amdgcn_readlane(lanes_sum(total), 63)));
+    for (int s0 = 0;; s0 += 64) {
+        const int n = s0 + lane < p.S ? count_of(blocks_of(m), per_share) : 0, upto = lanes_sum(n), front = before + upto - n;
+        const uint64_t found = __builtin_amdgcn_ballot_w64(want < 0 ? s0 + lane == -1 - want : want >= front && want < front + n);
+        if (found) {
+            const int l = __builtin_ctzll(found);
+            auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
+            return {s0 + l, max(want - of(front), 0), of(n), of(front),
+                    {of(m.n_init), of(m.n_sep), of(m.n_past), of(m.n_loc), of(m.sep_head), of(m.win_head), p.a, p.s, m.wcap}};
+        }
+        if (s0 + 64 >= p.S) return {0, 0, 0, 0, m};
+        before += __builtin_amdgcn_readlane(upto, 63);
+        m = cache_map(p, sizes + SEPKV_SIZES_COLS * min(s0 + 64 + lane, p.S - 1));
+    }
+}
+
+__device__ inline Slice find_slice(const sepkv_params &p, const Plan &plan, const int32_t *__restrict__ sizes, int want) {
+    const Slice x = slice_of(p, plan, sizes, want);
+    auto s = [](int v) { return __builtin_amdgcn_readfirstlane(v); };  // (the same in all lanes, which the compiler does not see)
+    return {s(x.sq), s(x.index), s(x.count), s(x.before),
+            {s(x.map.n_init), s(x.map.n_sep), s(x.map.n_past), s(x.map.n_loc), s(x.map.sep_head), s(x.map.win_head), p.a, p.s, p.c - p.a - p.s}};
+}
+
 template <int D>
 constexpr int kMergeParts = 256 / (D / 2);  // threads of the merge launch that share two columns
 
 // ADD: the slices of a sequence are added by the workgroup that finishes last.  Otherwise, where there are several, they are left to a merge launch.
 template <typename T, int D, bool ROPE, bool ADD>
 __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, ROPE>)) void decode_fp4_kernel(
-    sepkv_params p, int G, int n_pos, const T *__restrict__ q, Fp4Cache cache, const int32_t *__restrict__ sizes, const float *__restrict__ rope,
+    sepkv_params p, Plan plan, int G, int n_pos, const T *__restrict__ q, Fp4Cache cache, const int32_t *__restrict__ sizes, const float *__restrict__ rope,
     uint64_t one, char *__restrict__ ws, T *__restrict__ out, float *__restrict__ lse) {
     constexpr int KSTEPS = D / 32, KS2 = KSTEPS / 2, DB = D / 16, NW = kWaves;
     constexpr int QP = Precision<T>::kQuery, WP = Precision<T>::kWeights, KP = ROPE ? Precision<T>::kTurned : 1;
@@ -145,18 +221,19 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, ROPE>)) void decode_f
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, g = lane >> 4;
-    const int nsplit = gridDim.x, split = blockIdx.x, chunks = (G + kColumns - 1) / kColumns;
-    const int kv = blockIdx.y / chunks, first = (blockIdx.y % chunks) * kColumns, sq = blockIdx.z;
+    const int chunks = (G + kColumns - 1) / kColumns, kv = blockIdx.x / chunks, first = (blockIdx.x % chunks) * kColumns;
+    const Slice slice = find_slice(p, plan, sizes, blockIdx.y);
+    if (slice.count == 0) return;
+    const int sq = slice.sq, nsplit = slice.count, split = slice.index;
     const int heads = min(G - first, kColumns), h0 = kv * G + first;
     const long head = (long)sq * p.Hkv + kv;
     const uint8_t *Kc = cache.Kc + head * p.c * (D / 2), *Vc = cache.Vc + head * p.c * (D / 2);
     const uint8_t *Ks = cache.Ks + head * p.c * (D / 32), *Vs = cache.Vs + head * p.c * (D / 32);
-    const Runs runs(cache_map(p, sizes + SEPKV_SIZES_COLS * sq));
+    const Runs runs(slice.map);
     const int nv = runs.nv, nb = (nv + kRows - 1) / kRows;
-    // slices of whole blocks (c d < 2^30, so nb < 2^19)
-    const int share = small_quotient(nb + nsplit - 1, reciprocal(nsplit));
-    const int per = (nsplit == 1 ? nb : __builtin_amdgcn_readfirstlane(share)) * kRows;
-    const int e0 = min(split * per, nv), e1 = min(nv, e0 + per);
+    // as even as can be: the first ones have a block more
+    const int each = nsplit == 1 ? nb : __builtin_amdgcn_readfirstlane(small_quotient(nb, reciprocal(nsplit))), more = nb - each * nsplit;
+    const int e0 = min((split * each + min(split, more)) * kRows, nv), e1 = min(e0 + (each + (split < more)) * kRows, nv);
 
     // first dimension of this lane's fragment ks: whole rows by the four lane groups; with ROPE both members of every pair are one lane's
     auto dim_of = [&](int ks) { return ROPE ? (ks < KS2 ? 0 : D / 2) + (D / 8) * g + 8 * (ks % KS2) : (D / 4) * g + 8 * ks; };
@@ -412,9 +489,9 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, ROPE>)) void decode_f
     // the word in which this pair's slices are counted, and the records behind all words
     const long pair = head * chunks + first / kColumns;
     uint64_t *const arrived = reinterpret_cast<uint64_t *>(ws + pair * kWordPitch);
-    float *const recs = reinterpret_cast<float *>(ws + words_bytes((long)p.S * p.Hkv * chunks)) + ((long)sq * p.Hq + h0) * nsplit * PF;
+    float *const recs = reinterpret_cast<float *>(ws + words_bytes((long)p.S * p.Hkv * chunks)) + ((long)slice.before * p.Hq + h0 * nsplit) * PF;
     uint64_t seen = 0;
-    if constexpr (ADD) {
+    if (ADD && nsplit > 1) {
         if (tid == 0) seen = arrival_seen(arrived);
     }
     for (int item = tid; item < heads * (D / 2); item += 64 * NW) {  // two columns per thread
@@ -434,7 +511,7 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, ROPE>)) void decode_f
             lsum = fmaf(wgt, ml[w].y, lsum), o0 = fmaf(wgt, o[w].x, o0), o1 = fmaf(wgt, o[w].y, o1);
         }
         const long sh = (long)sq * p.Hq + h0 + h;
-        if (!ADD && nsplit == 1) {
+        if (nsplit == 1) {
             finish<T>(nv, M, lsum, o0, out + sh * D + 2 * c2, nullptr);
             finish<T>(nv, M, lsum, o1, out + sh * D + 2 * c2 + 1, lse && c2 == 0 ? lse + sh : nullptr);
         } else {
@@ -448,7 +525,7 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, ROPE>)) void decode_f
             }
         }
     }
-    if constexpr (!ADD) return;
+    if (!ADD || nsplit == 1) return;
 
     // ---- the workgroup that finishes last adds the slices' records, in slice order, whichever it is
     __shared__ int last_s;
@@ -498,15 +575,18 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, ROPE>)) void decode_f
 // The slices' records of a (sequence, query head), where there are several.  Thread k of the first wave has slice k's maximum and sum (there are at most
 // 64), all of them its weight through LDS; the records are requested before that is known.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void merge_fp4_kernel(sepkv_params p, int nsplit, const int32_t *__restrict__ sizes, const float *__restrict__ part,
+__global__ __launch_bounds__(256) void merge_fp4_kernel(sepkv_params p, Plan plan, const int32_t *__restrict__ sizes, const float *__restrict__ part,
                                                          T *__restrict__ out, float *__restrict__ lse) {
     constexpr int PF = D + 2, PARTS = kMergeParts<D>, N = kMostSlices / PARTS;  // a thread: two columns, every PARTS-th slice
     __shared__ float weight[kMostSlices], sums[PARTS][D];
     __shared__ float2 state;
     const long sh = blockIdx.x;
-    const CacheMap cm = cache_map(p, sizes + SEPKV_SIZES_COLS * (sh / p.Hq));
+    const int sq = sh / p.Hq, h = sh - (long)sq * p.Hq;
+    const Slice slice = find_slice(p, plan, sizes, -1 - sq);
+    const int nsplit = slice.count;
+    if (nsplit == 1) return;
     const int c2 = threadIdx.x % (D / 2), which = threadIdx.x / (D / 2);
-    const float *r = part + sh * nsplit * PF;
+    const float *r = part + ((long)slice.before * p.Hq + h * nsplit) * PF;
     float2 o[N];
 #pragma unroll
     for (int n = 0; n < N; ++n) {
@@ -540,35 +620,31 @@ __global__ __launch_bounds__(256) void merge_fp4_kernel(sepkv_params p, int nspl
     float total = 0.f;
 #pragma unroll
     for (int i = 0; i < PARTS; ++i) total += sums[i][c];
-    finish<T>(cm.n_init + cm.n_sep + cm.n_past + cm.n_loc, state.x, state.y, total, out + sh * D + c, lse && c == 0 ? lse + sh : nullptr);
+    finish<T>(1, state.x, state.y, total, out + sh * D + c, lse && c == 0 ? lse + sh : nullptr);  // (without entries there is one slice)
 }
 
 int chunks_of(const sepkv_params &p) { return (p.Hq / p.Hkv + kColumns - 1) / kColumns; }
 
 struct Shape {
-    int nsplit;
-    bool add;  // the kernel adds the slices itself
+    Plan plan;
+    int slices;  // there are no more, for one (KV head, 16 query heads)
+    bool add;    // the kernel adds them itself
 };
-// Enough slices for two workgroups per compute unit, for four where these still have 32 blocks, eight a wave.  Measured in us with 2 / 4 per unit (bf16,
-// d = 128, 32 query heads on 8 KV heads):  4 sequences of 65536 entries (16 or 32 slices, 128 or 64 blocks) 32.1 / 29.8, with positions
-// 59.5 / 50.9;  32 of 3332 (2 or 4, 53 or 27 blocks) 20.5 / 21.9;  8 of 8192 (8 or 16, 32 or 16) 15.8 / 18.0;  64 of 300 (1 or 2, 10 or 5) 8.0 / 11.6.
 Shape shape_of(const sepkv_params &p, int units) {
-    const long pairs = (long)p.S * p.Hkv * chunks_of(p);
-    const int nb = (p.c + kRows - 1) / kRows, row = p.Hq / p.Hkv * p.d;
-    long n = 4L * units / pairs;
-    if (n * kManyBlocks > nb) n = 2L * units / pairs;
-    const long most = (nb + kLeastBlocks - 1) / kLeastBlocks;
-    if (n > most) n = most;
-    Shape x = {(int)(n < 1 ? 1 : n > kMostSlices ? kMostSlices : n), false};
-    x.add = x.nsplit > 1 && x.nsplit <= kMostAdded && row <= 1024 && x.nsplit * row <= 8192;
-    return x;
+    const int rows = p.Hkv * chunks_of(p), nb = (p.c + kRows - 1) / kRows, row = std::min(p.Hq / p.Hkv, kColumns) * p.d;
+    // three workgroups per compute unit (what the widest form's registers leave room for); cut lengths add about half a slice per sequence, or S at most
+    const int one = std::max(units / rows, 1), all = 3 * units / rows - std::min(p.S, 4 + p.S / 2);
+    if (nb <= kLeastBlocks || all <= 0 || p.S > kMostDivided) return {{1, 0, 0.f, 0.f}, p.S, false};
+    const bool add = row <= 1024 && kMostAdded * row <= 8192 && nb <= kMostAdded * kMostAdded;
+    const int most = std::min((nb + kLeastBlocks - 1) / kLeastBlocks, add ? kMostAdded : kMostSlices);
+    return {{most, kManyBlocks, 1.f / one, 1.f / all}, all + p.S, add};
 }
+size_t records_of(const sepkv_params &p, const Shape &x) { return x.plan.most == 1 ? 0 : (size_t)x.slices * p.Hq; }
 
 }  // namespace
 
 size_t decode_fp4_workspace(const sepkv_params &p) {
-    return words_bytes((long)p.S * p.Hkv * chunks_of(p)) +
-           align_up((size_t)p.S * p.Hq * shape_of(p, compute_units()).nsplit * (p.d + 2) * sizeof(float), 256);
+    return words_bytes((long)p.S * p.Hkv * chunks_of(p)) + align_up(records_of(p, shape_of(p, compute_units())) * (p.d + 2) * sizeof(float), 256);
 }
 
 int launch_decode_fp4(const sepkv_params &p, const void *q, const Fp4Cache &cache, const int32_t *sizes, const float *rope, int n_pos, void *out,
@@ -582,15 +658,15 @@ int launch_decode_fp4(const sepkv_params &p, const void *q, const Fp4Cache &cach
         constexpr int D = decltype(D_)::value;
         auto launch = [&](auto ADD_) {
             ProfScope prof(SEPATTN_K_DECODE_SPLIT, st);
-            hipLaunchKernelGGL((decode_fp4_kernel<T, D, decltype(ROPE_)::value, decltype(ADD_)::value>), dim3(shape.nsplit, p.Hkv * chunks, p.S),
-                               dim3(64 * kWaves), 0, st, p, G, n_pos, static_cast<const T *>(q), cache, sizes, rope, one, static_cast<char *>(ws),
+            hipLaunchKernelGGL((decode_fp4_kernel<T, D, decltype(ROPE_)::value, decltype(ADD_)::value>), dim3(p.Hkv * chunks, shape.slices),
+                               dim3(64 * kWaves), 0, st, p, shape.plan, G, n_pos, static_cast<const T *>(q), cache, sizes, rope, one, static_cast<char *>(ws),
                                static_cast<T *>(out), lse);
         };
         add ? launch(std::true_type{}) : launch(std::false_type{});
-        if (shape.nsplit == 1 || add) return launch_status();
+        if (shape.plan.most == 1 || add) return launch_status();
         if (hipGetLastError() != hipSuccess) return (int)SEPATTN_ERR_HIP;
         ProfScope prof(SEPATTN_K_DECODE_MERGE, st);
-        hipLaunchKernelGGL((merge_fp4_kernel<T, D>), dim3(p.S * p.Hq), dim3(256), 0, st, p, shape.nsplit, sizes,
+        hipLaunchKernelGGL((merge_fp4_kernel<T, D>), dim3(p.S * p.Hq), dim3(256), 0, st, p, shape.plan, sizes,
                            reinterpret_cast<const float *>(static_cast<char *>(ws) + words_bytes((long)p.S * p.Hkv * chunks)), static_cast<T *>(out), lse);
         return launch_status();
     };

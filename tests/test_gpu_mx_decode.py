@@ -324,3 +324,45 @@ def test_generation(sp, dtype, positions):
         x.sizes = sizes.tolist()
         assert [sum(r[:4]) for r in x.sizes] == [n + 1 for n in before]
         x.check(*x.run(sp, not text), not text)
+
+
+@pytest.mark.parametrize("rope", [False, True])
+@pytest.mark.parametrize("S,d,entries", [(2, 128, 600), (33, 128, 600), (70, 64, 600), (130, 64, 300), (512, 64, 200), (513, 64, 200)])
+def test_uneven_lengths(sp, rope, S, d, entries):
+    """Sequences of every length in one call, which are cut into slices by their lengths; a captured call (whose slices another launch adds) gives the same
+    bits, also for lengths that the device learns after the capture."""
+    rng = np.random.default_rng(S)
+    lengths = [entries, 0, 1] + [int(n) for n in rng.integers(0, entries + 1, S)]
+    x = Case(S, 3, 1, d, "bf16", (2, 40, 30, entries), lengths, seed=S)
+    want = x.run(sp, rope)
+    x.check(*want, rope)
+    table = sp.sepkv_rope_table(x.c, d, BASE, "cuda")
+    ws = torch.zeros(sp.sepattn_decode_mx_workspace_bytes(x.q, x.cache[0], x.a, x.s, x.w), dtype=torch.uint8, device="cuda")
+    out = (torch.empty_like(x.q), torch.empty(S, 3, device="cuda"))
+
+    def call():
+        if rope:
+            sp.sepattn_decode_rope_mx(x.q, *x.cache, x.sz, table, x.a, x.s, x.w, x.scale, out=out, ws=ws)
+        else:
+            sp.sepattn_decode_mx(x.q, *x.cache, x.sz, x.a, x.s, x.w, x.scale, out=out, ws=ws)
+
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    full = x.sz.clone()
+    for keep in (1.0, 0.4, 0.0, 0.7, 1.0):
+        x.sz.copy_(full)
+        x.sz[1::2, 2] = (full[1::2, 2] * keep).int()  # (of every second sequence; a shorter window holds no slot that was empty)
+        eager = [t.clone() for t in x.run(sp, rope, ws=ws)]
+        out[0].fill_(5.0), out[1].fill_(5.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, eager))
+        if keep == 1.0:
+            assert all(torch.equal(a, b) for a, b in zip(eager, want))
+        else:
+            y = x.__class__.__new__(x.__class__)
+            y.__dict__.update(x.__dict__, sizes=x.sz.tolist())
+            y.check(*eager, rope)

@@ -62,6 +62,12 @@ __device__ inline float groups_sum(float x) {
     return pair_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
 }
 
+// of another lane of the same sixteen: row_ror 8 (0x128) and 4 (0x124), quad_perm [2, 3, 0, 1] (0x4E) and [1, 0, 3, 2] (0xB1)
+template <int CTRL>
+__device__ inline float dpp_of(float x) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, 0xF, 0xF, true));
+}
+
 // x as a sum of PARTS bf16 numbers: all but the last cut off, so that what they leave is exact
 template <int PARTS>
 __device__ inline void split_bf16(const f32x8 &x, bf16x8 (&part)[PARTS]) {
@@ -221,6 +227,16 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, ROPE>)) void decode_f
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, g = lane >> 4;
+    // the table's rows 0 .. 31, which pass through LDS below: on their way while the slice is found
+    constexpr int CH = D / 4, TABLE = ROPE ? kRows * CH / (64 * NW) : 1;
+    f32x4 table[TABLE];
+    if constexpr (ROPE) {
+#pragma unroll
+        for (int n = 0; n < TABLE; ++n) {
+            const int i = tid + n * 64 * NW, r = i / CH;
+            table[n] = *reinterpret_cast<const f32x4 *>(rope + (long)min(r, n_pos - 1) * D + (i % CH) * 4);
+        }
+    }
     const int chunks = (G + kColumns - 1) / kColumns, kv = blockIdx.x / chunks, first = (blockIdx.x % chunks) * kColumns;
     const Slice slice = find_slice(p, plan, sizes, blockIdx.y);
     if (slice.count == 0) return;
@@ -316,20 +332,13 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, ROPE>)) void decode_f
         }
     };
     if constexpr (ROPE) {
-        constexpr int CH = D / 4, N = kRows * CH / (64 * NW);
         static_assert(kRows * D * 4 <= NW * STAGE, "the table's rows fit the stages");
-        f32x4 t[N];
-#pragma unroll
-        for (int n = 0; n < N; ++n) {
-            const int i = tid + n * 64 * NW, r = i / CH;
-            t[n] = *reinterpret_cast<const f32x4 *>(rope + (long)min(r, n_pos - 1) * D + (i % CH) * 4);
-        }
         request_first();
         const uint32_t t_lds = lds_addr(&smem[0][0]);
 #pragma unroll
-        for (int n = 0; n < N; ++n) {
+        for (int n = 0; n < TABLE; ++n) {
             const int i = tid + n * 64 * NW, r = i / CH;
-            lds_write_b128_at(t_lds + r * D * 4 + (((uint32_t)(i % CH) ^ chunk_swizzle<128>(r)) << 4), t[n]);
+            lds_write_b128_at(t_lds + r * D * 4 + (((uint32_t)(i % CH) ^ chunk_swizzle<128>(r)) << 4), table[n]);
         }
         auto barrier = [] {  // of LDS alone: a __syncthreads would also wait for the rows
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -596,13 +605,11 @@ __global__ __launch_bounds__(256) void merge_fp4_kernel(sepkv_params p, Plan pla
     if (threadIdx.x < 64) {
         const int k = threadIdx.x;
         const float2 ml = k < nsplit ? *reinterpret_cast<const float2 *>(r + k * PF) : float2{-INFINITY, 0.f};
-        float M = ml.x;
-#pragma unroll
-        for (int x = 32; x > 0; x /= 2) M = fmaxf(M, __shfl_xor(M, x));
+        float M = groups_max(ml.x);  // over lanes 16, 32, 8, 4, 2 and 1 apart
+        M = fmaxf(M, dpp_of<0x128>(M)), M = fmaxf(M, dpp_of<0x124>(M)), M = fmaxf(M, dpp_of<0x4E>(M)), M = fmaxf(M, dpp_of<0xB1>(M));
         const float w = ml.x == -INFINITY ? 0.f : exp2f(ml.x - M);
-        float sum = w * ml.y;
-#pragma unroll
-        for (int x = 32; x > 0; x /= 2) sum += __shfl_xor(sum, x);
+        float sum = groups_sum(w * ml.y);
+        sum += dpp_of<0x128>(sum), sum += dpp_of<0x124>(sum), sum += dpp_of<0x4E>(sum), sum += dpp_of<0xB1>(sum);
         weight[k] = w;
         if (k == 0) state = float2{M, sum};
     }

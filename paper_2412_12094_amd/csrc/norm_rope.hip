@@ -194,30 +194,32 @@ __global__ __launch_bounds__(kNormThreads, LAYOUT == kHalvesOdd ? 2 : 3) void no
         part[(long)blockIdx.x * D + threadIdx.x] = (sums[0][threadIdx.x] + sums[1][threadIdx.x]) + (sums[2][threadIdx.x] + sums[3][threadIdx.x]);
 }
 
-// dw of q (blockIdx.y 0) and of k (1): rows of partial sums, eight columns per workgroup
+// dw of q (blockIdx.y 0) and of k (1): rows of partial sums, four columns per workgroup, a row per thread
 __global__ __launch_bounds__(kNormThreads) void norm_weights_kernel(int D, int rows_q, int rows_k, const float *__restrict__ part,
                                                                      float *__restrict__ dq_weight, float *__restrict__ dk_weight) {
     float *out = blockIdx.y ? dk_weight : dq_weight;
     if (!out) return;
-    const int col = blockIdx.x * 8 + threadIdx.x % 8, first = threadIdx.x / 8, rows = blockIdx.y ? rows_k : rows_q;
-    const float *p = part + (blockIdx.y ? (long)rows_q * D : 0) + col;
-    constexpr int STEP = kNormThreads / 8, N = 32;
-    double sum = 0.0;
-    for (int r = first; r < rows; r += N * STEP) {
-        float v[N];
+    const int rows = blockIdx.y ? rows_k : rows_q, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const float *p = part + (blockIdx.y ? (long)rows_q * D : 0) + 4 * blockIdx.x;
+    constexpr int N = 4;  // rows of a thread on their way
+    double sum[4] = {0.0, 0.0, 0.0, 0.0};
+    for (int r = threadIdx.x; r < rows; r += N * kNormThreads) {
+        float4 v[N];
 #pragma unroll
-        for (int n = 0; n < N; ++n) v[n] = r + n * STEP < rows ? p[(long)(r + n * STEP) * D] : 0.f;
+        for (int n = 0; n < N; ++n)
+            v[n] = r + n * kNormThreads < rows ? *reinterpret_cast<const float4 *>(p + (long)(r + n * kNormThreads) * D) : float4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int n = 0; n < N; ++n) sum += v[n];
+        for (int n = 0; n < N; ++n) sum[0] += v[n].x, sum[1] += v[n].y, sum[2] += v[n].z, sum[3] += v[n].w;
     }
-    __shared__ double sums[kNormThreads];
-    sums[threadIdx.x] = sum;
+    static_assert(kNormThreads == 256, "a wave per column");
+    __shared__ double sums[4][kNormThreads];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sums[i][threadIdx.x] = sum[i];
     __syncthreads();
-    for (int n = kNormThreads / 2; n >= 8; n /= 2) {
-        if (threadIdx.x < n) sums[threadIdx.x] += sums[threadIdx.x + n];
-        __syncthreads();
-    }
-    if (threadIdx.x < 8) out[col] = (float)sums[threadIdx.x];
+    double x = (sums[wave][lane] + sums[wave][lane + 64]) + (sums[wave][lane + 128] + sums[wave][lane + 192]);
+#pragma unroll
+    for (int n = 32; n > 0; n /= 2) x += __shfl_xor(x, n);
+    if (lane == 0) out[4 * blockIdx.x + wave] = (float)x;
 }
 
 int log_tokens_of(int L, int rows) {
@@ -314,7 +316,7 @@ int launch_norm_rope_backward(const sepattn_norm_rope_params &p, const double *f
     });
     if (!sums) return launch_status();
     if (hipGetLastError() != hipSuccess) return SEPATTN_ERR_HIP;
-    hipLaunchKernelGGL(norm_weights_kernel, dim3(p.d / 8, 2), dim3(kNormThreads), 0, st, p.d, g.first[1], g.first[2] - g.first[1], part,
+    hipLaunchKernelGGL(norm_weights_kernel, dim3(p.d / 4, 2), dim3(kNormThreads), 0, st, p.d, g.first[1], g.first[2] - g.first[1], part,
                        dq_weight, dk_weight);
     return launch_status();
 }

@@ -531,7 +531,8 @@ int sepkv_fill_from_prefill_zeroed(const sepkv_params *p, int L, int nw, const v
  * sepattn_decode_mx, sepattn_decode_rope_mx: as sepattn_decode, _rope, over the cache's values.  lse holds to 1e-5 in bf16 too, also with positions
  *   (sepattn_decode rounds its weights to bf16 once, here they have 16 bits).  Any number of query heads per KV head.  The workspace may hold anything
  *   and is left in no particular state; calls that overlap in time need one each.
- *   NaN in a query or in the cache reaches the results that see it, and no others.
+ *   NaN in a query or in the cache reaches the results that see it, and no others.  Scores and the weighted sums of values are fp32 until the end:
+ *   keys and values of magnitudes above 2^95 may overflow them in a full cache.
  * ------------------------------------------------------------------------------------------ */
 int sepkv_fill_from_prefill_mx(const sepkv_params *p, int L, int nw, const void *K, const void *V, const uint8_t *is_sep,
                                 const int32_t *sep_idx, int cap, const int32_t *sep_prefix, void *Kc, void *Ks, void *Vc,

@@ -12,6 +12,14 @@
 // and the query's operand follows it.  Rows of a block are requested while the one before it is worked on.  V has to be transposed for the second
 // contraction: its converted rows pass through 8 KB of LDS per wave, read back with ds_read_b64_tr_b16.
 //
+// What bounds it, d = 128, bf16, 32 query heads on 8 KV heads.  Long caches: memory.  4 sequences of up to 53019 entries, 137 MB in 26.8 us, 5.1 TB/s, and
+// 4.6 for the merge launch.  Shorter ones: vector instructions and the start.  A block is 190 of them (64 convert, 24 split the weights), with positions
+// 640: 128 form the angles, 128 turn, 192 split the turned keys.  A wave alone on its SIMD needs 1.8 us for a block with positions, three together 1.2
+// each, so kResident is as much as fits without a spill: a spilled register is waited for with every load before it.  32 sequences of 1 to 3277
+// entries, 60 MB, 18.8 us; with positions 30.  The other half of both is the start (launch, slice, first rows: 6 us) and the sum of the slices (4).
+// The remainder of a cut number as one dot product of bf16 pairs instead of a mask and a subtraction took 72 instructions out of the 640 and changed no
+// time, nor did a second block on its way (d = 64: 17.4 -> 18.9).
+//
 // Operand layouts of 16x16x32 and the order of a block's rows as in decode_wide.hip: row 4g+i of score tile t is row 8g+4t+i of the block, so
 // that a lane group's scores are the k-slots that it holds of the weights as B operand.
 #include <algorithm>
@@ -32,15 +40,12 @@ constexpr int kColumns = 16;   // query heads of a workgroup
 template <typename T, int D, bool ROPE>
 constexpr int kResident = sizeof(T) == 2 ? (ROPE && D == 128 ? 3 : 4) : (D == 128 ? (ROPE ? 2 : 3) : (ROPE ? 3 : 4));
 constexpr int kWaves = 4;
-template <int D, bool ROPE>
-constexpr int kDepth = D == 64 && !ROPE ? 2 : 1;  // blocks of a wave on their way
 constexpr int kLeastBlocks = kWaves;  // of a slice
 constexpr int kManyBlocks = 20;       // of a slice where there is more than one workgroup per compute unit
 constexpr int kMostSlices = 64;       // of a sequence
 constexpr int kMostAdded = 16;        // of a sequence whose slices the kernel itself adds
 constexpr int kMostDivided = 512;     // sequences of a call in which they are cut
-constexpr int kWordPitch = 128;  // bytes: a cache line for each word in which slices are counted
-__host__ __device__ inline size_t words_bytes(long pairs) { return align_up((size_t)pairs * kWordPitch, 256); }
+__host__ __device__ inline size_t words_bytes(long pairs) { return align_up((size_t)pairs * sizeof(uint64_t), 256); }
 
 __device__ inline f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
@@ -318,18 +323,14 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, ROPE>)) void decode_f
     // cos / sin of the place of the lane's row krow within a block (that of row krow + 4 is the same behind entry 4): the table's rows 0 .. 31 pass through
     // LDS, where the V stages lie later, with the 16-byte chunks of a row permuted (row by row from memory, an instruction is 64 pieces of 16 bytes)
     float rc[KS2][8], rs[KS2][8];
-    constexpr int STEP = NW * kRows, DEPTH = kDepth<D, ROPE>;
-    Rows ring[DEPTH];
+    constexpr int STEP = NW * kRows;
+    Rows rows;
     auto request_first = [&] {
         if (eb >= e1) return;
-#pragma unroll
-        for (int i = 0; i < DEPTH; ++i) {
-            const int at = eb + i * STEP;
-            uint32_t slot[2];
-            find_slots(at, slot);
-            request_keys(ring[i], at, slot);
-            request_values(ring[i], slot);
-        }
+        uint32_t slot[2];
+        find_slots(eb, slot);
+        request_keys(rows, eb, slot);
+        request_values(rows, slot);
     };
     if constexpr (ROPE) {
         static_assert(kRows * D * 4 <= NW * STAGE, "the table's rows fit the stages");
@@ -374,10 +375,10 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, ROPE>)) void decode_f
     for (int db = 0; db < DB; ++db) acc[db] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m_run = -INFINITY, l_run = 0.f;
 
-    auto work = [&](Rows &rows) __attribute__((always_inline)) {
+    for (; eb < e1; eb += STEP) {
         // (requested in any case, beyond the end as the last entry again: behind a branch the compiler could not count the loads, and would wait for all)
         uint32_t next[2];
-        find_slots(eb + DEPTH * STEP, next);
+        find_slots(eb + STEP, next);
         // ---- scores
         f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
         if constexpr (ROPE) {
@@ -430,7 +431,7 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, ROPE>)) void decode_f
                 }
         }
         __builtin_amdgcn_sched_barrier(0);
-        request_keys(rows, eb + DEPTH * STEP, next);
+        request_keys(rows, eb + STEP, next);
         // ---- V rows into LDS
         asm volatile("" : "+v"(vwrite), "+v"(vread));
 #pragma unroll
@@ -475,14 +476,6 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, ROPE>)) void decode_f
 #pragma unroll
             for (int i = 0; i < WP; ++i) acc[db] = mfma16(v, w[i], acc[db]);
         }
-        eb += STEP;
-    };
-    while (eb < e1) {
-        work(ring[0]);
-        if constexpr (DEPTH == 2) {
-            if (eb >= e1) break;
-            work(ring[1]);
-        }
     }
 
     // ---- the waves' states: D outputs, max, sum of a head
@@ -497,7 +490,7 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, ROPE>)) void decode_f
     __syncthreads();
     // the word in which this pair's slices are counted, and the records behind all words
     const long pair = head * chunks + first / kColumns;
-    uint64_t *const arrived = reinterpret_cast<uint64_t *>(ws + pair * kWordPitch);
+    uint64_t *const arrived = reinterpret_cast<uint64_t *>(ws) + pair;
     float *const recs = reinterpret_cast<float *>(ws + words_bytes((long)p.S * p.Hkv * chunks)) + ((long)slice.before * p.Hq + h0 * nsplit) * PF;
     uint64_t seen = 0;
     if (ADD && nsplit > 1) {

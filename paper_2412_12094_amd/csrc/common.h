@@ -97,7 +97,7 @@ __device__ inline int quotient(int x, FastDiv f) { return (int)(((uint64_t)(uint
 // least 1/(2d) of a whole number off, and the product's relative error is below 2^-22, so this holds for 0 <= x < 2^21.
 constexpr int kSmallQuotient = 1 << 21;
 __device__ inline float reciprocal(int d) { return __builtin_amdgcn_rcpf((float)d); }
-__device__ inline int small_quotient(int x, float rcp) { return (int)(((float)x + 0.5f) * rcp); }
+__host__ __device__ inline int small_quotient(int x, float rcp) { return (int)(((float)x + 0.5f) * rcp); }
 
 // Head-wise neighbour windows (the head-wise variant of Sec. 4.6): every attention kernel is given
 // p.n = the LARGEST window of the call and, by value, how much shorter each query head's own window

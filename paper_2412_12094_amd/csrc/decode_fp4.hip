@@ -22,10 +22,9 @@
 //
 // Operand layouts of 16x16x32 and the order of a block's rows as in decode_wide.hip: row 4g+i of score tile t is row 8g+4t+i of the block, so
 // that a lane group's scores are the k-slots that it holds of the weights as B operand.
-#include <algorithm>
-
 #include "common.h"
 #include "decode_common.h"
+#include "decode_fp4.h"
 #include "fp4.h"
 #include "mfma_common.h"
 #include "rotary.h"
@@ -34,17 +33,10 @@ namespace sepattn {
 
 namespace {
 
-constexpr int kRows = 32;      // entries per block
-constexpr int kColumns = 16;   // query heads of a workgroup
 // waves per SIMD that the registers have to leave room for
 template <typename T, int D, bool ROPE>
 constexpr int kResident = sizeof(T) == 2 ? (ROPE && D == 128 ? 3 : 4) : (D == 128 ? (ROPE ? 2 : 3) : (ROPE ? 3 : 4));
-constexpr int kWaves = 4;
-constexpr int kLeastBlocks = kWaves;  // of a slice
-constexpr int kManyBlocks = 20;       // of a slice where there is more than one workgroup per compute unit
-constexpr int kMostSlices = 64;       // of a sequence
-constexpr int kMostAdded = 16;        // of a sequence whose slices the kernel itself adds
-constexpr int kMostDivided = 512;     // sequences of a call in which they are cut
+constexpr int kWaves = kMxWaves, kRows = kMxRows, kColumns = kMxColumns, kMostSlices = kMxMostSlices;
 __host__ __device__ inline size_t words_bytes(long pairs) { return align_up((size_t)pairs * sizeof(uint64_t), 256); }
 
 __device__ inline f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
@@ -141,18 +133,7 @@ struct Runs {
     }
 };
 
-// How sequences are cut into slices.  Their lengths stand on the device, and those of a batch differ, so every workgroup finds its slice by itself, a
-// sequence per lane.  With T blocks in all sequences a slice has at most  share = max(kLeastBlocks, min(T / one, max(many, T / all)))  blocks, where `one`
-// and `all` are the workgroups that one (KV head, 16 query heads) has if there is one per compute unit and if there are as many as it holds: more than one
-// only where slices stay long enough to pay for being added.  A sequence of nb blocks has ceil(nb / share) slices, at least 1, at most `most`; they are
-// numbered through all sequences and at most  all + S.  (most 1: the slices are the sequences.)
-// Against as many slices for every sequence of the batch, chosen by the capacity (bf16, d = 128, 32 query heads on 8 KV heads): 32 sequences of 1 to 3277
-// entries 20.5 -> 18.8 us, with positions 36.5 -> 30.1; 8 of up to 8192 15.8 -> 14.5; 4 of up to 53019 29.7 -> 30.8, where memory was the bound and the
-// search is on the way.  With positions and equal lengths of 1706 entries, one, two and three workgroups per unit take 29.8, 27.7 and 26.8 us.
-struct Plan {
-    int most, many;
-    float per_one, per_all;  // 1 / one, 1 / all
-};
+// A slice, which every workgroup finds by itself from the sizes, a sequence per lane (MxPlan, decode_fp4.h).
 struct Slice {
     int sq, index, count, before;  // sequence, which of its slices, how many it has (0: there is no such slice), slices of the sequences in front of it
     CacheMap map;
@@ -169,19 +150,15 @@ __device__ inline int lanes_sum(int x) {
 }
 __device__ inline int blocks_of(const CacheMap &m) { return (m.n_init + m.n_sep + m.n_past + m.n_loc + kRows - 1) / kRows; }
 // slice number `want`; `want` < 0: the first one of sequence -1 - want
-__device__ inline Slice slice_of(const sepkv_params &p, const Plan &plan, const int32_t *__restrict__ sizes, int want) {
+__device__ inline Slice slice_of(const sepkv_params &p, const MxPlan &plan, const int32_t *__restrict__ sizes, int want) {
     if (plan.most == 1) {
         if (want >= p.S) return {0, 0, 0, 0, {}};
         const int sq = want < 0 ? -1 - want : want;
         return {sq, 0, 1, sq, cache_map(p, sizes + SEPKV_SIZES_COLS * sq)};
     }
-    auto count_of = [&](int nb, float per_share) { return min(1 + small_quotient(max(nb - 1, 0), per_share), plan.most); };  // (c d < 2^30, so nb < 2^19)
-    auto share_of = [&](int total) {  // (512 sequences: below 2^28; rounded in fp32, alike in every workgroup)
-        return max(kLeastBlocks, min((int)((float)total * plan.per_one), max(plan.many, (int)((float)total * plan.per_all))) + 1);
-    };
     if (p.S == 1) {
         const CacheMap m = cache_map(p, sizes);
-        const int nb = blocks_of(m), n = __builtin_amdgcn_readfirstlane(count_of(nb, reciprocal(share_of(nb))));
+        const int nb = blocks_of(m), n = __builtin_amdgcn_readfirstlane(mx_slices(plan, nb, reciprocal(mx_share(plan, nb))));
         return {0, max(want, 0), want < n ? n : 0, 0, m};
     }
     const int lane = threadIdx.x & 63;
@@ -191,9 +168,9 @@ __device__ inline Slice slice_of(const sepkv_params &p, const Plan &plan, const 
         m = cache_map(p, sizes + SEPKV_SIZES_COLS * min(s0 + lane, p.S - 1));
         total += s0 + lane < p.S ? blocks_of(m) : 0;
     }
-    const float per_share = reciprocal(share_of(__builtin_amdgcn_readlane(lanes_sum(total), 63)));
+    const float per_share = reciprocal(mx_share(plan, __builtin_amdgcn_readlane(lanes_sum(total), 63)));
     for (int s0 = 0;; s0 += 64) {
-        const int n = s0 + lane < p.S ? count_of(blocks_of(m), per_share) : 0, upto = lanes_sum(n), front = before + upto - n;
+        const int n = s0 + lane < p.S ? mx_slices(plan, blocks_of(m), per_share) : 0, upto = lanes_sum(n), front = before + upto - n;
         const uint64_t found = __builtin_amdgcn_ballot_w64(want < 0 ? s0 + lane == -1 - want : want >= front && want < front + n);
         if (found) {
             const int l = __builtin_ctzll(found);
@@ -207,7 +184,7 @@ __device__ inline Slice slice_of(const sepkv_params &p, const Plan &plan, const 
     }
 }
 
-__device__ inline Slice find_slice(const sepkv_params &p, const Plan &plan, const int32_t *__restrict__ sizes, int want) {
+__device__ inline Slice find_slice(const sepkv_params &p, const MxPlan &plan, const int32_t *__restrict__ sizes, int want) {
     const Slice x = slice_of(p, plan, sizes, want);
     auto s = [](int v) { return __builtin_amdgcn_readfirstlane(v); };  // (the same in all lanes, which the compiler does not see)
     return {s(x.sq), s(x.index), s(x.count), s(x.before),
@@ -220,7 +197,7 @@ constexpr int kMergeParts = 256 / (D / 2);  // threads of the merge launch that 
 // ADD: the slices of a sequence are added by the workgroup that finishes last.  Otherwise, where there are several, they are left to a merge launch.
 template <typename T, int D, bool ROPE, bool ADD>
 __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, ROPE>)) void decode_fp4_kernel(
-    sepkv_params p, Plan plan, int G, int n_pos, const T *__restrict__ q, Fp4Cache cache, const int32_t *__restrict__ sizes, const float *__restrict__ rope,
+    sepkv_params p, MxPlan plan, int G, int n_pos, const T *__restrict__ q, Fp4Cache cache, const int32_t *__restrict__ sizes, const float *__restrict__ rope,
     uint64_t one, char *__restrict__ ws, T *__restrict__ out, float *__restrict__ lse) {
     constexpr int KSTEPS = D / 32, KS2 = KSTEPS / 2, DB = D / 16, NW = kWaves;
     constexpr int QP = Precision<T>::kQuery, WP = Precision<T>::kWeights, KP = ROPE ? Precision<T>::kTurned : 1;
@@ -541,22 +518,22 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, ROPE>)) void decode_f
     for (int item = tid; item < heads * (D / 2); item += 64 * NW) {
         const int h = item / (D / 2), c2 = item % (D / 2);
         const float *rec = recs + h * nsplit * PF;
-        float2 ml[kMostAdded], o[kMostAdded];
+        float2 ml[kMxMostAdded], o[kMxMostAdded];
 #pragma unroll
-        for (int k = 0; k < kMostAdded; ++k)
+        for (int k = 0; k < kMxMostAdded; ++k)
             if (k < nsplit) ml[k] = fetch_published(rec + k * PF), o[k] = fetch_published(rec + k * PF + 2 + 2 * c2);
         // every sum in the order in which merge_fp4_kernel forms it: captured calls, which that kernel finishes, give the same bits
-        float M = -INFINITY, wgt[kMostAdded], sum[kMostAdded], o0 = 0.f, o1 = 0.f;
+        float M = -INFINITY, wgt[kMxMostAdded], sum[kMxMostAdded], o0 = 0.f, o1 = 0.f;
 #pragma unroll
-        for (int k = 0; k < kMostAdded; ++k)
+        for (int k = 0; k < kMxMostAdded; ++k)
             if (k < nsplit) M = fmaxf(M, ml[k].x);
 #pragma unroll
-        for (int k = 0; k < kMostAdded; ++k) {
+        for (int k = 0; k < kMxMostAdded; ++k) {
             wgt[k] = k >= nsplit || ml[k].x == -INFINITY ? 0.f : exp2f(ml[k].x - M);
             sum[k] = k < nsplit ? wgt[k] * ml[k].y : 0.f;
         }
 #pragma unroll
-        for (int x = kMostAdded / 2; x > 0; x /= 2)
+        for (int x = kMxMostAdded / 2; x > 0; x /= 2)
 #pragma unroll
             for (int k = 0; k < x; ++k) sum[k] += sum[k + x];
         const float lsum = sum[0];
@@ -564,7 +541,7 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, ROPE>)) void decode_f
         for (int i = 0; i < kMergeParts<D>; ++i) {
             float a0 = 0.f, a1 = 0.f;
 #pragma unroll
-            for (int k = i; k < kMostAdded; k += kMergeParts<D>)
+            for (int k = i; k < kMxMostAdded; k += kMergeParts<D>)
                 if (k < nsplit) a0 = fmaf(wgt[k], o[k].x, a0), a1 = fmaf(wgt[k], o[k].y, a1);
             o0 += a0, o1 += a1;
         }
@@ -577,7 +554,7 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, ROPE>)) void decode_f
 // The slices' records of a (sequence, query head), where there are several.  Thread k of the first wave has slice k's maximum and sum (there are at most
 // 64), all of them its weight through LDS; the records are requested before that is known.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void merge_fp4_kernel(sepkv_params p, Plan plan, const int32_t *__restrict__ sizes, const float *__restrict__ part,
+__global__ __launch_bounds__(256) void merge_fp4_kernel(sepkv_params p, MxPlan plan, const int32_t *__restrict__ sizes, const float *__restrict__ part,
                                                          T *__restrict__ out, float *__restrict__ lse) {
     constexpr int PF = D + 2, PARTS = kMergeParts<D>, N = kMostSlices / PARTS;  // a thread: two columns, every PARTS-th slice
     __shared__ float weight[kMostSlices], sums[PARTS][D];
@@ -623,34 +600,16 @@ __global__ __launch_bounds__(256) void merge_fp4_kernel(sepkv_params p, Plan pla
     finish<T>(1, state.x, state.y, total, out + sh * D + c, lse && c == 0 ? lse + sh : nullptr);  // (without entries there is one slice)
 }
 
-int chunks_of(const sepkv_params &p) { return (p.Hq / p.Hkv + kColumns - 1) / kColumns; }
-
-struct Shape {
-    Plan plan;
-    int slices;  // there are no more, for one (KV head, 16 query heads)
-    bool add;    // the kernel adds them itself
-};
-Shape shape_of(const sepkv_params &p, int units) {
-    const int rows = p.Hkv * chunks_of(p), nb = (p.c + kRows - 1) / kRows, row = std::min(p.Hq / p.Hkv, kColumns) * p.d;
-    // three workgroups per compute unit (what the widest form's registers leave room for); cut lengths add about half a slice per sequence, or S at most
-    const int one = std::max(units / rows, 1), all = 3 * units / rows - std::min(p.S, 4 + p.S / 2);
-    if (nb <= kLeastBlocks || all <= 0 || p.S > kMostDivided) return {{1, 0, 0.f, 0.f}, p.S, false};
-    const bool add = row <= 1024 && kMostAdded * row <= 8192 && nb <= kMostAdded * kMostAdded;
-    const int most = std::min((nb + kLeastBlocks - 1) / kLeastBlocks, add ? kMostAdded : kMostSlices);
-    return {{most, kManyBlocks, 1.f / one, 1.f / all}, all + p.S, add};
-}
-size_t records_of(const sepkv_params &p, const Shape &x) { return x.plan.most == 1 ? 0 : (size_t)x.slices * p.Hq; }
-
 }  // namespace
 
 size_t decode_fp4_workspace(const sepkv_params &p) {
-    return words_bytes((long)p.S * p.Hkv * chunks_of(p)) + align_up(records_of(p, shape_of(p, compute_units())) * (p.d + 2) * sizeof(float), 256);
+    return words_bytes((long)p.S * p.Hkv * mx_chunks(p)) + align_up(mx_records(p, mx_shape(p, compute_units())) * (p.d + 2) * sizeof(float), 256);
 }
 
 int launch_decode_fp4(const sepkv_params &p, const void *q, const Fp4Cache &cache, const int32_t *sizes, const float *rope, int n_pos, void *out,
                       float *lse, void *ws, hipStream_t st) {
-    const int G = p.Hq / p.Hkv, chunks = chunks_of(p);
-    const Shape shape = shape_of(p, compute_units());
+    const int G = p.Hq / p.Hkv, chunks = mx_chunks(p);
+    const MxShape shape = mx_shape(p, compute_units());
     const bool add = shape.add && !being_captured(st);  // else a merge launch adds the slices
     const uint64_t one = add ? launch_number() : 0;
     auto go = [&](auto T_, auto D_, auto ROPE_) {

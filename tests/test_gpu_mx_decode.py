@@ -366,3 +366,13 @@ def test_uneven_lengths(sp, rope, S, d, entries):
             y = x.__class__.__new__(x.__class__)
             y.__dict__.update(x.__dict__, sizes=x.sz.tolist())
             y.check(*eager, rope)
+
+
+@pytest.mark.parametrize("rope", [False, True])
+def test_few_long_among_many_short(sp, rope):
+    """More sequences than there are workgroups to spare: the slices of the long ones fit what is launched and the workspace."""
+    x = Case(140, 9, 9, 64, "bf16", (2, 40, 30, 800), [800, 1, 30, 0, 20, 9, 31], seed=4)
+    need = sp.sepattn_decode_mx_workspace_bytes(x.q, x.cache[0], x.a, x.s, x.w)
+    ws = torch.full((need + 4096,), 0xA5, dtype=torch.uint8, device="cuda")
+    x.check(*x.run(sp, rope, ws=ws[:need]), rope)
+    assert (ws[need:] == 0xA5).all()

@@ -37,7 +37,10 @@ namespace {
 template <typename T, int D, bool ROPE>
 constexpr int kResident = sizeof(T) == 2 ? (ROPE && D == 128 ? 3 : 4) : (D == 128 ? (ROPE ? 2 : 3) : (ROPE ? 3 : 4));
 constexpr int kWaves = kMxWaves, kRows = kMxRows, kColumns = kMxColumns, kMostSlices = kMxMostSlices;
-__host__ __device__ inline size_t words_bytes(long pairs) { return align_up((size_t)pairs * sizeof(uint64_t), 256); }
+// a cache line for each word in which slices are counted: side by side, 8 sequences of up to 8192 entries took 18.3 us instead of 14.2, with positions 28.3
+// instead of 24.5
+constexpr int kWordPitch = 128;
+__host__ __device__ inline size_t words_bytes(long pairs) { return align_up((size_t)pairs * kWordPitch, 256); }
 
 __device__ inline f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
@@ -467,7 +470,7 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, ROPE>)) void decode_f
     __syncthreads();
     // the word in which this pair's slices are counted, and the records behind all words
     const long pair = head * chunks + first / kColumns;
-    uint64_t *const arrived = reinterpret_cast<uint64_t *>(ws) + pair;
+    uint64_t *const arrived = reinterpret_cast<uint64_t *>(ws + pair * kWordPitch);
     float *const recs = reinterpret_cast<float *>(ws + words_bytes((long)p.S * p.Hkv * chunks)) + ((long)slice.before * p.Hq + h0 * nsplit) * PF;
     uint64_t seen = 0;
     if (ADD && nsplit > 1) {

@@ -16,9 +16,10 @@
 // 4.6 for the merge launch.  Shorter ones: vector instructions and the start.  A block is 190 of them (64 convert, 24 split the weights), with positions
 // 640: 128 form the angles, 128 turn, 192 split the turned keys.  A wave alone on its SIMD needs 1.8 us for a block with positions, three together 1.2
 // each, so kResident is as much as fits without a spill: a spilled register is waited for with every load before it.  32 sequences of 1 to 3277
-// entries, 60 MB, 18.8 us; with positions 30.  The other half of both is the start (launch, slice, first rows: 6 us) and the sum of the slices (4).
+// entries, 60 MB, 17.9 us; with positions 29.6.  The other half of both is the start (launch, slice, first rows: 6 us) and the sum of the slices (4).
 // The remainder of a cut number as one dot product of bf16 pairs instead of a mask and a subtraction took 72 instructions out of the 640 and changed no
-// time, nor did a second block on its way (d = 64: 17.4 -> 18.9).
+// time, nor did a second block on its way (d = 64: 17.4 -> 18.9).  The second halves of turned keys as fp32 products (16x16x4) instead of two parts: 96
+// instructions fewer, 29.8 -> 34.8: eight products that wait for each other.
 //
 // Operand layouts of 16x16x32 and the order of a block's rows as in decode_wide.hip: row 4g+i of score tile t is row 8g+4t+i of the block, so
 // that a lane group's scores are the k-slots that it holds of the weights as B operand.
@@ -449,12 +450,17 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, ROPE>)) void decode_f
         }
         bf16x8 w[WP];
         split_bf16<WP>(pr, w);
-        // ---- output
+        // ---- output, by four independent sums at a time (32 sequences 18.6 -> 17.9 us: one after the other, a product waits for the one before)
+        constexpr int VB = 4;
 #pragma unroll
-        for (int db = 0; db < DB; ++db) {
-            const bf16x8 v = lds_read_tr_at(vread ^ (uint32_t)(db << 5), 4 * D * 2);
+        for (int db = 0; db < DB; db += VB) {
+            bf16x8 v[VB];
 #pragma unroll
-            for (int i = 0; i < WP; ++i) acc[db] = mfma16(v, w[i], acc[db]);
+            for (int x = 0; x < VB; ++x) v[x] = lds_read_tr_at(vread ^ (uint32_t)((db + x) << 5), 4 * D * 2);
+#pragma unroll
+            for (int i = 0; i < WP; ++i)
+#pragma unroll
+                for (int x = 0; x < VB; ++x) acc[db + x] = mfma16(v[x], w[i], acc[db + x]);
         }
     }
 

@@ -376,3 +376,71 @@ def test_few_long_among_many_short(sp, rope):
     ws = torch.full((need + 4096,), 0xA5, dtype=torch.uint8, device="cuda")
     x.check(*x.run(sp, rope, ws=ws[:need]), rope)
     assert (ws[need:] == 0xA5).all()
+
+
+@pytest.mark.parametrize("rope", [False, True])
+def test_sizes_outside_their_ranges(sp, rope):
+    """Clamped on the device before sequences are cut into slices: the bits of the clamped sizes."""
+    a, s, w, c = 4, 100, 30, 500
+    x = Case(5, 8, 2, 64, "bf16", (a, s, w, c), [1], seed=9)
+    for scales in (x.cache[1], x.cache[3]):
+        scales.fill_(126)
+    big, room = 1 << 30, c - a - s
+    x.sz.copy_(torch.tensor([[big] * 6, [-5] * 6, [2, 40, 100, 30, 7, 9], [big, -1, 3, big, -1, big], [a, s, room, 5, s, room]], dtype=torch.int32))
+    got = [t.clone() for t in x.run(sp, rope)]
+    x.sz.copy_(torch.tensor([[a, s, room, 0, s - 1, room - 1], [0] * 6, [2, 40, 100, 30, 7, 9], [a, 0, 3, room - 3, 0, room - 1], [a, s, room, 0, s - 1, room - 1]],
+                            dtype=torch.int32))
+    want = x.run(sp, rope)
+    assert all(torch.equal(i, j) for i, j in zip(got, want)) and torch.isfinite(got[1][[0, 2, 3, 4]]).all() and (got[0][1] == 0).all()
+
+
+@pytest.mark.parametrize("rope", [False, True])
+def test_captured_generation(sp, rope):
+    """A step (compression, token through norm and rotation, attention) captured once and replayed with the program's own eager calls between, against
+    the same steps one by one: the same bits, in the cache too."""
+    S, Hq, Hkv, L, d = 3, 8, 2, 400, 128
+    a, s, w, c = 2, 60, 40, 600
+    g = torch.Generator().manual_seed(3)
+    randn = lambda *shape: torch.randn(*shape, generator=g).to(torch.bfloat16).cuda()
+    freqs, table = sp.sepattn_rope_frequencies(d, BASE, device="cuda"), sp.sepkv_rope_table(c, d, BASE, "cuda")
+    weights = [(1 + 0.2 * torch.randn(d, generator=g)).cuda() for _ in range(2)]
+    sep = (torch.rand(S, L, generator=g) < 0.2).to(torch.uint8).cuda()
+    idx, _, pre = sp.sepattn_compact_indices(sep)
+    state = sp.sepkv_fill_from_prefill_mx(randn(S, Hkv, L, d), randn(S, Hkv, L, d), sep, idx, pre, Hq, a, s, w, c, 200)
+    tokens = [(randn(S, Hq, d), randn(S, Hkv, d), randn(S, Hkv, d)) for _ in range(8)]
+    q, k, v = (t.clone() for t in tokens[0])
+    pos, new = torch.zeros(S, dtype=torch.int32, device="cuda"), torch.ones(S, dtype=torch.uint8, device="cuda")
+    out, turned = (torch.empty_like(q), torch.empty(S, Hq, device="cuda")), torch.empty_like(q)
+    ws = torch.zeros(sp.sepattn_decode_mx_workspace_bytes(q, state[0], a, s, w), dtype=torch.uint8, device="cuda")
+
+    def step(cache, flags, sizes):
+        sp.sepkv_evict_window_mx(*cache, flags, sizes, Hq, a, s, w)
+        sp.sepkv_append_norm_rope_mx(q, k, v, new, None if rope else pos, *weights, None if rope else freqs, 1e-6, *cache, flags, sizes, a, s, w, out=turned)
+        if rope:
+            sp.sepattn_decode_rope_mx(turned, *cache, sizes, table, a, s, w, 0.1, out=out, ws=ws)
+        else:
+            sp.sepattn_decode_mx(turned, *cache, sizes, a, s, w, 0.1, out=out, ws=ws)
+
+    def enter(t):
+        for x, y in zip((q, k, v), tokens[t]):
+            x.copy_(y)
+        pos.fill_(L + t)
+
+    mine, eager = [t.clone() for t in state], [t.clone() for t in state]
+    step(mine[:4], *mine[4:])
+    for x, y in zip(mine, state):
+        x.copy_(y)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(mine[:4], *mine[4:])
+    for t in range(len(tokens)):
+        enter(t)
+        step(eager[:4], *eager[4:])
+        want = [x.clone() for x in (*out, turned)]
+        for x in (*out, turned):
+            x.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip((*out, turned), want)), t
+        assert all(torch.equal(x, y) for x, y in zip(mine, eager)), t

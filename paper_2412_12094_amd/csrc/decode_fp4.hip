@@ -16,7 +16,7 @@
 // 4.6 for the merge launch.  Shorter ones: vector instructions and the start.  A block is 190 of them (64 convert, 24 split the weights), with positions
 // 640: 128 form the angles, 128 turn, 192 split the turned keys.  A wave alone on its SIMD needs 1.8 us for a block with positions, three together 1.2
 // each, so kResident is as much as fits without a spill: a spilled register is waited for with every load before it.  32 sequences of 1 to 3277
-// entries, 60 MB, 17.9 us; with positions 29.6.  The other half of both is the start (launch, slice, first rows: 6 us) and the sum of the slices (4).
+// entries, 60 MB, 17.8 us; with positions 28.8.  The other half of both is the start (launch, slice, first rows: 6 us) and the sum of the slices (4).
 // The remainder of a cut number as one dot product of bf16 pairs instead of a mask and a subtraction took 72 instructions out of the 640 and changed no
 // time, nor did a second block on its way (d = 64: 17.4 -> 18.9).  The second halves of turned keys as fp32 products (16x16x4) instead of two parts: 96
 // instructions fewer, 29.8 -> 34.8: eight products that wait for each other.
@@ -254,6 +254,9 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, ROPE>)) void decode_f
         }
     }
 
+    typedef const __attribute__((address_space(1))) char *GlobalBytes;
+    auto turns = (GlobalBytes)rope;
+    asm volatile("" : "+s"(turns));  // (known as never written, its first loads would be moved behind the barriers)
     const int krow = 8 * (col >> 2) + (col & 3);  // this lane's rows of a block: krow, krow + 4
     struct Rows {
         RowCodes<D> k[2], v[2];
@@ -284,8 +287,7 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, ROPE>)) void decode_f
                 for (int ks = 0; ks < KS2; ++ks) rows.k[t][ks] = a[ks], rows.k[t][ks + KS2] = b[ks];
 #pragma unroll
                 for (int i = 0; i < D / 64; ++i)  // (4 c d < 2^32; beyond the end: masked)
-                    rows.base[t][i] = *reinterpret_cast<const float *>(reinterpret_cast<const char *>(rope) +
-                                                                       (size_t)((uint32_t)(max(nv - 1 - eb - 4 * t, 0) * D + 64 * i + lane) * 4u));
+                    rows.base[t][i] = *(const __attribute__((address_space(1))) float *)(turns + (size_t)((uint32_t)(max(nv - 1 - eb - 4 * t, 0) * D + 64 * i + lane) * 4u));
             } else {
                 rows.k[t] = __builtin_nontemporal_load(reinterpret_cast<const RowCodes<D> *>(Kc + (size_t)off));
             }
@@ -306,12 +308,14 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, ROPE>)) void decode_f
     float rc[KS2][8], rs[KS2][8];
     constexpr int STEP = NW * kRows;
     Rows rows;
-    auto request_first = [&] {
-        if (eb >= e1) return;
+    auto request_first = [&] {  // (of any slot where the wave has no block: behind a branch, as below, these loads would be waited for with all before)
         uint32_t slot[2];
         find_slots(eb, slot);
+        slot[0] = min(slot[0], (uint32_t)p.c - 1u), slot[1] = min(slot[1], (uint32_t)p.c - 1u);  // a sequence without entries has none to repeat
         request_keys(rows, eb, slot);
+        __builtin_amdgcn_sched_barrier(0);  // in the loop's order: else it waits for what the first round has on its way
         request_values(rows, slot);
+        __builtin_amdgcn_sched_barrier(0);
     };
     if constexpr (ROPE) {
         static_assert(kRows * D * 4 <= NW * STAGE, "the table's rows fit the stages");

@@ -444,3 +444,16 @@ def test_captured_generation(sp, rope):
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for x, y in zip((*out, turned), want)), t
         assert all(torch.equal(x, y) for x, y in zip(mine, eager)), t
+
+
+def test_one_workspace_for_calls_of_other_shapes(sp):
+    """What one call leaves in a workspace is where the next one counts its slices: every call gives the bits of one with a workspace of its own."""
+    xs = [Case(2, 8, 2, 128, "bf16", (2, 40, 30, 900), [900, 333], seed=1), Case(70, 3, 1, 64, "bf16", (2, 40, 30, 600), [600, 0, 1, 77, 410], seed=2),
+          Case(4, 12, 12, 64, "fp32", STREAM, [300, 211, 7, 150], seed=3)]
+    want = [x.run(sp, rope) for x in xs for rope in (False, True)]
+    need = max(sp.sepattn_decode_mx_workspace_bytes(x.q, x.cache[0], x.a, x.s, x.w) for x in xs)
+    ws = torch.randint(0, 256, (need,), dtype=torch.uint8, generator=torch.Generator().manual_seed(0)).cuda()
+    for _ in range(5):
+        got = [x.run(sp, rope, ws=ws) for x in xs for rope in (False, True)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for i, j in zip(got, want) for a, b in zip(i, j))

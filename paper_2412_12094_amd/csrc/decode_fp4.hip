@@ -88,6 +88,15 @@ __device__ inline void split_bf16(const f32x8 &x, bf16x8 (&part)[PARTS]) {
     part[PARTS - 1] = __builtin_convertvector(rest, bf16x8);
 }
 
+// Weights are 2^(x sl2 - m) by one fma, with m the rounded product of the largest x.  What that rounding left is in every exponent, up to half a step of m:
+// a common factor, which costs nothing until it leaves fp32 (m = 2^31: steps of 256).  From here on the products are rounded as m is.
+constexpr float kFarMaximum = 16777216.f;  // 2^24, steps of 2
+__device__ inline float rounded_product(float x, float y) {
+#pragma clang fp contract(off)
+    const float z = x * y;
+    return z;
+}
+
 template <typename T>
 struct Precision;
 template <>
@@ -445,11 +454,17 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, ROPE>)) void decode_f
             for (int db = 0; db < DB; ++db) acc[db] *= alpha;
             m_run = m_new;
         }
-        const float shift = m_run == -INFINITY ? 0.f : -m_run;
+        float factor = sl2, shift = m_run == -INFINITY ? 0.f : -m_run;
+        if (__builtin_amdgcn_ballot_w64(fabsf(shift) >= kFarMaximum)) {
+            const bool far = fabsf(shift) >= kFarMaximum;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = far ? rounded_product(x[i], sl2) + shift : x[i];
+            factor = far ? 1.f : factor, shift = far ? 0.f : shift;
+        }
         f32x8 pr;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            pr[i] = __builtin_amdgcn_exp2f(fmaf(x[i], sl2, shift));
+            pr[i] = __builtin_amdgcn_exp2f(fmaf(x[i], factor, shift));
             l_run += pr[i];
         }
         bf16x8 w[WP];

@@ -294,7 +294,7 @@ int sepattn_rope_backward(const sepattn_rope_params *p, const double *freqs, con
  *     dx = r (u - x r^2 mean(u x)),   dw = sum over all rows of g x r   (V's gradient is moved as it is).
  * The sum for dw has a fixed order: two calls give the same bits on one GPU.
  *   p->rotary_dim   even, 0 <= rotary_dim <= d (SEPATTN_ERR_PARAM otherwise); 0: normed only, freqs may be NULL
- *   p->eps          finite, >= 0 (SEPATTN_ERR_PARAM otherwise).  With eps = 0 a row of zeros gives NaN, as the formula does
+ *   p->eps          0 <= eps <= 1e30 (SEPATTN_ERR_PARAM otherwise).  With eps = 0 a row of zeros gives NaN, as the formula does
  *   q_weight, k_weight   DEVICE [d] in p->weight_dtype (bf16 or fp32, whatever p->dtype is), or NULL: ones
  *   q, k            of the backward call: the rows that the forward call read
  *   dq_weight, dk_weight DEVICE fp32 [d]  out, each may be NULL

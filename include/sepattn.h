@@ -516,9 +516,12 @@ int sepkv_fill_from_prefill_zeroed(const sepkv_params *p, int L, int nw, const v
  *   scales  d/32 bytes: the values of dimensions 32b .. 32b+31 are the codes' times 2^(byte b - 127) (E8M0); 255: all of them are NaN
  * Rounding a row to it: 2^(E-2) with E the exponent of the block's largest magnitude after that is rounded to two bits of significand
  * (7/4 2^E stays, anything above counts as 2^(E+1)), kept within 2^-125 .. 2^125; then each value over it to the nearest magnitude, ties to the
- * even code, values above 6 (up to 7, or beyond the largest scale) to 6.  So a value is off by at most half the step around it (1/4, 1/2 or 1 times
- * the scale), the scale being at most 2/7 of the block's largest magnitude.  A block with an infinity or a NaN becomes NaN.  Every value is
- * exact in bf16 and fp32.
+ * even code, values above 6 to 6.  So a value is off by at most half the step around it (1/4, 1/2 or 1 times the scale; magnitudes above 7 2^125, which become
+ * 6 2^125, by more), the scale being 2^-125 or at most 2/7 of the block's largest magnitude.  A block with an infinity or a NaN becomes NaN, and every other
+ * value is exact in bf16 and fp32.
+ * Scale bytes written here are 2 .. 252 and 255.  A cache from elsewhere may hold the others: 0 and 1, some of whose values are subnormal, are read exactly too; with
+ * 253 and 254 magnitudes of 2^128 and more are infinite in sepkv_expand_mx, and a decode gives a query head that sees such a key, or a dimension of a value, no
+ * defined result, all others theirs.
  *   Kc, Vc   DEVICE uint8 [S, Hkv, c, d/2], 16-byte aligned;   Ks, Vs   DEVICE uint8 [S, Hkv, c, d/32], aligned to d/32
  * p->dtype is the type of all other tensors (k_new, q, out, ...).
  *

@@ -3,7 +3,8 @@
 // The power of two of a block is that of its largest magnitude, rounded to the two bits of significand that an element has, so that the
 // largest element falls on 4 or 6 and nothing is off by more than half a step: bits of a float + 0x1FFFFF carry into the exponent above 7/4.
 // It is kept within 2^-125 .. 2^125, where every product of element and power is a normal bf16 (and fp32) number: reading a cache rounds
-// nothing.  Elements are rounded to nearest, ties to the even code, and end at 6; a block that holds an infinity or a NaN gets the byte 255,
+// nothing.  (The conversions read the exponent bits of a scale alone: bytes 0 and 1, which other encoders write, come out right, with their subnormal
+// values.)  Elements are rounded to nearest, ties to the even code, and end at 6; a block that holds an infinity or a NaN gets the byte 255,
 // for which the conversion instructions give NaN.  Both directions are single instructions for two values.
 #pragma once
 

@@ -531,9 +531,10 @@ int sepkv_fill_from_prefill_zeroed(const sepkv_params *p, int L, int nw, const v
  *   p->dtype first, so that the cache holds what the separate calls would leave.
  * sepkv_evict_window_mx: as sepkv_evict_window (bit-exact rows); p->dtype is not looked at beyond its check.
  * sepkv_expand_mx: the values of all valid entries, in their slots: K, V  DEVICE dtype [S, Hkv, c, d]  out; other slots receive 0.
- * sepattn_decode_mx, sepattn_decode_rope_mx: as sepattn_decode, _rope, over the cache's values.  lse holds to 1e-5 in bf16 too, also with positions
- *   (sepattn_decode rounds its weights to bf16 once, here they have 16 bits).  Any number of query heads per KV head.  The workspace may hold anything
- *   and is left in no particular state; calls that overlap in time need one each.
+ * sepattn_decode_mx, sepattn_decode_rope_mx: as sepattn_decode, _rope, over the cache's values.  With A the largest scale * sum over the dimensions of
+ *   |q| |k| of a row's entries (with positions: |k| and its partner's), lse is off by at most 2^-16 A (with positions in bf16 2^-15 A) and the roundings of
+ *   fp32, 2^-20 and 2^-22 of itself.  The weights have 16 bits or more (sepattn_decode rounds them to bf16 once).
+ *   Any number of query heads per KV head.  The workspace may hold anything and is left in no particular state; calls that overlap in time need one each.
  *   NaN in a query or in the cache reaches the results that see it, and no others.  Scores and the weighted sums of values are fp32 until the end:
  *   keys and values of magnitudes above 2^95 may overflow them in a full cache.
  * ------------------------------------------------------------------------------------------ */
@@ -597,8 +598,9 @@ int sepattn_decode_rope_mx(const sepkv_params *p, const void *q, const void *Kc,
  * oldest first, are at positions 0 .. np-1, its own at np .. np+nv-1, the query at np+nv-1.  The positions of a
  * prefix never change, so its keys are turned once, by sepkv_rope_cache, and Kp holds them turned; own keys and q are
  * stored without encoding.  rope_table needs n_pos >= pp->c + p->c rows (SEPATTN_ERR_SHAPE).  The turned query and turned own keys
- * count with 16 bits or more of mantissa, so that lse holds to 1e-5 for Kp as it is.  In bf16 sepkv_rope_cache rounds a turned key, by 2^-8 of it at
- * most; against keys that are not rounded there lse is off by about 1e-4 behind thousands of entries, 1e-3 behind a few.
+ * count with 16 bits or more of mantissa: with A the largest scale * sum over the dimensions of |q| |k| of a row's entries (turned), lse is off by at
+ * most 2^-15 A (fp32, and bf16 without positions: 2^-16 A), 2^-20 and 2^-22 of itself, for Kp as it is.  In bf16 sepkv_rope_cache rounds a turned key, by 2^-8 of it at
+ * most; against keys that are not rounded there lse is off by about 1e-4 behind thousands of entries, 1e-3 behind a few (values of order one).
  *   sepkv_rope_cache: the key of the entry of rank e (oldest first) is turned by table row e, for all valid entries of
  *                Kc DEVICE dtype [S, Hkv, c, d] -> K_out, of the same shape, which may be Kc (in place: once).  Slots without a
  *                valid entry are not written.  n_pos >= c.

@@ -535,6 +535,8 @@ int sepkv_fill_from_prefill_zeroed(const sepkv_params *p, int L, int nw, const v
  *   |q| |k| of a row's entries (with positions: |k| and its partner's), lse is off by at most 2^-16 A (with positions in bf16 2^-15 A) and the roundings of
  *   fp32, 2^-20 and 2^-22 of itself.  The weights have 16 bits or more (sepattn_decode rounds them to bf16 once).
  *   Any number of query heads per KV head.  The workspace may hold anything and is left in no particular state; calls that overlap in time need one each.
+ *   Sequences are cut into slices by their lengths as long as a batch leaves workgroups for that; in one of many sequences (from 182 at 8 KV heads, 38 at 32
+ *   on, and above 512 always) a sequence is walked by one workgroup per KV head and 16 query heads, and one long sequence among short ones decides the time.
  *   NaN in a query or in the cache reaches the results that see it, and no others.  Scores and the weighted sums of values are fp32 until the end:
  *   keys and values of magnitudes above 2^95 may overflow them in a full cache.
  * ------------------------------------------------------------------------------------------ */

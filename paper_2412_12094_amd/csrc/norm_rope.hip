@@ -9,7 +9,8 @@
 // of partial sums, which a second kernel adds in fp64, in a fixed order, so that two runs give the same bits.
 //
 // Memory bounds both.  8192 tokens, 32 + 8 heads of 128, bf16: forward 201 MB in 37 us, 5.4 TB/s (rope.hip without the norm: 36); backward 285 MB in
-// 58 us, 4.9 TB/s, and 4.9 for the second kernel.  8 x 2048 tokens, 12 + 12 heads of 64: backward 201 MB in 43 us.  fp32, 4096 tokens: 56 us both.
+// 58 us, 4.9 TB/s, and 4.9 for the second kernel.  8 x 2048 tokens, 12 + 12 heads of 64: backward 201 MB in 43 us.  fp32, 4096 tokens, 32 + 8 heads of 128:
+// forward 35 us, backward 52, and 4.7.
 // The forward's registers decide: with the weights behind a branch per dimension it took 140 of them and 41 us, with one branch 96 and 37.
 #include "norm.h"
 

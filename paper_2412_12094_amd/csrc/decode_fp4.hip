@@ -16,7 +16,7 @@
 // 4.6 for the merge launch.  Shorter ones: vector instructions and the start.  A block is 190 of them (64 convert, 24 split the weights), with positions
 // 640: 128 form the angles, 128 turn, 192 split the turned keys.  A wave alone on its SIMD needs 1.8 us for a block with positions, three together 1.2
 // each, so kResident is as much as fits without a spill: a spilled register is waited for with every load before it.  32 sequences of 1 to 3277
-// entries, 60 MB, 17.8 us; with positions 28.8.  The other half of both is the start (launch, slice, first rows: 6 us) and the sum of the slices (4).
+// entries, 60 MB, 17.9 us; with positions 28.9.  The other half of both is the start (launch, slice, first rows: 6 us) and the sum of the slices (4).
 // The remainder of a cut number as one dot product of bf16 pairs instead of a mask and a subtraction took 72 instructions out of the 640 and changed no
 // time, nor did a second block on its way (d = 64: 17.4 -> 18.9).  The second halves of turned keys as fp32 products (16x16x4) instead of two parts: 96
 // instructions fewer, 29.8 -> 34.8: eight products that wait for each other.
